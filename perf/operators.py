@@ -295,7 +295,8 @@ def _plain_quant(s):
     x, c = s["x"].float(), s["case"]
     b = _blocks(x, c["block_rows"])
     top = b.abs().amax((1, 3))
-    scale = torch.where(top == 0, torch.ones_like(top), top / 448.0)
+    scale = top / 448.0
+    scale = torch.where(scale == 0, 1.0, scale)
     q = (b / scale[:, None, :, None]).clamp(-448, 448).view(-1, b.shape[2] * 128)[: c["m"], : c["k"]]
     return q.to(torch.float8_e4m3fn), scale
 
