@@ -17,7 +17,13 @@
  *   - decode fused with the matrix product, the decoded weights never written
  *     as a whole (ep_decode_matmul_i8 for a few int8 rows of X;
  *     ep_decode_gemm_i8 and ep_decode_gemm_bf16 on the matrix cores for any
- *     number of rows; App. D).
+ *     number of rows; App. D),
+ *   - the operators of an attention layer served in 8 bits, next to decoded
+ *     FP8 weights: activations to FP8 with a scale for each block of 128
+ *     (ep_quant_fp8_block), the FP8 product with such scales
+ *     (ep_gemm_fp8_block), and a paged 8-bit key/value cache: its block tables
+ *     and slot maps (ep_kv8_slots), its writer (ep_kv8_append) and the
+ *     attention that reads it (ep_kv8_attention).
  *
  * Conventions shared by every entry point:
  *   - Return value: EP_OK (0) or a negative ep_status.  ep_last_error() gives a
@@ -98,7 +104,11 @@ enum ep_container {
 enum ep_status_bits {
   EP_STATUS_PAYLOAD_OVERRUN = 1,  /* a tile tried to read past its payload window */
   EP_STATUS_BAD_FINAL_STATE = 2,  /* a terminal state was not 2^15 after decoding */
-  EP_STATUS_BAD_END_OFFSET = 4    /* a tile ended before its successor's offset */
+  EP_STATUS_BAD_END_OFFSET = 4,   /* a tile ended before its successor's offset */
+  /* set by ep_kv8_slots */
+  EP_STATUS_NO_PAGES = 8,         /* a request was refused: the free pages ran out */
+  EP_STATUS_TABLE_FULL = 16,      /* a request was refused: its row of the table is too short */
+  EP_STATUS_SLOTS_FULL = 32       /* a request was refused: its tokens pass the slot map's end */
 };
 
 /* ---- encoder ------------------------------------------------------------- */
@@ -424,6 +434,163 @@ int ep_stack_decode(const ep_stack* stack, int32_t* d_status, void* hip_stream);
  * memset node (graph capture is safe).  Errors: EP_ERR_ARG, EP_ERR_HIP. */
 int ep_gemm_i8_nt(const int8_t* d_a, const int8_t* d_b, int32_t* d_y, int64_t m, int64_t n,
                   int64_t k, void* hip_stream);
+
+/* ---- FP8 product with block scales ---------------------------------------- */
+/* Activations (or weights) to FP8 E4M3 with one FP32 scale for each block of
+ * block_rows (1 or 128) rows and 128 columns; the last block of a row or column
+ * may be partial.  With amax the block's largest magnitude:
+ *   scale = fp32(amax / 448), or 1 where that is zero;
+ *   q     = E4M3(fp32(x / scale)), round to nearest even.
+ * A block that holds a NaN or an infinity gets a scale that is one, so its values
+ * do not pass as finite.  d_x: m rows of k elements (x_dtype EP_BF16, EP_FP16 or
+ * EP_FP32), x_row elements from one row to the next (x_row >= k; 16-byte aligned
+ * rows); d_q: m x k bytes, row-major, 16-byte aligned; d_scale: ceil(m /
+ * block_rows) x ceil(k / 128) floats, row-major.  m may be 0 (nothing is done).
+ * Asynchronous on hip_stream, no allocation, one launch.
+ * Errors: EP_ERR_ARG (null or misaligned pointers, m < 0, k <= 0, k % 16,
+ * x_row < k, block_rows other than 1 and 128, another dtype), EP_ERR_HIP. */
+int ep_quant_fp8_block(const void* d_x, int x_dtype, int64_t m, int64_t k, int64_t x_row,
+                       int block_rows, void* d_q, float* d_scale, void* hip_stream);
+
+/* What the scales of W in ep_gemm_fp8_block belong to. */
+enum ep_scale_layout {
+  EP_SCALE_BLOCK = 1,      /* ceil(n/128) x ceil(k/128): 128 x 128 blocks */
+  EP_SCALE_ROW_BLOCK = 2,  /* n x ceil(k/128): 128 values of one row */
+  EP_SCALE_ROW = 3         /* n: a row (delta_r of a decoded FP8 row container) */
+};
+
+/* Y[i][j] = sum_b xs[i][b] * ws(j, b) * sum_{p in block b} X[i][p] * W[j][p],
+ * b running over the blocks of 128 along k.  X: m x k E4M3 with d_x_scale m x
+ * ceil(k/128) as ep_quant_fp8_block writes them with block_rows 1; W: n x k,
+ * w_dtype EP_FP8_E4M3 or EP_FP8_E5M2 (for example the output of ep_decode_tiles),
+ * with d_w_scale in layout w_scales; Y: m x n of y_dtype EP_BF16, EP_FP16 or
+ * EP_FP32 (round to nearest even; a sum beyond the type's range becomes an
+ * infinity).  All row-major; X and W 16-byte aligned.  Every block's sum is scaled
+ * in FP32 and the blocks are added in FP32 in an order fixed by the shape, so equal
+ * calls give equal bits.  BF16 and FP16 outputs sum their blocks on the FP8 matrix
+ * instructions, which carry fewer bits than FP32 (measured: off by 1.4e-5 of a
+ * block of Gaussian codes, 5e-5 of uniform ones, well below those types' own
+ * rounding).  FP32 outputs take FP16 instructions with FP32 sums, into which both
+ * FP8 types widen exactly, at half the rate.  m may be 0 (nothing is done).  Asynchronous on hip_stream, no allocation,
+ * no workspace, one launch.
+ * Errors: EP_ERR_ARG (null or misaligned pointers, m < 0, n <= 0, k <= 0,
+ * k % 16, m, n or k above 2^24, another dtype or layout), EP_ERR_HIP. */
+int ep_gemm_fp8_block(const void* d_x, const float* d_x_scale, const void* d_w, int w_dtype,
+                      const float* d_w_scale, int w_scales, void* d_y, int y_dtype, int64_t m,
+                      int64_t n, int64_t k, void* hip_stream);
+
+/* ---- paged 8-bit key/value cache ------------------------------------------ */
+/* A cache of one layer in pages of page_tokens tokens (16, 32, 64, 128 or 256),
+ * with one FP32 scale for each page and head: a key or value is scale * code.
+ * Slot s = page * page_tokens + offset names a token's place in it.  Keys lie
+ * token by token, values channel by channel, so that both products of an
+ * attention read along their sums.  All arrays are device memory owned by the
+ * caller; codes 16-byte aligned. */
+typedef struct {
+  void* d_k;               /* [n_pages][kv_heads][page_tokens][head_dim] codes */
+  void* d_v;               /* [n_pages][kv_heads][head_dim][page_tokens] codes */
+  float* d_k_scale;        /* [n_pages][kv_heads] */
+  float* d_v_scale;        /* [n_pages][kv_heads] */
+  int64_t n_pages;         /* below 2^31 */
+  int32_t kv_heads;
+  int32_t page_tokens;
+  int32_t head_dim;        /* 64, 128 or 256 */
+  int32_t dtype;           /* EP_FP8_E4M3 or EP_INT8 (codes -127 .. 127) */
+} ep_kv8_cache;
+
+/* Give the new tokens of n_req requests their places: block tables and slot maps
+ * from lengths that are on the device.  Request b holds d_cached[b] tokens in the
+ * cache and brings d_new[b] more (negative counts read as 0, of *d_n_free too).  With T =
+ * page_tokens, have = ceil(cached / T) and want = ceil((cached + new) / T), it
+ * needs want - have pages.  Requests take them from d_free (page numbers, *d_n_free
+ * of them) in order: request b's are d_free[off .. off + need), off the need of
+ * the requests before it.  A request is refused if want > table_ld
+ * (EP_STATUS_TABLE_FULL), if its tokens end past n_slots (EP_STATUS_SLOTS_FULL; such
+ * requests need no pages) or if off + need passes *d_n_free with need > 0
+ * (EP_STATUS_NO_PAGES).  Written:
+ *   d_table [n_req][table_ld] : entries have .. want - 1 of each admitted row; the
+ *                               others stay (0 .. have - 1 are read)
+ *   d_len   [n_req]           : cached + new, or cached where refused
+ *   d_cu    [n_req + 1]       : sums of the requests' new tokens before each, and
+ *                               in all (refused ones included: the tokens of the
+ *                               batch keep their places; at most 2^31 - 1)
+ *   d_slots [n_slots]         : for each new token, in order, its slot; -1 for the
+ *                               tokens of refused requests and past the last token
+ *   d_used  [1]               : pages taken from d_free
+ *   *d_status (nullable, zeroed by the caller): the bits above, OR-ed
+ * Outputs must not alias inputs.  Asynchronous on hip_stream, one launch.
+ * Errors: EP_ERR_ARG (null pointers, n_req <= 0, page_tokens, table_ld <= 0,
+ * n_slots outside 0 .. 2^31 - 1), EP_ERR_HIP. */
+int ep_kv8_slots(const int32_t* d_cached, const int32_t* d_new, int64_t n_req, int page_tokens,
+                 const int32_t* d_free, const int32_t* d_n_free, int32_t* d_table, int64_t table_ld,
+                 int32_t* d_len, int32_t* d_cu, int64_t* d_slots, int64_t n_slots, int32_t* d_used,
+                 int32_t* d_status, void* hip_stream);
+
+/* Write new keys and values into their slots.  d_k, d_v: n_tokens rows of kv_heads
+ * x head_dim elements (dtype EP_BF16, EP_FP16 or EP_FP32; heads contiguous), k_row
+ * and v_row elements from one token to the next (16-byte aligned rows), so that
+ * both may lie in one fused projection's output.  d_slots[t]: the token's slot, as
+ * ep_kv8_slots gives it; tokens with a slot outside the cache (-1) are skipped.
+ * The tokens that fall into one page must be consecutive in d_slots and take
+ * consecutive offsets.  With o the first one's offset and top = 448 or 127, each
+ * page and head gets
+ *   scale' = max(scale if o > 0 else 0, fp32(amax of the new values / top))
+ * the tokens before o are carried over as code' = round(fp32(fp32(code * scale) /
+ * scale')) (unchanged where the scale does not grow), the new ones are round(fp32(x
+ * / scale')): to nearest even, saturating, and 0 where scale' is 0.  A NaN or
+ * infinity among the new values of a page and head makes its scale one and with it
+ * the page's values for that head.
+ * n_tokens may be 0.  Asynchronous on hip_stream, one launch.
+ * Errors: EP_ERR_ARG (null or misaligned pointers, a bad cache, rows shorter than
+ * kv_heads * head_dim or misaligned, another dtype), EP_ERR_HIP. */
+int ep_kv8_append(const ep_kv8_cache* cache, const void* d_k, const void* d_v, int dtype,
+                  int64_t k_row, int64_t v_row, const int64_t* d_slots, int64_t n_tokens,
+                  void* hip_stream);
+
+/* One attention call over such a cache. */
+typedef struct {
+  const void* d_q;         /* total_q rows of q_heads x head_dim, q_row elements apart */
+  void* d_out;             /* the same of dtype, out_row elements apart */
+  float* d_lse;            /* nullable: [total_q][q_heads], log of the row's sum of exponentials */
+  const int32_t* d_cu_q;   /* [n_req + 1]: request b's queries are rows cu_q[b] .. cu_q[b + 1] */
+  const int32_t* d_len;    /* [n_req]: tokens in the cache, the queries' own among them */
+  const int32_t* d_table;  /* [n_req][table_ld]: page of tokens i * page_tokens .. */
+  int64_t table_ld;
+  int64_t n_req;
+  int64_t total_q;
+  int64_t q_row, out_row;  /* 0: packed, q_heads * head_dim */
+  int32_t q_heads;         /* a multiple of kv_heads; head h reads kv head h / (q_heads / kv_heads) */
+  int32_t dtype;           /* EP_BF16 or EP_FP16: queries and outputs */
+  int32_t causal;          /* nonzero: query i of m sees keys up to position len - m + i */
+  int32_t window;          /* > 0 (causal only): and no more than this many of them, itself included */
+  int32_t max_q;           /* the most queries of a request and the most tokens of one, as far as */
+  int32_t max_len;         /*  the host knows: they size the launch, and may be exceeded */
+  float scale;             /* of the scores, usually 1 / sqrt(head_dim) */
+  int32_t reserved;
+} ep_kv8_attn;
+
+/* Device bytes ep_kv8_attention needs for this call (0 for a bad one): partial
+ * results of requests whose keys are shared out over workgroups. */
+uint64_t ep_kv8_attention_workspace(const ep_kv8_cache* cache, const ep_kv8_attn* call);
+
+/* Softmax attention of queries over the cache:
+ *   out_i = sum_j exp(scale q_i . k_j) v_j / sum_j exp(scale q_i . k_j)
+ * over the keys j that query i sees: positions 0 .. len - 1 of its request, and
+ * what causal and window leave of them.  A row that sees none (a length of 0, a
+ * causal query before the first key) is 0 with lse -infinity.  Codes, scales and
+ * pages beyond a request's length may hold anything.  Table entries outside the
+ * cache count as unseen.  Scores, softmax statistics and sums are FP32; the codes
+ * enter the matrix instructions exactly, a query with all 11 bits of FP16 (scaled
+ * by a power of two for each row, its sums scaled back), a weight p rounded to
+ * 11 bits (22 where a call has few query rows).  Outputs round to nearest even.
+ * d_workspace: >= ep_kv8_attention_workspace bytes of device memory (nullable if
+ * that is 0), 16-byte aligned, not shared by calls that overlap.  Equal calls give
+ * equal bits.  total_q may be 0.  Asynchronous on hip_stream, no allocation, at
+ * most two launches.
+ * Errors: EP_ERR_ARG (null or misaligned pointers, a bad cache or call, rows
+ * shorter than q_heads * head_dim or misaligned, a short workspace), EP_ERR_HIP. */
+int ep_kv8_attention(const ep_kv8_cache* cache, const ep_kv8_attn* call, void* d_workspace,
+                     uint64_t ws_bytes, void* hip_stream);
 
 /* ---- errors -------------------------------------------------------------- */
 const char* ep_last_error(void);

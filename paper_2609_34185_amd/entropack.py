@@ -22,6 +22,8 @@ OK, ERR_ARG, ERR_FORMAT, ERR_UNSUPPORTED, ERR_NOMEM, ERR_HIP, ERR_CORRUPT = 0, -
 BF16, FP16, FP32, FP8_E4M3, INT8, FP8_E5M2, UINT8, COORD2_I32 = 1, 2, 3, 4, 5, 6, 7, 100
 CONT_DIRECT, CONT_FP8_ROW, CONT_INT8_ROW, CONT_FP8E5M2_ROW, CONT_UINT8_TENSOR = 0, 1, 2, 3, 4
 STATUS_PAYLOAD_OVERRUN, STATUS_BAD_FINAL_STATE, STATUS_BAD_END_OFFSET = 1, 2, 4
+STATUS_NO_PAGES, STATUS_TABLE_FULL, STATUS_SLOTS_FULL = 8, 16, 32
+SCALE_BLOCK, SCALE_ROW_BLOCK, SCALE_ROW = 1, 2, 3
 
 ITEMSIZE = {BF16: 2, FP16: 2, FP32: 4, FP8_E4M3: 1, INT8: 1, FP8_E5M2: 1, UINT8: 1, COORD2_I32: 4}
 
@@ -78,6 +80,22 @@ class Stack(C.Structure):
                 ("reserved", C.c_uint32 * 4)]
 
 
+class Kv8Cache(C.Structure):
+    _fields_ = [("d_k", C.c_void_p), ("d_v", C.c_void_p), ("d_k_scale", C.c_void_p),
+                ("d_v_scale", C.c_void_p), ("n_pages", C.c_int64), ("kv_heads", C.c_int32),
+                ("page_tokens", C.c_int32), ("head_dim", C.c_int32), ("dtype", C.c_int32)]
+
+
+class Kv8Attn(C.Structure):
+    _fields_ = [("d_q", C.c_void_p), ("d_out", C.c_void_p), ("d_lse", C.c_void_p),
+                ("d_cu_q", C.c_void_p), ("d_len", C.c_void_p), ("d_table", C.c_void_p),
+                ("table_ld", C.c_int64), ("n_req", C.c_int64), ("total_q", C.c_int64),
+                ("q_row", C.c_int64), ("out_row", C.c_int64), ("q_heads", C.c_int32),
+                ("dtype", C.c_int32), ("causal", C.c_int32), ("window", C.c_int32),
+                ("max_q", C.c_int32), ("max_len", C.c_int32), ("scale", C.c_float),
+                ("reserved", C.c_int32)]
+
+
 class EntroPackError(RuntimeError):
     def __init__(self, code: int, what: str, msg: str):
         super().__init__(f"{what}: status {code}: {msg}")
@@ -127,6 +145,13 @@ def lib():
         L.ep_decode_gemm_bf16_workspace.restype = u64
         L.ep_decode_gemm_i8_workspace.argtypes = [C.POINTER(TensorInfo)]
         L.ep_decode_gemm_i8_workspace.restype = u64
+        L.ep_quant_fp8_block.argtypes = [vp, C.c_int, i64, i64, i64, C.c_int, vp, vp, vp]
+        L.ep_gemm_fp8_block.argtypes = [vp, vp, vp, C.c_int, vp, C.c_int, vp, C.c_int, i64, i64, i64, vp]
+        L.ep_kv8_slots.argtypes = [vp, vp, i64, C.c_int, vp, vp, vp, i64, vp, vp, vp, i64, vp, vp, vp]
+        L.ep_kv8_append.argtypes = [C.POINTER(Kv8Cache), vp, vp, C.c_int, i64, i64, vp, i64, vp]
+        L.ep_kv8_attention_workspace.argtypes = [C.POINTER(Kv8Cache), C.POINTER(Kv8Attn)]
+        L.ep_kv8_attention_workspace.restype = u64
+        L.ep_kv8_attention.argtypes = [C.POINTER(Kv8Cache), C.POINTER(Kv8Attn), vp, u64, vp]
         L.ep_last_error.restype = C.c_char_p
         _lib = L
     return _lib
@@ -140,6 +165,8 @@ EXPORTS = ["ep_encode_params_default", "ep_encode_cpu", "ep_encode_gpu", "ep_blo
            "ep_decode_gemm_i8_prepare", "ep_decode_gemm_i8_prepared",
            "ep_decode_gemm_bf16", "ep_decode_gemm_bf16_workspace", "ep_decode_gemm_bf16_prepare",
            "ep_decode_gemm_bf16_prepared",
+           "ep_quant_fp8_block", "ep_gemm_fp8_block", "ep_kv8_slots", "ep_kv8_append",
+           "ep_kv8_attention_workspace", "ep_kv8_attention",
            "ep_last_error"]
 
 
@@ -323,6 +350,68 @@ def decode_gemm_bf16_prepared(info: TensorInfo, d_blob: int, d_x: int, m: int, d
     _check(lib().ep_decode_gemm_bf16_prepared(C.byref(info), d_blob, d_x, m, d_y, d_dequant or None,
                                               d_ws, ws_bytes, d_status or None, stream or None),
            "ep_decode_gemm_bf16_prepared")
+
+
+def quant_fp8_block(d_x: int, x_dtype: int, m: int, k: int, d_q: int, d_scale: int,
+                    block_rows: int = 1, x_row: int | None = None, stream: int = 0):
+    """X (m x k, rows x_row elements apart) to E4M3 codes and FP32 scales of its blocks of
+    block_rows x 128."""
+    _check(lib().ep_quant_fp8_block(d_x or None, x_dtype, m, k, k if x_row is None else x_row, block_rows,
+                                    d_q or None, d_scale or None, stream or None), "ep_quant_fp8_block")
+
+
+def gemm_fp8_block(d_x: int, d_x_scale: int, d_w: int, d_w_scale: int, d_y: int, m: int, n: int,
+                   k: int, w_dtype: int = FP8_E4M3, w_scales: int = SCALE_BLOCK, y_dtype: int = BF16,
+                   stream: int = 0):
+    """Y (m x n) = X (m x k E4M3) times W (n x k FP8) transposed, with X's scales for each row
+    and block of 128 and W's in layout w_scales."""
+    _check(lib().ep_gemm_fp8_block(d_x or None, d_x_scale or None, d_w or None, w_dtype,
+                                   d_w_scale or None, w_scales, d_y or None, y_dtype, m, n, k,
+                                   stream or None), "ep_gemm_fp8_block")
+
+
+def kv8_cache(d_k: int, d_v: int, d_k_scale: int, d_v_scale: int, n_pages: int, kv_heads: int,
+              page_tokens: int, head_dim: int, dtype: int = FP8_E4M3) -> Kv8Cache:
+    """Describe one layer's paged 8-bit cache (the arrays stay the caller's)."""
+    return Kv8Cache(d_k, d_v, d_k_scale, d_v_scale, n_pages, kv_heads, page_tokens, head_dim, dtype)
+
+
+def kv8_slots(d_cached: int, d_new: int, n_req: int, page_tokens: int, d_free: int, d_n_free: int,
+              d_table: int, table_ld: int, d_len: int, d_cu: int, d_slots: int, n_slots: int,
+              d_used: int, d_status: int = 0, stream: int = 0):
+    """Pages and slots of the new tokens of n_req requests (block tables, slot map, lengths)."""
+    _check(lib().ep_kv8_slots(d_cached or None, d_new or None, n_req, page_tokens, d_free or None,
+                              d_n_free or None, d_table or None, table_ld, d_len or None, d_cu or None,
+                              d_slots or None, n_slots, d_used or None, d_status or None,
+                              stream or None), "ep_kv8_slots")
+
+
+def kv8_append(cache: Kv8Cache, d_k: int, d_v: int, dtype: int, k_row: int, v_row: int, d_slots: int,
+               n_tokens: int, stream: int = 0):
+    """Quantise n_tokens keys and values into their slots of the cache."""
+    _check(lib().ep_kv8_append(C.byref(cache), d_k or None, d_v or None, dtype, k_row, v_row,
+                               d_slots or None, n_tokens, stream or None), "ep_kv8_append")
+
+
+def kv8_attention_args(d_q: int, d_out: int, d_cu_q: int, d_len: int, d_table: int, table_ld: int,
+                       n_req: int, total_q: int, q_heads: int, dtype: int, scale: float,
+                       causal: bool = True, window: int = 0, max_q: int = 1, max_len: int = 1,
+                       q_row: int = 0, out_row: int = 0, d_lse: int = 0) -> Kv8Attn:
+    """Describe one attention call.  q_row and out_row are elements from one token to the next
+    (0: packed rows of q_heads x head_dim)."""
+    return Kv8Attn(d_q or None, d_out or None, d_lse or None, d_cu_q or None, d_len or None,
+                   d_table or None, table_ld, n_req, total_q, q_row, out_row, q_heads, dtype, int(causal),
+                   window, max_q, max_len, scale, 0)
+
+
+def kv8_attention_workspace(cache: Kv8Cache, call: Kv8Attn) -> int:
+    return int(lib().ep_kv8_attention_workspace(C.byref(cache), C.byref(call)))
+
+
+def kv8_attention(cache: Kv8Cache, call: Kv8Attn, d_ws: int, ws_bytes: int, stream: int = 0):
+    """Attention of call's queries over the cache."""
+    _check(lib().ep_kv8_attention(C.byref(cache), C.byref(call), d_ws or None, ws_bytes,
+                                  stream or None), "ep_kv8_attention")
 
 
 # ---- torch conveniences (device memory and streams only) ------------------------

@@ -1,0 +1,301 @@
+"""GPU tests of FP8 with a scale for each block of 128: the quantiser (ep_quant_fp8_block), bit
+for bit against its definition in numpy, and the product (ep_gemm_fp8_block) against a product
+in 64 bits, every element within a bound that is derived from how it sums.
+
+The product's bound: with S = sum_p |xs ws X W| over all of k, the 128 exact products of a block
+are summed in FP32 in any order, each addition off by at most 2^-23 of what it adds up (a
+truncating adder included); scaling a block and adding it to the others costs a rounding of
+2^-24 for the scales' product and one for each block.  So |Y - exact| <= (256 + kb + 4) 2^-24 S,
+kb the blocks of k, before Y is rounded to its type: half a unit, 2^-8 of a BF16 value, 2^-11 of
+an FP16 one (or half its smallest step, 2^-25).  BF16 and FP16 outputs come from FP8 matrix
+instructions, which add in fewer bits than FP32 (off by 1.4e-5 of a block of such inputs); their
+own rounding hides it, and they are held to the same bound.
+"""
+import sys
+
+import numpy as np
+import pytest
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+
+
+def say(*a):
+    print(*a, flush=True, file=sys.stderr)
+
+
+@pytest.fixture(scope="module")
+def E():
+    from paper_2609_34185_amd import entropack
+    assert torch.cuda.is_available(), "GPU tests need a HIP device"
+    entropack.lib()
+    return entropack
+
+
+def stream():
+    return torch.cuda.current_stream().cuda_stream
+
+
+# ---- quantiser ------------------------------------------------------------------------
+def e4m3_codes(v):
+    """E4M3 codes of float32 values: nearest, halves to even, at most 448 (no NaN among them)."""
+    a = np.minimum(np.abs(v.astype(np.float64)), 448.0)
+    e = np.maximum(np.frexp(np.maximum(a, 1e-300))[1] - 1, -6)
+    n = np.rint(np.ldexp(a, 3 - e)).astype(np.int64)          # in steps of 2^(e - 3)
+    code = np.where(n >= 16, ((e + 8) << 3), np.where(n >= 8, ((e + 7) << 3) + (n - 8), n))
+    return (code | np.where(np.signbit(v), 0x80, 0)).astype(np.uint8)
+
+
+def quant_ref(x, block_rows):
+    """Codes and scales of float32 x by the definition, in float32 arithmetic."""
+    m, k = x.shape
+    pm, pk = -m % block_rows, -k % 128
+    b = np.pad(x, ((0, pm), (0, pk))).reshape((m + pm) // block_rows, block_rows, (k + pk) // 128, 128)
+    s = (np.abs(b).max((1, 3)) / np.float32(448)).astype(np.float32)
+    s = np.where(s == 0, np.float32(1), s)
+    q = e4m3_codes((b / s[:, None, :, None]).astype(np.float32))
+    return q.reshape(m + pm, k + pk)[:m, :k], s
+
+
+def quant_gpu(E, x, code, block_rows, x_row=None):
+    """x: a torch tensor on the GPU whose rows may lie x_row elements apart."""
+    m, k = x.shape
+    nb = -(-m // block_rows)
+    q = torch.full((m + 1, k), 0xEE, dtype=torch.uint8, device="cuda")          # a row of sentinels
+    s = torch.full((nb * -(-k // 128) + 1,), -7.0, dtype=torch.float32, device="cuda")
+    E.quant_fp8_block(x.data_ptr(), code, m, k, q.data_ptr(), s.data_ptr(), block_rows=block_rows,
+                      x_row=x.stride(0) if x_row is None else x_row, stream=stream())
+    torch.cuda.synchronize()
+    assert (q[m] == 0xEE).all() and s[-1] == -7.0
+    return q[:m].cpu().numpy(), s[:-1].view(nb, -1).cpu().numpy()
+
+
+SHAPES = [(1, 16), (1, 128), (1, 5120), (3, 144), (7, 256), (17, 4112), (128, 128), (129, 272), (300, 2048),
+          (1000, 3856)]
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("m,k", SHAPES)
+def test_quant_matches_definition(E, m, k, dtype, block_rows):
+    say(f"  quant {m}x{k} {dtype} blocks of {block_rows}")
+    dt = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}[dtype]
+    code = {"bf16": E.BF16, "fp16": E.FP16, "fp32": E.FP32}[dtype]
+    rng = np.random.default_rng([21, m, k])
+    x = rng.standard_normal((m, k)) * np.exp(rng.standard_normal((m, 1)))
+    x[rng.random((m, k)) < 0.3] = 0.0
+    x[:, :: 97] *= 30
+    x[0, : 16] = 0.0
+    t = torch.from_numpy(x).to(dt).cuda()
+    q, s = quant_gpu(E, t, code, block_rows)
+    rq, rs = quant_ref(t.float().cpu().numpy(), block_rows)
+    assert np.array_equal(s.view(np.uint32), rs.view(np.uint32))
+    assert np.array_equal(q, rq)
+
+
+def test_quant_strided_rows(E):
+    """Rows of a wider matrix (one head's share of a fused projection's output)."""
+    wide = torch.randn((37, 1024), generator=torch.Generator().manual_seed(3)).to(torch.bfloat16).cuda()
+    part = wide[:, 256: 256 + 400]
+    q, s = quant_gpu(E, part, E.BF16, 1)
+    rq, rs = quant_ref(part.float().cpu().numpy(), 1)
+    assert np.array_equal(q, rq) and np.array_equal(s, rs)
+
+
+@pytest.mark.parametrize("block_rows", [1, 128])
+def test_quant_extremes(E, block_rows):
+    """Blocks of zeros, of subnormals (scales that underflow or are subnormal themselves), of the
+    largest values, and of ties between two codes."""
+    k = 128 * 8
+    x = np.zeros((128, k), np.float32)
+    x[:, 128:256] = 1e-45
+    x[:, 256:384] = np.linspace(-3e-43, 3e-43, 128, dtype=np.float32)
+    x[:, 384:512] = np.linspace(-1e-38, 1e-38, 128, dtype=np.float32)
+    x[:, 512:640] = np.linspace(-3.4e38, 3.4e38, 128, dtype=np.float32)
+    x[:, 640:768] = np.linspace(-1e-20, 1e-20, 128, dtype=np.float32)
+    x[:, 768:896] = 1.0
+    x[0, 768:896] = 448.0 * (np.arange(128) % 2)             # scale 1: what follows are the codes' ties
+    x[:, 896:] = np.arange(128, dtype=np.float32) / 16 + 1 / 32
+    x[:, 896] = 448.0
+    q, s = quant_gpu(E, torch.from_numpy(x).cuda(), E.FP32, block_rows)
+    rq, rs = quant_ref(x, block_rows)
+    assert np.array_equal(s.view(np.uint32), rs.view(np.uint32))
+    assert np.array_equal(q, rq)
+
+
+def test_quant_non_finite_blocks_show(E):
+    """A NaN or infinity makes its block's scale one, and leaves the other blocks alone."""
+    x = torch.randn((4, 384), generator=torch.Generator().manual_seed(4)).to(torch.bfloat16)
+    clean_q, clean_s = quant_gpu(E, x.cuda(), E.BF16, 1)
+    x[0, 5], x[1, 200], x[2, 300] = float("nan"), float("inf"), float("-inf")
+    q, s = quant_gpu(E, x.cuda(), E.BF16, 1)
+    hit = np.zeros((4, 3), bool)
+    hit[0, 0] = hit[1, 1] = hit[2, 2] = True
+    assert np.isnan(s[0, 0]) and np.isinf(s[1, 1]) and np.isinf(s[2, 2])
+    assert np.array_equal(s[~hit], clean_s[~hit])
+    wide = np.repeat(hit, 128, 1)
+    assert np.array_equal(q[~wide], clean_q[~wide])
+    # the values they stand for are not finite
+    v = torch.from_numpy(q).view(torch.float8_e4m3fn).float().numpy() * np.repeat(s, 128, 1)
+    assert np.isnan(v[0, :128]).all() and np.isnan(v[1, 128:256]).all()
+
+
+# ---- product ----------------------------------------------------------------------------
+LAYOUTS = ("block", "row_block", "row")
+
+
+def product_inputs(m, n, k, w_kind, layout, seed):
+    g = torch.Generator().manual_seed(seed)
+    kb = -(-k // 128)
+    x = (torch.randn((m, k), generator=g) * 60).clamp(-448, 448).to(torch.float8_e4m3fn)
+    w = (torch.randn((n, k), generator=g) * 60).clamp(-448, 448).to(torch.float8_e4m3fn if w_kind == "e4m3" else torch.float8_e5m2)
+    xs = torch.exp(torch.randn((m, kb), generator=g) - 4)
+    ws = torch.exp(torch.randn({"block": (-(-n // 128), kb), "row_block": (n, kb), "row": (n,)}[layout], generator=g) - 6)
+    return x.cuda(), xs.cuda(), w.cuda(), ws.cuda()
+
+
+def wide_scales(ws, layout, n, k):
+    ws = ws.double()
+    at = torch.arange(k, device="cuda") // 128
+    if layout == "block":
+        return ws[torch.arange(n, device="cuda") // 128][:, at]
+    return ws[:, at] if layout == "row_block" else ws[:, None].expand(n, k)
+
+
+def product_gpu(E, x, xs, w, ws, layout, y_dtype):
+    m, n, k = x.shape[0], w.shape[0], x.shape[1]
+    y = torch.full((m + 1, n), float("nan"), dtype={"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}[y_dtype],
+                   device="cuda")
+    y[m] = 3.0
+    E.gemm_fp8_block(x.data_ptr(), xs.data_ptr(), w.data_ptr(), ws.data_ptr(), y.data_ptr(), m, n, k,
+                     w_dtype=E.FP8_E4M3 if w.dtype == torch.float8_e4m3fn else E.FP8_E5M2,
+                     w_scales={"block": E.SCALE_BLOCK, "row_block": E.SCALE_ROW_BLOCK, "row": E.SCALE_ROW}[layout],
+                     y_dtype={"bf16": E.BF16, "fp16": E.FP16, "fp32": E.FP32}[y_dtype], stream=stream())
+    torch.cuda.synchronize()
+    assert (y[m] == 3.0).all()
+    return y[:m]
+
+
+def check_product(y, x, xs, w, ws, layout, y_dtype):
+    m, n, k = x.shape[0], w.shape[0], x.shape[1]
+    kb = -(-k // 128)
+    a = x.double() * xs.double()[:, torch.arange(k, device="cuda") // 128]
+    b = w.double() * wide_scales(ws, layout, n, k)
+    exact, size = a @ b.t(), a.abs() @ b.abs().t()
+    half = {"bf16": 2.0 ** -8, "fp16": 2.0 ** -11, "fp32": 0.0}[y_dtype]
+    least = {"bf16": 0.0, "fp16": 2.0 ** -25, "fp32": 0.0}[y_dtype]
+    tol = (256 + kb + 4) * 2.0 ** -24 * size
+    tol = tol + half * (exact.abs() + tol) + least
+    off = (y.double() - exact).abs()
+    assert (off <= tol).all(), f"off by {float((off / tol).max()):.3g} of the bound"
+
+
+PRODUCTS = [(1, 1, 16), (1, 16, 128), (1, 200, 5120), (2, 33, 144), (5, 257, 1040), (16, 512, 2048), (17, 130, 272),
+            (31, 1000, 4112), (33, 16, 8192), (64, 640, 1280), (65, 129, 640), (100, 2048, 512), (128, 128, 128),
+            (129, 300, 1296), (200, 5, 3856), (256, 256, 1024), (257, 513, 400), (500, 1024, 2064), (1025, 515, 256),
+            (700, 1300, 1424)]
+
+
+@pytest.mark.parametrize("i", range(len(PRODUCTS)))
+def test_product_matches_64_bits(E, i):
+    """Every shape with every layout of scales, over both weight types and the three outputs."""
+    m, n, k = PRODUCTS[i]
+    for j, layout in enumerate(LAYOUTS):
+        w_kind, y_dtype = ("e4m3", "e5m2")[(i + j) % 2], ("bf16", "fp32", "fp16")[(i + 2 * j) % 3]
+        say(f"  product {m}x{n}x{k} {w_kind} {layout} {y_dtype}")
+        t = product_inputs(m, n, k, w_kind, layout, 100 + i)
+        check_product(product_gpu(E, *t, layout, y_dtype), *t, layout, y_dtype)
+
+
+@pytest.mark.parametrize("m,n,k,layout", [(1, 17408, 5120, "block"), (61, 5120, 17408, "row"), (300, 10240, 3840, "row_block"),
+                                          (2200, 4100, 5120, "block"), (4096, 5120, 1536, "row")])
+def test_product_large(E, m, n, k, layout):
+    say(f"  product {m}x{n}x{k} {layout}")
+    t = product_inputs(m, n, k, "e4m3", layout, 7)
+    check_product(product_gpu(E, *t, layout, "fp32"), *t, layout, "fp32")
+
+
+def test_product_repeats_its_bits(E):
+    for m, n, k in ((3, 2000, 5120), (61, 1280, 17408), (300, 700, 2048), (1500, 1500, 1280)):
+        t = product_inputs(m, n, k, "e4m3", "block", 9)
+        a = product_gpu(E, *t, "block", "fp32")
+        for _ in range(3):
+            assert torch.equal(a, product_gpu(E, *t, "block", "fp32"))
+
+
+def test_product_row_values_do_not_depend_on_the_batch_neighbours(E):
+    """A NaN scale or code in one row of X (or W) shows in that row (column) of Y alone."""
+    for m, n, k in ((3, 40, 256), (40, 300, 512), (300, 300, 384)):
+        x, xs, w, ws = product_inputs(m, n, k, "e4m3", "row_block", 11)
+        clean = product_gpu(E, x, xs, w, ws, "row_block", "fp32")
+        xs2, w2 = xs.clone(), w.clone()
+        xs2[1, 0] = float("nan")
+        w2.view(torch.uint8)[7, 3] = 0x7F
+        y = product_gpu(E, x, xs2, w2, ws, "row_block", "fp32")
+        keep = torch.ones((m, n), dtype=torch.bool, device="cuda")
+        keep[1], keep[:, 7] = False, False
+        assert torch.equal(y[keep], clean[keep])
+        assert torch.isnan(y[1]).all() and torch.isnan(y[:, 7]).all()
+
+
+@pytest.mark.parametrize("m,n,k", [(4, 300, 512), (40, 300, 512), (300, 520, 512)])
+def test_product_of_extremes(E, m, n, k):
+    """The largest codes of both types with scales that make sums beyond FP16 and within it."""
+    x = torch.full((m, k), 448.0).to(torch.float8_e4m3fn).cuda()
+    w = torch.full((n, k), 57344.0).to(torch.float8_e5m2).cuda()
+    xs = torch.ones((m, k // 128), device="cuda")
+    ws = torch.ones((n,), device="cuda")
+    assert (product_gpu(E, x, xs, w, ws, "row", "fp32") == 448.0 * 57344.0 * k).all()
+    assert torch.isinf(product_gpu(E, x, xs, w, ws, "row", "fp16")).all()
+    assert (product_gpu(E, x, xs, w, ws * 2.0 ** -24, "row", "fp16") == 448.0 * 57344.0 * k * 2.0 ** -24).all()
+
+
+def test_product_on_another_stream_and_in_a_graph(E):
+    """The call orders itself on the stream it is given, and replays from a graph."""
+    m, n, k = 24, 640, 1024
+    t = product_inputs(m, n, k, "e4m3", "block", 13)
+    want = product_gpu(E, *t, "block", "bf16")
+    s = torch.cuda.Stream()
+    x, xs, w, ws = t
+    q_in = torch.randn((m, k), device="cuda").to(torch.bfloat16)
+    q, qs = torch.empty((m, k), dtype=torch.uint8, device="cuda"), torch.empty((m, k // 128), device="cuda")
+    y = torch.zeros((m, n), dtype=torch.bfloat16, device="cuda")
+    torch.cuda.synchronize()
+
+    def step():
+        E.quant_fp8_block(q_in.data_ptr(), E.BF16, m, k, q.data_ptr(), qs.data_ptr(), stream=stream())
+        E.gemm_fp8_block(q.data_ptr(), qs.data_ptr(), w.data_ptr(), ws.data_ptr(), y.data_ptr(), m, n, k, stream=stream())
+
+    with torch.cuda.stream(s):
+        E.gemm_fp8_block(x.data_ptr(), xs.data_ptr(), w.data_ptr(), ws.data_ptr(), y.data_ptr(), m, n, k, stream=stream())
+    s.synchronize()
+    assert torch.equal(y, want)
+    with torch.cuda.stream(s):
+        step()
+    s.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        step()
+    for seed in range(3):
+        q_in.copy_(torch.randn((m, k), generator=torch.Generator().manual_seed(seed)).to(torch.bfloat16))
+        graph.replay()
+        torch.cuda.synchronize()
+        got = y.clone()
+        step()
+        torch.cuda.synchronize()
+        assert torch.equal(got, y) and torch.isfinite(y).all()
+
+
+def test_decoded_container_feeds_the_product(E, oracle):
+    """An FP8 row container decoded on the GPU, times quantised activations with its row scales."""
+    from paper_2609_34185_amd import workloads as W
+    w = W.ragged_tensor(31, 200, 512, scale=0.05)
+    blob, _ = E.encode(w, 4.0, container=E.CONT_FP8_ROW)
+    out, delta, st = E.decode(blob, E.FP8_E4M3)
+    torch.cuda.synchronize()
+    assert int(st.item()) == 0
+    x = torch.randn((19, 512), generator=torch.Generator().manual_seed(5)).to(torch.bfloat16).cuda()
+    q, s = torch.empty((19, 512), dtype=torch.float8_e4m3fn, device="cuda"), torch.empty((19, 4), device="cuda")
+    E.quant_fp8_block(x.data_ptr(), E.BF16, 19, 512, q.data_ptr(), s.data_ptr(), stream=stream())
+    check_product(product_gpu(E, q, s, out, delta, "row", "fp32"), q, s, out, delta, "row", "fp32")
