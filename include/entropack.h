@@ -474,7 +474,7 @@ enum ep_scale_layout {
  * FP8 types widen exactly, at half the rate.  m may be 0 (nothing is done).  Asynchronous on hip_stream, no allocation,
  * no workspace, one launch.
  * Errors: EP_ERR_ARG (null or misaligned pointers, m < 0, n <= 0, k <= 0,
- * k % 16, m, n or k above 2^24, another dtype or layout), EP_ERR_HIP. */
+ * k % 16, m or n above 2^24, k above 2^22, another dtype or layout), EP_ERR_HIP. */
 int ep_gemm_fp8_block(const void* d_x, const float* d_x_scale, const void* d_w, int w_dtype,
                       const float* d_w_scale, int w_scales, void* d_y, int y_dtype, int64_t m,
                       int64_t n, int64_t k, void* hip_stream);

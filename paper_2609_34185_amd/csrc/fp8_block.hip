@@ -7,6 +7,7 @@
 
 #include "../../include/entropack.h"
 #include "common.h"
+#include "tile_order.h"
 
 namespace ep {
 namespace {
@@ -182,16 +183,45 @@ __device__ __forceinline__ float w_scale_at(const Product& P, int64_t j, uint32_
   return P.w_scale[(P.w_scales == EP_SCALE_BLOCK ? j / 128 : j) * P.kb + b];
 }
 
-__device__ __forceinline__ uint16_t bf16_of(float f) {
-  const uint32_t u = __float_as_uint(f);
-  if ((u & 0x7FFFFFFFu) > 0x7F800000u) return (uint16_t)((u >> 16) | 0x40u);   // a NaN stays one
-  return (uint16_t)((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
-}
+__device__ __forceinline__ uint16_t bf16_of(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
 
 __device__ __forceinline__ void store_y(const Product& P, int64_t at, float f) {
   if (P.y_dtype == EP_FP32) static_cast<float*>(P.y)[at] = f;
   else if (P.y_dtype == EP_FP16) static_cast<_Float16*>(P.y)[at] = (_Float16)f;
   else static_cast<uint16_t*>(P.y)[at] = bf16_of(f);
+}
+
+// Four values of one row, from column j on; in one store where the row's address allows it.
+__device__ __forceinline__ void store_y4(const Product& P, int64_t i, int64_t j, const float (&v)[4]) {
+  const int64_t at = i * P.n + j;
+  if (P.n % 4 == 0 && j + 4 <= P.n) {
+    if (P.y_dtype == EP_FP32) {
+      *reinterpret_cast<v4f*>(static_cast<float*>(P.y) + at) = v4f{v[0], v[1], v[2], v[3]};
+    } else {
+      typedef uint16_t v4s __attribute__((ext_vector_type(4)));
+      v4s w;
+#pragma unroll
+      for (int r = 0; r < 4; r++)
+        w[r] = P.y_dtype == EP_FP16 ? __builtin_bit_cast(uint16_t, (_Float16)v[r]) : bf16_of(v[r]);
+      *reinterpret_cast<v4s*>(static_cast<uint16_t*>(P.y) + at) = w;
+    }
+  } else {
+#pragma unroll
+    for (int r = 0; r < 4; r++)
+      if (j + r < P.n) store_y(P, at + r, v[r]);
+  }
+}
+
+// Workgroup barrier for direct loads: this wave's LDS reads have returned and at most N of its
+// direct loads are still in flight, then s_barrier.  The scheduling barriers keep the compiler
+// from moving LDS accesses across it.
+template <int N>
+__device__ __forceinline__ void stage_barrier() {
+  static_assert(N >= 0 && N < 64, "vmcnt");
+  __builtin_amdgcn_sched_barrier(0);
+  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));   // vmcnt(N) lgkmcnt(0)
+  __builtin_amdgcn_s_barrier();
+  __builtin_amdgcn_sched_barrier(0);
 }
 
 // One 16 x 16 tile of Y for each wave.  v_mfma_f32_16x16x128_f8f6f4 multiplies 16 rows of W by
@@ -269,12 +299,167 @@ __global__ __launch_bounds__(256) void product_kernel(Product P) {
   }
 }
 
+// ---- product in tiles, operands through LDS --------------------------------------------
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+
+__device__ __forceinline__ uint32_t swz(uint32_t r) { return (r & 7) ^ ((r >> 3) & 1); }
+
+constexpr uint32_t kOutside = 0x80000000u;   // past the end of every buffer below (2^30 bytes at most), also with a row's offset added
+
+__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, int64_t bytes) {
+  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, (int)bytes, 0x00020000);
+}
+
+template <int WFMT, bool EXACT, int LAYOUT, int NW, int NX, int WW, int WX, int NS>
+__global__ __launch_bounds__(64 * WW * WX) void product_tiles_kernel(Product P, uint32_t tw, uint32_t tx) {
+  constexpr int kWaves = WW * WX, TW = 16 * NW * WW, TX = 16 * NX * WX;
+  constexpr int kSegsW = TW / 8 / kWaves, kSegsX = TX / 8 / kWaves;   // 1 KiB loads of a wave and step
+  constexpr int kScaleLoads = (TW + TX) / 64;
+  constexpr int kPerStep = kSegsW + kSegsX + (kScaleLoads + kWaves - 1) / kWaves;
+  constexpr int kStage = (TW + TX) * 128, kScaleStage = (TW + TX) * 4;
+  static_assert(TW % (8 * kWaves) == 0 && TX % (8 * kWaves) == 0 && TW % 64 == 0 && TX % 64 == 0, "tile");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds_mem[NS * (kStage + kScaleStage)];
+  lds_u8* const lds = (lds_u8*)lds_mem;
+  lds_u8* const lds_scales = lds + NS * kStage;
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, quarter = lane >> 4;
+  const int ww = wave % WW, wx = wave / WW;
+  uint32_t ti, tj;
+  tile_of(xcd_spread(blockIdx.x, gridDim.x), tx, tw, ti, tj);
+  const int64_t i0 = (int64_t)ti * TX, j0 = (int64_t)tj * TW;      // first rows of X and W
+  const int64_t rows_x = min(P.m - i0, (int64_t)TX), rows_w = min(P.n - j0, (int64_t)TW);
+  const uint32_t k = (uint32_t)P.k, kb = P.kb;
+  const __amdgpu_buffer_rsrc_t rx = rsrc_of(P.x + i0 * P.k, rows_x * P.k), rw = rsrc_of(P.w + j0 * P.k, rows_w * P.k);
+  const __amdgpu_buffer_rsrc_t rxs = rsrc_of(P.x_scale + i0 * kb, rows_x * kb * 4);
+  const __amdgpu_buffer_rsrc_t rws =
+      LAYOUT == EP_SCALE_BLOCK ? rsrc_of(P.w_scale + j0 / 128 * kb, (rows_w + 127) / 128 * kb * 4)
+                               : rsrc_of(P.w_scale + j0 * kb, LAYOUT == EP_SCALE_ROW ? 0 : rows_w * kb * 4);
+
+  // direct loads: a wave instruction fills one segment of 8 rows; lane l writes the 16 bytes at
+  // 16 l, the place of chunk (l mod 8) ^ swz(row) of row l / 8
+  const uint32_t seg_row = 8 * wave + (lane >> 3);
+  const uint32_t chunk = 16 * ((lane & 7) ^ swz(seg_row & 15));
+  static_assert(8 * kWaves % 16 == 0, "rows of a lane's segments share their swizzle");
+  const uint32_t scale_at = [&] {   // this lane's scale of a step, in floats from the step's first
+    const uint32_t s = 64 * (wave % kScaleLoads) + lane;
+    return s < TX ? s * kb : LAYOUT == EP_SCALE_BLOCK ? ((s - TX) >> 7) * kb : (s - TX) * kb;
+  }();
+  auto fetch = [&](uint32_t b, uint32_t stage) {
+    lds_u8* const dst = lds + kStage * stage + 1024 * wave;
+    const uint32_t at = 128 * b + chunk;
+    const uint32_t off = at < k ? seg_row * k + at : kOutside;
+#pragma unroll
+    for (int q = 0; q < kSegsX; q++)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, dst + 1024 * kWaves * q, 16, off + 8 * kWaves * q * k, 0, 0, 0);
+#pragma unroll
+    for (int q = 0; q < kSegsW; q++)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, dst + TX * 128 + 1024 * kWaves * q, 16, off + 8 * kWaves * q * k, 0, 0, 0);
+    const bool of_x = wave % kScaleLoads < TX / 64;
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(of_x ? rxs : rws, lds_scales + kScaleStage * stage + 256 * (wave % kScaleLoads), 4,
+                                             b < kb ? 4 * (scale_at + b) : kOutside, 0, 0, 0);
+  };
+
+  v4f acc[NW][NX];
+#pragma unroll
+  for (int i = 0; i < NW; i++)
+#pragma unroll
+    for (int t = 0; t < NX; t++) acc[i][t] = v4f{};
+
+  // fragments: row col of a 16-row tile, chunks quarter and 4 + quarter
+  const uint32_t fs = swz(col);
+  const uint32_t fo0 = 16 * (quarter ^ fs), fo1 = 16 * ((4 + quarter) ^ fs);
+  const uint32_t fx = (16 * NX * wx + col) * 128, fw = (TX + 16 * NW * ww + col) * 128;
+  auto fragment = [&](const lds_u8* p) {
+    const v4i a = *reinterpret_cast<const __attribute__((address_space(3))) v4i*>(p + fo0);
+    const v4i b = *reinterpret_cast<const __attribute__((address_space(3))) v4i*>(p + fo1);
+    return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  };
+
+#pragma unroll
+  for (int s = 0; s < NS - 1; s++) fetch(s, s);
+  stage_barrier<(NS - 2) * kPerStep>();
+  uint32_t stage = 0;
+  for (uint32_t b = 0; b < kb; b++) {
+    const lds_u8* const p = lds + kStage * stage;
+    const __attribute__((address_space(3))) float* const sc =
+        (const __attribute__((address_space(3))) float*)(lds_scales + kScaleStage * stage);
+    const uint32_t ahead = stage == 0 ? NS - 1 : stage - 1;
+    fetch(b + NS - 1, ahead);
+    v8i xf[NX];
+    float xs[NX];
+#pragma unroll
+    for (int t = 0; t < NX; t++) {
+      xf[t] = fragment(p + fx + 16 * 128 * t);
+      xs[t] = sc[16 * NX * wx + 16 * t + col];
+    }
+    if (LAYOUT == EP_SCALE_BLOCK) {
+      const float ws = sc[TX + 16 * NW * ww];
+#pragma unroll
+      for (int t = 0; t < NX; t++) xs[t] *= ws;
+    }
+#pragma unroll
+    for (int i = 0; i < NW; i++) {
+      const v8i wf = fragment(p + fw + 16 * 128 * i);
+      v4f ws;
+      if (LAYOUT == EP_SCALE_ROW_BLOCK)
+        ws = *reinterpret_cast<const __attribute__((address_space(3))) v4f*>(sc + TX + 16 * NW * ww + 16 * i + 4 * quarter);
+#pragma unroll
+      for (int t = 0; t < NX; t++) {
+        const v4f part = block_product<WFMT, EXACT>(wf, xf[t]);
+#pragma unroll
+        for (int r = 0; r < 4; r++)
+          acc[i][t][r] = __builtin_fmaf(LAYOUT == EP_SCALE_ROW_BLOCK ? part[r] * ws[r] : part[r], xs[t], acc[i][t][r]);
+      }
+    }
+    stage_barrier<(NS - 2) * kPerStep>();
+    stage = stage + 1 == NS ? 0 : stage + 1;
+  }
+  __builtin_amdgcn_s_waitcnt(0);   // direct loads still in flight land before the wave ends
+
+#pragma unroll
+  for (int i = 0; i < NW; i++) {
+    const int64_t j = j0 + 16 * (NW * ww + i) + 4 * quarter;
+    float ws[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+    if (LAYOUT == EP_SCALE_ROW) {
+#pragma unroll
+      for (int r = 0; r < 4; r++) ws[r] = j + r < P.n ? P.w_scale[j + r] : 0.0f;
+    }
+#pragma unroll
+    for (int t = 0; t < NX; t++) {
+      const int64_t row = i0 + 16 * (NX * wx + t) + col;
+      if (row < P.m) {
+        float v[4];
+#pragma unroll
+        for (int r = 0; r < 4; r++) v[r] = LAYOUT == EP_SCALE_ROW ? acc[i][t][r] * ws[r] : acc[i][t][r];
+        store_y4(P, row, j, v);
+      }
+    }
+  }
+}
+
+template <int WFMT, bool EXACT, int LAYOUT>
+void product_launch(const Product& P, hipStream_t stream) {
+  if (P.m > 64) {
+    const uint32_t tx = (uint32_t)((P.m + 255) / 256), tw = (uint32_t)((P.n + 255) / 256);
+    hipLaunchKernelGGL((product_tiles_kernel<WFMT, EXACT, LAYOUT, 8, 4, 2, 4, 2>), dim3(tx * tw), dim3(512), 0, stream, P, tw, tx);
+  } else {
+    const int64_t tiles = (P.m + 15) / 16 * ((P.n + 15) / 16);
+    hipLaunchKernelGGL((product_kernel<WFMT, EXACT>), dim3((uint32_t)((tiles + 3) / 4)), dim3(256), 0, stream, P);
+  }
+}
+
+template <int WFMT, bool EXACT>
+void product_launch(const Product& P, hipStream_t stream) {
+  if (P.w_scales == EP_SCALE_BLOCK) product_launch<WFMT, EXACT, EP_SCALE_BLOCK>(P, stream);
+  else if (P.w_scales == EP_SCALE_ROW_BLOCK) product_launch<WFMT, EXACT, EP_SCALE_ROW_BLOCK>(P, stream);
+  else product_launch<WFMT, EXACT, EP_SCALE_ROW>(P, stream);
+}
+
 template <int WFMT>
-void product_launch(const Product& P, uint32_t groups, hipStream_t stream) {
-  if (P.y_dtype == EP_FP32)
-    hipLaunchKernelGGL((product_kernel<WFMT, true>), dim3(groups), dim3(256), 0, stream, P);
-  else
-    hipLaunchKernelGGL((product_kernel<WFMT, false>), dim3(groups), dim3(256), 0, stream, P);
+void product_launch(const Product& P, hipStream_t stream) {
+  if (P.y_dtype == EP_FP32) product_launch<WFMT, true>(P, stream);
+  else product_launch<WFMT, false>(P, stream);
 }
 
 bool misaligned(const void* p) { return reinterpret_cast<uintptr_t>(p) & 15; }
@@ -311,9 +496,9 @@ extern "C" int ep_quant_fp8_block(const void* d_x, int x_dtype, int64_t m, int64
 extern "C" int ep_gemm_fp8_block(const void* d_x, const float* d_x_scale, const void* d_w, int w_dtype,
                                  const float* d_w_scale, int w_scales, void* d_y, int y_dtype, int64_t m,
                                  int64_t n, int64_t k, void* hip_stream) {
-  constexpr int64_t kMost = 1 << 24;
-  if (m < 0 || n <= 0 || k <= 0 || k % 16 || m > kMost || n > kMost || k > kMost)
-    return ep::fail(EP_ERR_ARG, "ep_gemm_fp8_block: need m >= 0, n, k > 0, k % 16 == 0, none above 2^24");
+  constexpr int64_t kMost = 1 << 24, kMostK = 1 << 22;   // 256 rows of k bytes stay below 2^31
+  if (m < 0 || n <= 0 || k <= 0 || k % 16 || m > kMost || n > kMost || k > kMostK)
+    return ep::fail(EP_ERR_ARG, "ep_gemm_fp8_block: need m >= 0, n, k > 0, k % 16 == 0, m and n up to 2^24, k to 2^22");
   if (w_dtype != EP_FP8_E4M3 && w_dtype != EP_FP8_E5M2)
     return ep::fail(EP_ERR_ARG, "ep_gemm_fp8_block: w_dtype must be FP8_E4M3 or FP8_E5M2");
   if (w_scales < EP_SCALE_BLOCK || w_scales > EP_SCALE_ROW)
@@ -328,10 +513,8 @@ extern "C" int ep_gemm_fp8_block(const void* d_x, const float* d_x_scale, const 
   const ep::Product P = {static_cast<const uint8_t*>(d_x), d_x_scale, static_cast<const uint8_t*>(d_w), d_w_scale,
                          d_y, m, n, k, (uint32_t)((k + 127) / 128), (uint32_t)w_scales, (uint32_t)y_dtype};
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  const int64_t tiles = (m + 15) / 16 * ((n + 15) / 16), groups = (tiles + 3) / 4;
-  if (groups > 0x7FFFFFFF) return ep::fail(EP_ERR_ARG, "ep_gemm_fp8_block: matrix too large");
-  if (w_dtype == EP_FP8_E4M3) ep::product_launch<0>(P, (uint32_t)groups, stream);
-  else ep::product_launch<1>(P, (uint32_t)groups, stream);
+  if (w_dtype == EP_FP8_E4M3) ep::product_launch<0>(P, stream);
+  else ep::product_launch<1>(P, stream);
   if (hipGetLastError() != hipSuccess) return ep::fail(EP_ERR_HIP, "ep_gemm_fp8_block: launch failed");
   return EP_OK;
 }
