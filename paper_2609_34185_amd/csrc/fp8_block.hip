@@ -3,6 +3,7 @@
 // container decodes to.
 #include <hip/hip_runtime.h>
 
+#include <algorithm>
 #include <cstdint>
 
 #include "../../include/entropack.h"
@@ -16,7 +17,9 @@ typedef int v4i __attribute__((ext_vector_type(4)));
 typedef int v8i __attribute__((ext_vector_type(8)));
 typedef float v4f __attribute__((ext_vector_type(4)));
 typedef _Float16 v2h __attribute__((ext_vector_type(2)));
+typedef _Float16 v4h __attribute__((ext_vector_type(4)));
 typedef _Float16 v8h __attribute__((ext_vector_type(8)));
+typedef __bf16 v4b __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
@@ -173,42 +176,32 @@ struct Product {
   void* y;
   int64_t m, n, k;
   uint32_t kb;         // blocks of 128 along k
-  uint32_t w_scales;   // ep_scale_layout
-  uint32_t y_dtype;
 };
 
-// Scale of W's row j in block b.
-__device__ __forceinline__ float w_scale_at(const Product& P, int64_t j, uint32_t b) {
-  if (P.w_scales == EP_SCALE_ROW) return P.w_scale[j];
-  return P.w_scale[(P.w_scales == EP_SCALE_BLOCK ? j / 128 : j) * P.kb + b];
+// Y's element types: ep_dtype codes as template arguments.
+template <int OUT>
+__device__ __forceinline__ void store_y(void* y, int64_t at, float f) {
+  if (OUT == EP_FP32) static_cast<float*>(y)[at] = f;
+  else if (OUT == EP_FP16) static_cast<_Float16*>(y)[at] = (_Float16)f;
+  else static_cast<__bf16*>(y)[at] = (__bf16)f;
 }
 
-__device__ __forceinline__ uint16_t bf16_of(float f) { return __builtin_bit_cast(uint16_t, (__bf16)f); }
-
-__device__ __forceinline__ void store_y(const Product& P, int64_t at, float f) {
-  if (P.y_dtype == EP_FP32) static_cast<float*>(P.y)[at] = f;
-  else if (P.y_dtype == EP_FP16) static_cast<_Float16*>(P.y)[at] = (_Float16)f;
-  else static_cast<uint16_t*>(P.y)[at] = bf16_of(f);
-}
-
-// Four values of one row, from column j on; in one store where the row's address allows it.
-__device__ __forceinline__ void store_y4(const Product& P, int64_t i, int64_t j, const float (&v)[4]) {
+// Four values of row i from column j on; in one store where n keeps its address aligned.
+template <int OUT>
+__device__ __forceinline__ void store_y4(const Product& P, int64_t i, int64_t j, const v4f& v) {
   const int64_t at = i * P.n + j;
   if (P.n % 4 == 0 && j + 4 <= P.n) {
-    if (P.y_dtype == EP_FP32) {
-      *reinterpret_cast<v4f*>(static_cast<float*>(P.y) + at) = v4f{v[0], v[1], v[2], v[3]};
+    if (OUT == EP_FP32) {
+      *reinterpret_cast<v4f*>(static_cast<float*>(P.y) + at) = v;
+    } else if (OUT == EP_FP16) {
+      *reinterpret_cast<v4h*>(static_cast<_Float16*>(P.y) + at) = __builtin_convertvector(v, v4h);
     } else {
-      typedef uint16_t v4s __attribute__((ext_vector_type(4)));
-      v4s w;
-#pragma unroll
-      for (int r = 0; r < 4; r++)
-        w[r] = P.y_dtype == EP_FP16 ? __builtin_bit_cast(uint16_t, (_Float16)v[r]) : bf16_of(v[r]);
-      *reinterpret_cast<v4s*>(static_cast<uint16_t*>(P.y) + at) = w;
+      *reinterpret_cast<v4b*>(static_cast<__bf16*>(P.y) + at) = __builtin_convertvector(v, v4b);
     }
   } else {
 #pragma unroll
     for (int r = 0; r < 4; r++)
-      if (j + r < P.n) store_y(P, at + r, v[r]);
+      if (j + r < P.n) store_y<OUT>(P.y, at + r, v[r]);
   }
 }
 
@@ -224,10 +217,11 @@ __device__ __forceinline__ void stage_barrier() {
   __builtin_amdgcn_sched_barrier(0);
 }
 
-// One 16 x 16 tile of Y for each wave.  v_mfma_f32_16x16x128_f8f6f4 multiplies 16 rows of W by
-// 16 rows of X over one whole block: lane l supplies 32 bytes of row l mod 16 of both, and gets
-// the products of W rows 4 (l / 16) + 0 .. 3 with X row l mod 16.  Which 32 of the block's 128
-// bytes a quarter of the wave supplies does not matter as long as both operands agree.
+// One block of 128 of a 16 x 16 tile.  v_mfma_f32_16x16x128_f8f6f4 multiplies 16 rows of W by 16
+// rows of X: lane l supplies 32 bytes of row l mod 16 of both, and gets the products of W rows
+// 4 (l / 16) + 0 .. 3 with X row l mod 16.  Which 32 of the block's 128 bytes a quarter of the
+// wave supplies does not matter as long as both operands agree: here two pieces of 16, so that
+// the four quarters of a load cover 64 bytes of a row.
 //
 // The FP8 instructions add their products in fewer bits than FP32: measured against 64 bits, a
 // block of Gaussian codes is off by 1.4e-5 of its size (root mean square), which disappears in the
@@ -260,45 +254,6 @@ __device__ __forceinline__ v4f block_product(const v8i& w, const v8i& x) {
   return part;
 }
 
-template <int WFMT, bool EXACT>
-__global__ __launch_bounds__(256) void product_kernel(Product P) {
-  const int lane = threadIdx.x & 63, row = lane & 15, quarter = lane >> 4;
-  const int64_t tn = (P.n + 15) / 16, tile = (int64_t)blockIdx.x * 4 + (threadIdx.x >> 6);
-  const int64_t i0 = tile / tn * 16, j0 = tile % tn * 16;
-  if (i0 >= P.m) return;
-  const int64_t i = i0 + row, j = j0 + row;
-  v4f acc = {};
-  for (uint32_t b = 0; b < P.kb; b++) {
-    v8i xw[2] = {};
-    const uint8_t* src[2] = {P.w + j * P.k, P.x + i * P.k};
-    const bool in[2] = {j < P.n, i < P.m};
-#pragma unroll
-    for (int o = 0; o < 2; o++)
-#pragma unroll
-      for (int h = 0; h < 2; h++) {
-        const int64_t at = (int64_t)b * 128 + 64 * h + 16 * quarter;
-        if (in[o] && at < P.k) {
-          const v4i t = *reinterpret_cast<const v4i*>(src[o] + at);
-#pragma unroll
-          for (int e = 0; e < 4; e++) xw[o][4 * h + e] = t[e];
-        }
-      }
-    const v4f part = block_product<WFMT, EXACT>(xw[0], xw[1]);
-    const float xs = i < P.m ? P.x_scale[i * P.kb + b] : 0.0f;
-#pragma unroll
-    for (int r = 0; r < 4; r++) {
-      const int64_t jr = j0 + 4 * quarter + r;
-      const float ws = jr < P.n ? w_scale_at(P, jr, b) : 0.0f;
-      acc[r] = __builtin_fmaf(part[r], xs * ws, acc[r]);
-    }
-  }
-#pragma unroll
-  for (int r = 0; r < 4; r++) {
-    const int64_t jr = j0 + 4 * quarter + r;
-    if (i < P.m && jr < P.n) store_y(P, i * P.n + jr, acc[r]);
-  }
-}
-
 // ---- product in tiles, operands through LDS --------------------------------------------
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 
@@ -310,24 +265,159 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, int64_t
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, (int)bytes, 0x00020000);
 }
 
-template <int WFMT, bool EXACT, int LAYOUT, int NW, int NX, int WW, int WX, int NS>
-__global__ __launch_bounds__(64 * WW * WX) void product_tiles_kernel(Product P, uint32_t tw, uint32_t tx) {
+// Few rows of X.  A workgroup owns `height` <= 16 NW rows of W and 16 NX rows of X; its KW waves
+// take blocks of 128 along k in turn, each through NS stages of LDS of its own, and add their sums
+// in the order of the waves at the end.  No wave waits for another before that, and what bounds the
+// kernel is how many bytes a CU has in flight: about 50 GB/s for each CU whatever the shape of the
+// workgroup, so that W is read once by as many CUs as there are.  (Fragments loaded from memory into
+// registers, 16 rows of 64 bytes a load instead of 8 of 128, took 94 us where this takes 28:
+// 61 x 5120 x 17408.)
+template <int WFMT, int OUT, int LAYOUT, int NW, int NX, int KW, int NS>
+__global__ __launch_bounds__(64 * KW) void product_ring_kernel(Product P, uint32_t height, uint32_t per_xcd) {
+  constexpr bool EXACT = OUT == EP_FP32;
+  constexpr int TW = 16 * NW, TX = 16 * NX;
+  constexpr int kXScaleLoads = (TX + 63) / 64, kWScaleLoads = LAYOUT == EP_SCALE_ROW_BLOCK ? (TW + 63) / 64 : 0;
+  constexpr int kPerStep = (TW + TX) / 8 + kXScaleLoads + kWScaleLoads;
+  constexpr int kScales = (TW + TX) * 128, kStage = kScales + 256 * (kXScaleLoads + kWScaleLoads);
+  constexpr int kTiles = NW * NX;
+  constexpr int kLds = NS * kStage * KW > KW * kTiles * 1024 ? NS * kStage * KW : KW * kTiles * 1024;
+  static_assert(kLds <= 160 * 1024, "LDS");
+  __shared__ __attribute__((aligned(1024))) uint8_t lds_mem[kLds];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, quarter = lane >> 4;
+  lds_u8* const lds = (lds_u8*)lds_mem + NS * kStage * wave;
+  const uint32_t xcd = blockIdx.x % kXcds, turn = blockIdx.x / kXcds;
+  const int64_t j0 = (int64_t)(turn % per_xcd * kXcds + xcd) * height, i0 = (int64_t)(turn / per_xcd) * TX;
+  if (j0 >= P.n) return;
+  const int64_t rows_x = min(P.m - i0, (int64_t)TX), rows_w = min(P.n - j0, (int64_t)height);
+  const uint32_t k = (uint32_t)P.k, kb = P.kb;
+  const __amdgpu_buffer_rsrc_t rx = rsrc_of(P.x + i0 * P.k, rows_x * P.k), rw = rsrc_of(P.w + j0 * P.k, rows_w * P.k);
+  const __amdgpu_buffer_rsrc_t rxs = rsrc_of(P.x_scale + i0 * kb, rows_x * kb * 4);
+  const __amdgpu_buffer_rsrc_t rws = rsrc_of(P.w_scale + j0 * kb, LAYOUT == EP_SCALE_ROW_BLOCK ? rows_w * kb * 4 : 0);
+
+  // direct loads: segments of 8 rows, lane l writing chunk (l mod 8) ^ swz(row) of row l / 8
+  const uint32_t seg_row = lane >> 3;
+  const uint32_t even = 16 * ((lane & 7) ^ swz(seg_row)), odd = 16 * ((lane & 7) ^ swz(seg_row + 8));
+  auto fetch = [&](uint32_t b, uint32_t stage) {
+    lds_u8* const dst = lds + kStage * stage;
+    const uint32_t at[2] = {128 * b + even, 128 * b + odd};
+    uint32_t off[2];
+#pragma unroll
+    for (int h = 0; h < 2; h++) off[h] = b < kb && at[h] < k ? seg_row * k + at[h] : kOutside;
+#pragma unroll
+    for (int q = 0; q < TX / 8; q++)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, dst + 1024 * q, 16, off[q & 1] + 8 * q * k, 0, 0, 0);
+#pragma unroll
+    for (int q = 0; q < TW / 8; q++)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rw, dst + TX * 128 + 1024 * q, 16, off[q & 1] + 8 * q * k, 0, 0, 0);
+#pragma unroll
+    for (int q = 0; q < kXScaleLoads; q++)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rxs, dst + kScales + 256 * q, 4,
+                                               b < kb ? 4 * ((64 * q + lane) * kb + b) : kOutside, 0, 0, 0);
+#pragma unroll
+    for (int q = 0; q < kWScaleLoads; q++)
+      __builtin_amdgcn_raw_ptr_buffer_load_lds(rws, dst + kScales + 256 * (kXScaleLoads + q), 4,
+                                               b < kb ? 4 * ((64 * q + lane) * kb + b) : kOutside, 0, 0, 0);
+  };
+
+  v4f acc[NW][NX];
+#pragma unroll
+  for (int i = 0; i < NW; i++)
+#pragma unroll
+    for (int t = 0; t < NX; t++) acc[i][t] = v4f{};
+  const int first_rows = (int)(128 - j0 % 128);   // of the strip before a multiple of 128
+  const uint32_t fs = swz(col), fo0 = 128 * col + 16 * (quarter ^ fs), fo1 = 128 * col + 16 * ((4 + quarter) ^ fs);
+  auto fragment = [&](const lds_u8* p) {
+    const v4i a = *reinterpret_cast<const __attribute__((address_space(3))) v4i*>(p + fo0);
+    const v4i b = *reinterpret_cast<const __attribute__((address_space(3))) v4i*>(p + fo1);
+    return v8i{a[0], a[1], a[2], a[3], b[0], b[1], b[2], b[3]};
+  };
+
+#pragma unroll
+  for (int s = 0; s < NS - 1; s++) fetch(wave + KW * s, s);
+  uint32_t stage = 0;
+  for (uint32_t b = wave; b < kb; b += KW) {
+    // the stage read last time is free: its reads have returned
+    fetch(b + KW * (NS - 1), stage == 0 ? NS - 1 : stage - 1);
+    float w0 = 1.0f, w1 = 1.0f;   // of the strip's first rows, and of those past a multiple of 128
+    if (LAYOUT == EP_SCALE_BLOCK) {
+      w0 = P.w_scale[j0 / 128 * kb + b];
+      w1 = P.w_scale[(j0 + rows_w - 1) / 128 * kb + b];
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    constexpr int kLater = (NS - 1) * kPerStep;   // loads of the stages after this one
+    static_assert(kLater < 64, "vmcnt");
+    __builtin_amdgcn_s_waitcnt((kLater & 15) | ((kLater >> 4) << 14) | (7 << 4) | (15 << 8));   // vmcnt(kLater)
+    __builtin_amdgcn_sched_barrier(0);
+    const lds_u8* const p = lds + kStage * stage;
+    const __attribute__((address_space(3))) float* const sc = (const __attribute__((address_space(3))) float*)(p + kScales);
+    v8i xf[NX];
+    float xs[NX];
+#pragma unroll
+    for (int t = 0; t < NX; t++) {
+      xf[t] = fragment(p + 2048 * t);
+      xs[t] = sc[16 * t + col];
+    }
+#pragma unroll
+    for (int i = 0; i < NW; i++) {
+      const v8i wf = fragment(p + TX * 128 + 2048 * i);
+      const float wblock = 16 * i + 4 * quarter < first_rows ? w0 : w1;
+      v4f ws;
+      if (LAYOUT == EP_SCALE_ROW_BLOCK)
+        ws = *reinterpret_cast<const __attribute__((address_space(3))) v4f*>(sc + 64 * kXScaleLoads + 16 * i + 4 * quarter);
+#pragma unroll
+      for (int t = 0; t < NX; t++) {
+        const v4f part = block_product<WFMT, EXACT>(wf, xf[t]);
+        const float s = LAYOUT == EP_SCALE_BLOCK ? xs[t] * wblock : xs[t];
+#pragma unroll
+        for (int r = 0; r < 4; r++)
+          acc[i][t][r] = __builtin_fmaf(LAYOUT == EP_SCALE_ROW_BLOCK ? part[r] * ws[r] : part[r], s, acc[i][t][r]);
+      }
+    }
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(15 | (3 << 14) | (7 << 4));   // lgkmcnt(0): this stage is read
+    __builtin_amdgcn_sched_barrier(0);
+    stage = stage + 1 == NS ? 0 : stage + 1;
+  }
+  __builtin_amdgcn_s_waitcnt(0);   // direct loads still in flight land before LDS is used again
+  __syncthreads();
+  v4f* const join = (v4f*)lds_mem;
+#pragma unroll
+  for (int i = 0; i < NW; i++)
+#pragma unroll
+    for (int t = 0; t < NX; t++) join[(wave * kTiles + NX * i + t) * 64 + lane] = acc[i][t];
+  __syncthreads();
+  for (int u = wave; u < kTiles; u += KW) {
+    v4f v = join[u * 64 + lane];
+#pragma unroll
+    for (int w = 1; w < KW; w++) v += join[(w * kTiles + u) * 64 + lane];
+    const int64_t j = j0 + 16 * (u / NX) + 4 * quarter, row = i0 + 16 * (u % NX) + col;
+    if (row >= P.m || j >= j0 + rows_w) continue;
+    if (LAYOUT == EP_SCALE_ROW)
+#pragma unroll
+      for (int r = 0; r < 4; r++) v[r] *= P.w_scale[min(j + r, P.n - 1)];
+    store_y4<OUT>(P, row, j, v);
+  }
+}
+
+// The tile of Y at row i0 of X and j0 of W.  Wave (ww, wx) of WW x WX owns NW x NX tiles of
+// 16 x 16; NS stages of operands (and their scales) are in LDS.
+template <int WFMT, int OUT, int LAYOUT, int NW, int NX, int WW, int WX, int NS>
+__device__ __forceinline__ void tile_product(const Product& P, int64_t i0, int64_t j0, lds_u8* lds) {
+  constexpr bool EXACT = OUT == EP_FP32;
   constexpr int kWaves = WW * WX, TW = 16 * NW * WW, TX = 16 * NX * WX;
   constexpr int kSegsW = TW / 8 / kWaves, kSegsX = TX / 8 / kWaves;   // 1 KiB loads of a wave and step
   constexpr int kScaleLoads = (TW + TX) / 64;
   constexpr int kPerStep = kSegsW + kSegsX + (kScaleLoads + kWaves - 1) / kWaves;
   constexpr int kStage = (TW + TX) * 128, kScaleStage = (TW + TX) * 4;
   static_assert(TW % (8 * kWaves) == 0 && TX % (8 * kWaves) == 0 && TW % 64 == 0 && TX % 64 == 0, "tile");
-  __shared__ __attribute__((aligned(1024))) uint8_t lds_mem[NS * (kStage + kScaleStage)];
-  lds_u8* const lds = (lds_u8*)lds_mem;
+  static_assert(LAYOUT != EP_SCALE_BLOCK || 128 % (16 * NW) == 0, "a wave's rows of W lie in one block of 128");
+  static_assert(kScaleLoads <= kWaves, "one scale load for each wave");
   lds_u8* const lds_scales = lds + NS * kStage;
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quarter = lane >> 4;
   const int ww = wave % WW, wx = wave / WW;
-  uint32_t ti, tj;
-  tile_of(xcd_spread(blockIdx.x, gridDim.x), tx, tw, ti, tj);
-  const int64_t i0 = (int64_t)ti * TX, j0 = (int64_t)tj * TW;      // first rows of X and W
   const int64_t rows_x = min(P.m - i0, (int64_t)TX), rows_w = min(P.n - j0, (int64_t)TW);
   const uint32_t k = (uint32_t)P.k, kb = P.kb;
   const __amdgpu_buffer_rsrc_t rx = rsrc_of(P.x + i0 * P.k, rows_x * P.k), rw = rsrc_of(P.w + j0 * P.k, rows_w * P.k);
@@ -420,46 +510,135 @@ __global__ __launch_bounds__(64 * WW * WX) void product_tiles_kernel(Product P, 
 #pragma unroll
   for (int i = 0; i < NW; i++) {
     const int64_t j = j0 + 16 * (NW * ww + i) + 4 * quarter;
-    float ws[4] = {1.0f, 1.0f, 1.0f, 1.0f};
+    v4f ws = {1.0f, 1.0f, 1.0f, 1.0f};
     if (LAYOUT == EP_SCALE_ROW) {
 #pragma unroll
-      for (int r = 0; r < 4; r++) ws[r] = j + r < P.n ? P.w_scale[j + r] : 0.0f;
+      for (int r = 0; r < 4; r++) ws[r] = P.w_scale[min(j + r, P.n - 1)];
     }
 #pragma unroll
     for (int t = 0; t < NX; t++) {
       const int64_t row = i0 + 16 * (NX * wx + t) + col;
-      if (row < P.m) {
-        float v[4];
-#pragma unroll
-        for (int r = 0; r < 4; r++) v[r] = LAYOUT == EP_SCALE_ROW ? acc[i][t][r] * ws[r] : acc[i][t][r];
-        store_y4(P, row, j, v);
-      }
+      if (row < P.m) store_y4<OUT>(P, row, j, LAYOUT == EP_SCALE_ROW ? acc[i][t] * ws : acc[i][t]);
     }
   }
 }
 
-template <int WFMT, bool EXACT, int LAYOUT>
-void product_launch(const Product& P, hipStream_t stream) {
-  if (P.m > 64) {
-    const uint32_t tx = (uint32_t)((P.m + 255) / 256), tw = (uint32_t)((P.n + 255) / 256);
-    hipLaunchKernelGGL((product_tiles_kernel<WFMT, EXACT, LAYOUT, 8, 4, 2, 4, 2>), dim3(tx * tw), dim3(512), 0, stream, P, tw, tx);
+// Workgroups [0, full) take whole tiles; the `split` last tiles are taken as two halves of W's
+// rows each by the others, so that a last round of few tiles takes half as long.
+template <int WFMT, int OUT, int LAYOUT, int NW, int NX, int WW, int WX, int NS>
+__global__ __launch_bounds__(64 * WW * WX) void product_tiles_kernel(Product P, uint32_t tw, uint32_t tx,
+                                                                     uint32_t full, uint32_t split) {
+  constexpr int TW = 16 * NW * WW, TX = 16 * NX * WX;
+  __shared__ __attribute__((aligned(1024))) uint8_t lds_mem[NS * (TW + TX) * 132];
+  lds_u8* const lds = (lds_u8*)lds_mem;
+  uint32_t ti, tj;
+  if (blockIdx.x < full) {
+    tile_of(xcd_spread(blockIdx.x, full), tx, tw, ti, tj);
+    tile_product<WFMT, OUT, LAYOUT, NW, NX, WW, WX, NS>(P, (int64_t)ti * TX, (int64_t)tj * TW, lds);
   } else {
-    const int64_t tiles = (P.m + 15) / 16 * ((P.n + 15) / 16);
-    hipLaunchKernelGGL((product_kernel<WFMT, EXACT>), dim3((uint32_t)((tiles + 3) / 4)), dim3(256), 0, stream, P);
+    const uint32_t u = xcd_spread(blockIdx.x - full, 2 * split);
+    tile_of(full + u / 2, tx, tw, ti, tj);
+    const int64_t j0 = (int64_t)tj * TW + TW / 2 * (u & 1);
+    if (j0 < P.n) tile_product<WFMT, OUT, LAYOUT, NW / 2, NX, WW, WX, NS>(P, (int64_t)ti * TX, j0, lds);
   }
 }
 
-template <int WFMT, bool EXACT>
-void product_launch(const Product& P, hipStream_t stream) {
-  if (P.w_scales == EP_SCALE_BLOCK) product_launch<WFMT, EXACT, EP_SCALE_BLOCK>(P, stream);
-  else if (P.w_scales == EP_SCALE_ROW_BLOCK) product_launch<WFMT, EXACT, EP_SCALE_ROW_BLOCK>(P, stream);
-  else product_launch<WFMT, EXACT, EP_SCALE_ROW>(P, stream);
+template <int WFMT, int OUT, int LAYOUT, int NW, int NX, int WW, int WX, int NS>
+void tiles_launch(const Product& P, int cus, hipStream_t stream) {
+  constexpr int TW = 16 * NW * WW, TX = 16 * NX * WX;
+  const uint32_t tx = (uint32_t)((P.m + TX - 1) / TX), tw = (uint32_t)((P.n + TW - 1) / TW);
+  const uint32_t tiles = tx * tw, last = tiles % cus, split = 2 * last <= (uint32_t)cus ? last : 0;
+  hipLaunchKernelGGL((product_tiles_kernel<WFMT, OUT, LAYOUT, NW, NX, WW, WX, NS>), dim3(tiles + split), dim3(64 * WW * WX),
+                     0, stream, P, tw, tx, tiles - split, split);
+}
+
+// ---- which kernel -----------------------------------------------------------------------
+// Workgroups of a launch, and how many of them a CU takes in all.
+int64_t rounds(int64_t groups, int cus) { return (groups + cus - 1) / cus; }
+
+// Rows of W for a workgroup of the streaming kernel: the multiple of 8 up to 16 NW that makes the
+// CU with the most work read the fewest rows.
+template <int NW, int NX>
+uint32_t ring_height(const Product& P, int cus) {
+  const int64_t tx = (P.m + 16 * NX - 1) / (16 * NX), rows_x = std::min<int64_t>(P.m, 16 * NX);
+  int64_t best = 16 * NW, least = INT64_MAX;
+  for (int64_t h = 16 * NW; h >= 8; h -= 8) {
+    const int64_t read = rounds((P.n + h - 1) / h * tx, cus) * (h + rows_x);
+    if (read < least) {
+      least = read;
+      best = h;
+    }
+  }
+  return (uint32_t)best;
+}
+
+template <int NX>
+int64_t ring_groups(const Product& P, uint32_t height) {
+  return (P.n + height - 1) / height * ((P.m + 16 * NX - 1) / (16 * NX));
+}
+
+template <int WFMT, int OUT, int LAYOUT, int NW, int NX, int KW, int NS>
+void ring_launch(const Product& P, uint32_t height, hipStream_t stream) {
+  const uint32_t strips = (uint32_t)((P.n + height - 1) / height), tx = (uint32_t)((P.m + 16 * NX - 1) / (16 * NX));
+  const uint32_t per_xcd = (strips + kXcds - 1) / kXcds;
+  hipLaunchKernelGGL((product_ring_kernel<WFMT, OUT, LAYOUT, NW, NX, KW, NS>), dim3(per_xcd * kXcds * tx), dim3(64 * KW), 0,
+                     stream, P, height, per_xcd);
+}
+
+// Time of a tiled launch on the busiest CU for each step along k, in ns, from its tiles: measured
+// with n = 5120 and 17408, k = 5120 and 17408, m = 64 .. 2048.  `half`: when it runs as half tiles
+// alone; `one`: a CU with one tile; `each`: with more, for each of them.
+struct TileCost {
+  int rows_w, rows_x, half, one, each;
+};
+constexpr TileCost kSmallTile = {128, 64, 510, 750, 490}, kMidTile = {128, 128, 780, 1170, 720},
+                   kLargeTile = {256, 256, 1310, 1970, 1970};
+
+int64_t tile_cost(const TileCost& c, const Product& P, int cus) {
+  const int64_t tiles = (P.m + c.rows_x - 1) / c.rows_x * ((P.n + c.rows_w - 1) / c.rows_w);
+  if (2 * tiles <= cus) return c.half;
+  if (tiles <= cus) return c.one;
+  const int64_t last = tiles % cus;
+  return std::max<int64_t>(c.one, c.each * (tiles / cus) + (last == 0 ? 0 : 2 * last <= cus ? c.half : c.each));
+}
+
+// Up to 16 rows of X the launch is W's stream from memory: 1 x 17408 x 5120 in 15.6 us with four
+// waves a workgroup, 18.0 with eight; 1 x 5120 x 17408, which has too few strips for several
+// workgroups on a CU, in 27.2 and 16.6.  Beyond, workgroups of the streaming kernel take 210 ns a
+// step with 48 x 32 rows and 270 with 48 x 64, and the tiled kernels what is stated above; the
+// least wins.
+template <int WFMT, int OUT, int LAYOUT>
+void product_launch(const Product& P, int cus, hipStream_t stream) {
+  if (P.m <= 16) {
+    const uint32_t h = ring_height<2, 1>(P, cus);
+    if (rounds(ring_groups<1>(P, h), cus) > 1) ring_launch<WFMT, OUT, LAYOUT, 2, 1, 4, 2>(P, h, stream);
+    else ring_launch<WFMT, OUT, LAYOUT, 2, 1, 8, 2>(P, h, stream);
+    return;
+  }
+  const uint32_t h2 = ring_height<3, 2>(P, cus), h4 = ring_height<3, 4>(P, cus);
+  const int64_t ring2 = 210 * rounds(ring_groups<2>(P, h2), cus), ring4 = 270 * rounds(ring_groups<4>(P, h4), cus);
+  const int64_t small = tile_cost(kSmallTile, P, cus), mid = tile_cost(kMidTile, P, cus),
+                large = tile_cost(kLargeTile, P, cus);
+  const int64_t least = std::min({ring2, ring4, small, mid, large});
+  if (least == large) tiles_launch<WFMT, OUT, LAYOUT, 8, 4, 2, 4, 2>(P, cus, stream);
+  else if (least == mid) tiles_launch<WFMT, OUT, LAYOUT, 4, 4, 2, 2, 2>(P, cus, stream);
+  else if (least == small) tiles_launch<WFMT, OUT, LAYOUT, 4, 2, 2, 2, 3>(P, cus, stream);
+  else if (least == ring4) ring_launch<WFMT, OUT, LAYOUT, 3, 4, 5, 2>(P, h4, stream);
+  else ring_launch<WFMT, OUT, LAYOUT, 3, 2, 6, 2>(P, h2, stream);
+}
+
+template <int WFMT, int OUT>
+void product_launch(const Product& P, int w_scales, int cus, hipStream_t stream) {
+  if (w_scales == EP_SCALE_BLOCK) product_launch<WFMT, OUT, EP_SCALE_BLOCK>(P, cus, stream);
+  else if (w_scales == EP_SCALE_ROW_BLOCK) product_launch<WFMT, OUT, EP_SCALE_ROW_BLOCK>(P, cus, stream);
+  else product_launch<WFMT, OUT, EP_SCALE_ROW>(P, cus, stream);
 }
 
 template <int WFMT>
-void product_launch(const Product& P, hipStream_t stream) {
-  if (P.y_dtype == EP_FP32) product_launch<WFMT, true>(P, stream);
-  else product_launch<WFMT, false>(P, stream);
+void product_launch(const Product& P, int w_scales, int y_dtype, int cus, hipStream_t stream) {
+  if (y_dtype == EP_FP32) product_launch<WFMT, EP_FP32>(P, w_scales, cus, stream);
+  else if (y_dtype == EP_FP16) product_launch<WFMT, EP_FP16>(P, w_scales, cus, stream);
+  else product_launch<WFMT, EP_BF16>(P, w_scales, cus, stream);
 }
 
 bool misaligned(const void* p) { return reinterpret_cast<uintptr_t>(p) & 15; }
@@ -510,11 +689,15 @@ extern "C" int ep_gemm_fp8_block(const void* d_x, const float* d_x_scale, const 
     return ep::fail(EP_ERR_ARG, "ep_gemm_fp8_block: null pointer");
   if (ep::misaligned(d_x) || ep::misaligned(d_w))
     return ep::fail(EP_ERR_ARG, "ep_gemm_fp8_block: operands must be 16-byte aligned");
+  int dev = 0, cus = 0;
+  if (hipGetDevice(&dev) != hipSuccess ||
+      hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0)
+    return ep::fail(EP_ERR_HIP, "ep_gemm_fp8_block: no device");
   const ep::Product P = {static_cast<const uint8_t*>(d_x), d_x_scale, static_cast<const uint8_t*>(d_w), d_w_scale,
-                         d_y, m, n, k, (uint32_t)((k + 127) / 128), (uint32_t)w_scales, (uint32_t)y_dtype};
+                         d_y, m, n, k, (uint32_t)((k + 127) / 128)};
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  if (w_dtype == EP_FP8_E4M3) ep::product_launch<0>(P, stream);
-  else ep::product_launch<1>(P, stream);
+  if (w_dtype == EP_FP8_E4M3) ep::product_launch<0>(P, w_scales, y_dtype, cus, stream);
+  else ep::product_launch<1>(P, w_scales, y_dtype, cus, stream);
   if (hipGetLastError() != hipSuccess) return ep::fail(EP_ERR_HIP, "ep_gemm_fp8_block: launch failed");
   return EP_OK;
 }
