@@ -20,6 +20,7 @@
 #include <algorithm>
 #include <cstdint>
 #include <string>
+#include <type_traits>
 
 #include "../../include/entropack.h"
 #include "common.h"
@@ -113,9 +114,7 @@ __device__ __forceinline__ float widen(uint16_t x) {
 template <bool FP16>
 __device__ __forceinline__ uint16_t narrow(float f) {
   if (FP16) return __builtin_bit_cast(uint16_t, (_Float16)f);
-  const uint32_t u = __float_as_uint(f);
-  if ((u & 0x7FFFFFFFu) > 0x7F800000u) return (uint16_t)((u >> 16) | 0x40u);
-  return (uint16_t)((u + 0x7FFFu + ((u >> 16) & 1u)) >> 16);
+  return __builtin_bit_cast(uint16_t, (__bf16)f);
 }
 
 // Over the four lanes that share a query (l mod 16).
@@ -134,6 +133,79 @@ __device__ __forceinline__ float exp2_from(float x, float m) {
   return __builtin_amdgcn_exp2f(x - (m == minus_inf() ? 0.0f : m));
 }
 
+// What one workgroup works on: a request's queries and keys, and one kv head.  Positions in a
+// request fit 32 bits.
+struct Work {
+  const int32_t* table;
+  int64_t q0, rows;      // first query; (query, head of the group) pairs
+  int32_t len, m, h;
+};
+
+__device__ __forceinline__ Work work_of(const Attn& A, uint32_t pair) {
+  Work W;
+  W.h = pair % A.heads;
+  const int64_t b = pair / A.heads;
+  W.len = (int32_t)min((int64_t)max(A.len[b], 0), min(A.table_ld << A.shift, (int64_t)0x7FFFFF00));
+  W.q0 = min((int64_t)max(A.cu[b], 0), A.total_q);
+  W.m = (int32_t)max(min((int64_t)max(A.cu[b + 1], 0), A.total_q) - W.q0, (int64_t)0);
+  W.rows = (int64_t)W.m * A.group;
+  W.table = A.table + b * A.table_ld;
+  return W;
+}
+
+// Page of token t, -1 where there is none to be seen.
+__device__ __forceinline__ int32_t page_at(const Attn& A, const Work& W, int32_t t) {
+  const int32_t p = t < W.len ? W.table[t >> A.shift] : -1;
+  return (int64_t)(uint32_t)p < A.n_pages ? p : -1;
+}
+
+// Keys [low, high) are seen by query row `row`; 0 <= low, high <= len.
+struct Span {
+  int32_t low, high;
+};
+
+__device__ __forceinline__ Span span_of(const Attn& A, const Work& W, int64_t row) {
+  if (!A.causal) return {0, W.len};
+  const int32_t high = max(W.len - W.m + (int32_t)(row / A.group) + 1, 0);   // at most len
+  return {A.window > 0 ? max(high - A.window, 0) : 0, high};
+}
+
+// A query row in FP16 at its own power of two: 16 channels of each 64 for a lane, those that its
+// key pieces hold.  Returns what a score is to be multiplied with.
+template <int D, bool FP16>
+__device__ __forceinline__ float load_query(const Attn& A, const Work& W, int64_t row, int quarter,
+                                            v8h (&q)[D / 64][2]) {
+  const int64_t i = row / A.group, g = row % A.group;
+  const uint16_t* const src = A.q + (W.q0 + i) * A.q_row + ((int64_t)W.h * A.group + g) * D + 16 * quarter;
+  v4u w[D / 64][2];
+  uint32_t top = 0;
+#pragma unroll
+  for (int p = 0; p < D / 64; p++)
+#pragma unroll
+    for (int e = 0; e < 2; e++) {
+      w[p][e] = *reinterpret_cast<const v4u*>(src + 64 * p + 8 * e);
+#pragma unroll
+      for (int c = 0; c < 4; c++) {
+        top = max(top, __float_as_uint(widen<FP16>((uint16_t)w[p][e][c])) & 0x7FFFFFFFu);
+        top = max(top, __float_as_uint(widen<FP16>((uint16_t)(w[p][e][c] >> 16))) & 0x7FFFFFFFu);
+      }
+    }
+  top = max(top, (uint32_t)__shfl_xor((int)top, 16));
+  top = max(top, (uint32_t)__shfl_xor((int)top, 32));
+  const uint32_t ex = max(top >> 23, 15u);                        // biased exponent of the largest
+  const float lift = __uint_as_float((268u - ex) << 23);          // 2^(14 - exponent)
+#pragma unroll
+  for (int p = 0; p < D / 64; p++)
+#pragma unroll
+    for (int e = 0; e < 2; e++)
+#pragma unroll
+      for (int c = 0; c < 4; c++) {
+        q[p][e][2 * c] = (_Float16)(widen<FP16>((uint16_t)w[p][e][c]) * lift);
+        q[p][e][2 * c + 1] = (_Float16)(widen<FP16>((uint16_t)(w[p][e][c] >> 16)) * lift);
+      }
+  return __uint_as_float((ex - 14u) << 23) * (A.scale * kLog2e);
+}
+
 // A tile of 16 query rows of one request and kv head, against one share of its tokens.  The
 // workgroup's waves take chunks of 64 tokens in turn and join their results in LDS.
 template <int D, bool INT8, bool FP16>
@@ -145,88 +217,36 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, quarter = lane >> 4;
-  const int h = blockIdx.x % A.heads;
-  const int64_t b = blockIdx.x / A.heads;
-  const int split = blockIdx.y;
-  const int64_t page_tokens = (int64_t)1 << A.shift;
+  const Work W = work_of(A, blockIdx.x);
+  const int split = blockIdx.y, page_tokens = 1 << A.shift;
+  const int64_t rows = W.rows, head_codes = (int64_t)page_tokens * D;
   const int64_t q_heads = (int64_t)A.heads * A.group;
-  const int64_t len = min((int64_t)max(A.len[b], 0), A.table_ld << A.shift);
-  const int64_t q0 = min((int64_t)max(A.cu[b], 0), A.total_q), q1 = min((int64_t)max(A.cu[b + 1], 0), A.total_q);
-  const int64_t m = q1 - q0, rows = m * A.group;
-  const int32_t* const table = A.table + b * A.table_ld;
-  const int64_t head_codes = page_tokens * D;
 
   for (int64_t tile = blockIdx.z; tile * kRows < rows; tile += gridDim.z) {
-    const int64_t row = tile * kRows + col;
-    const bool live = row < rows;
-    const int64_t i = min(row, rows - 1) / A.group, g = min(row, rows - 1) % A.group;
-    // keys [low, high) are seen by this row, [tile_low, tile_high) by any row of the tile
-    int64_t high = len, low = 0, tile_high = len, tile_low = 0, all_high = len, all_low = 0;
-    if (A.causal) {
-      const int64_t first = tile * kRows / A.group, last = min(tile * kRows + kRows - 1, rows - 1) / A.group;
-      high = len - m + i + 1;
-      tile_high = len - m + last + 1;
-      all_high = len - m + first + 1;
-      if (A.window > 0) {
-        low = high - A.window;
-        tile_low = max(all_high - A.window, (int64_t)0);
-        all_low = tile_high - A.window;
-      }
-    }
-    // this split's share of them
-    const int64_t share = (int64_t)split * A.split_tokens;
-    const int64_t begin = max(share, tile_low & ~(int64_t)(kChunk - 1));
-    const int64_t end = split == A.splits - 1 ? tile_high : min(share + A.split_tokens, tile_high);
+    const int64_t row = min(tile * kRows + col, rows - 1);
+    const Span mine = span_of(A, W, row), first = span_of(A, W, tile * kRows),
+               last = span_of(A, W, min(tile * kRows + kRows - 1, rows - 1));
+    // the split's share of the keys [first.low, last.high) that some row sees
+    const int share = split * A.split_tokens;
+    const int begin = max(share, first.low & ~(kChunk - 1));
+    const int end = split == A.splits - 1 ? last.high : min(share + A.split_tokens, last.high);
 
-    // the row's query: 16 channels of each 64 for a lane, in FP16 at the row's power of two
     v8h q[kPieces][2];
-    float row_scale;
-    {
-      const uint16_t* const src = A.q + (q0 + i) * A.q_row + (h * A.group + g) * D + 16 * quarter;
-      v4u w[kPieces][2];
-      uint32_t top = 0;
-#pragma unroll
-      for (int p = 0; p < kPieces; p++)
-#pragma unroll
-        for (int e = 0; e < 2; e++) {
-          w[p][e] = *reinterpret_cast<const v4u*>(src + 64 * p + 8 * e);
-#pragma unroll
-          for (int c = 0; c < 4; c++) {
-            top = max(top, __float_as_uint(widen<FP16>((uint16_t)w[p][e][c])) & 0x7FFFFFFFu);
-            top = max(top, __float_as_uint(widen<FP16>((uint16_t)(w[p][e][c] >> 16))) & 0x7FFFFFFFu);
-          }
-        }
-      top = max(top, (uint32_t)__shfl_xor((int)top, 16));
-      top = max(top, (uint32_t)__shfl_xor((int)top, 32));
-      const uint32_t ex = max(top >> 23, 15u);                        // biased exponent of the largest
-      const float lift = __uint_as_float((268u - ex) << 23);          // 2^(14 - exponent)
-      row_scale = __uint_as_float((ex - 14u) << 23) * (A.scale * kLog2e);
-#pragma unroll
-      for (int p = 0; p < kPieces; p++)
-#pragma unroll
-        for (int e = 0; e < 2; e++)
-#pragma unroll
-          for (int c = 0; c < 4; c++) {
-            q[p][e][2 * c] = (_Float16)(widen<FP16>((uint16_t)w[p][e][c]) * lift);
-            q[p][e][2 * c + 1] = (_Float16)(widen<FP16>((uint16_t)(w[p][e][c] >> 16)) * lift);
-          }
-    }
+    const float row_scale = load_query<D, FP16>(A, W, row, quarter, q);
 
     v4f o[kTiles];
 #pragma unroll
     for (int t = 0; t < kTiles; t++) o[t] = v4f{};
     float top = minus_inf(), total = 0.0f;
 
-    for (int64_t t0 = begin + kChunk * wave; t0 < end; t0 += kChunk * kWaves) {
+    for (int t0 = begin + kChunk * wave; t0 < end; t0 += kChunk * kWaves) {
       // pages of the tokens whose keys this lane loads, and of the tokens whose scores it holds
-      const int64_t tk = t0 + 16 * (col >> 2), tv = t0 + 16 * quarter;
-      uint32_t pk = tk < len ? (uint32_t)table[tk >> A.shift] : ~0u;
-      uint32_t pv = tv < len ? (uint32_t)table[tv >> A.shift] : ~0u;
-      const bool in_k = pk < A.n_pages, in_v = pv < A.n_pages;
+      const int tk = t0 + 16 * (col >> 2), tv = t0 + 16 * quarter;
+      const int32_t pk = page_at(A, W, tk), pv = page_at(A, W, tv);
       float ks = 0.0f, vs = 0.0f;
       v4u kc[4][kPieces], vc[kTiles];
-      if (in_k) {
-        const uint8_t* const src = A.k + ((int64_t)pk * A.heads + h) * head_codes +
+      if (pk >= 0) {
+        const uint8_t* const src = A.k + ((int64_t)pk * A.heads + W.h) * head_codes +
                                    ((tk & (page_tokens - 1)) + (col & 3)) * D + 16 * quarter;
 #pragma unroll
         for (int t = 0; t < 4; t++)
@@ -238,11 +258,11 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
 #pragma unroll
           for (int p = 0; p < kPieces; p++) kc[t][p] = v4u{};
       }
-      if (in_v) {
-        const uint8_t* const src = A.v + ((int64_t)pv * A.heads + h) * head_codes + (tv & (page_tokens - 1)) +
-                                   (int64_t)col * page_tokens;
-        ks = A.k_scale[(int64_t)pv * A.heads + h];
-        vs = A.v_scale[(int64_t)pv * A.heads + h];
+      if (pv >= 0) {
+        const uint8_t* const src =
+            A.v + ((int64_t)pv * A.heads + W.h) * head_codes + (tv & (page_tokens - 1)) + col * page_tokens;
+        ks = A.k_scale[(int64_t)pv * A.heads + W.h];
+        vs = A.v_scale[(int64_t)pv * A.heads + W.h];
 #pragma unroll
         for (int t = 0; t < kTiles; t++) vc[t] = *reinterpret_cast<const v4u*>(src + 16 * t * page_tokens);
       } else {
@@ -264,13 +284,13 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
         for (int r = 0; r < 4; r++) s[4 * t + r] = acc[r] * f;
       }
       // where a row of the tile does not see all of the chunk, or a page is missing
-      const bool cut = __any(t0 + kChunk > all_high || t0 < all_low || t0 + kChunk > len || !in_k || !in_v);
+      const bool cut = __any(t0 + kChunk > first.high || t0 < last.low || pk < 0 || pv < 0);
       uint32_t seen = 0xFFFFu;
       if (cut) {
         seen = 0;
 #pragma unroll
         for (int e = 0; e < 16; e++) {
-          const bool yes = in_v && live && tv + e < high && tv + e >= low && tv + e < len;
+          const bool yes = pv >= 0 && tv + e < mine.high && tv + e >= mine.low;
           seen |= (uint32_t)yes << e;
           s[e] = yes ? s[e] : minus_inf();
         }
@@ -338,7 +358,7 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
       }
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
       const float lse2 = l == 0.0f ? minus_inf() : all + __builtin_amdgcn_logf(l);
-      const int64_t token = q0 + out_row / A.group, head = h * A.group + out_row % A.group;
+      const int64_t token = W.q0 + out_row / A.group, head = W.h * A.group + out_row % A.group;
       if (A.splits > 1) {
         const int64_t at = ((int64_t)split * A.total_q + token) * q_heads + head;
 #pragma unroll
@@ -352,6 +372,276 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
       }
     }
     __syncthreads();
+  }
+}
+
+// ---- many query rows -----------------------------------------------------------------
+// A workgroup's four waves hold 32 query rows each (two column tiles; 16 for 256 channels) and share the chunks of 64
+// tokens, which direct loads bring to LDS as they lie in the cache, one chunk ahead.  Every wave
+// widens the codes it reads, so LDS and its bandwidth hold 8 bits a value.
+//
+// The weights enter the second product as FP16, lifted by 2^12.  The scale of a value page
+// multiplies them divided by `ref`, a power of two at least as large as every page's scale met so
+// far, so they stay inside FP16 whatever the scales are.  A row's maximum follows its scores only
+// when they pass it by more than 3 (weights stay below 2^15): the sums are rarely rescaled.
+constexpr int kPromptWaves = 4;
+constexpr int col_tiles(int dim) { return dim <= 128 ? 2 : 1; }   // what 256 registers hold
+constexpr int prompt_rows(int dim) { return kPromptWaves * col_tiles(dim) * 16; }
+constexpr float kLift = 12.0f, kSlack = 3.0f;
+
+typedef __attribute__((address_space(3))) uint8_t lds_u8;
+typedef __attribute__((address_space(1))) const uint8_t global_u8;
+
+// The largest over the four lanes that share a query, without LDS.
+__device__ __forceinline__ float swap_max4(float x) {
+  auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
+
+// Place of the 16-byte chunk j of token row r among its row's chunks: 16 lanes that read one chunk
+// of rows 16 (0 .. 3) + 4 i + (0 .. 3) meet 16 different 16-byte columns of the 64 banks.
+template <int D>
+__device__ __forceinline__ uint32_t key_place(uint32_t j, uint32_t r) {
+  if (D == 64) return j ^ ((r >> 4) & 3);
+  if (D == 128) return j ^ (((r >> 1) & 1) | ((r >> 4) & 3) << 1);
+  return j ^ ((r & 3) | ((r >> 4) & 3) << 2);
+}
+
+template <int D, bool INT8, bool FP16>
+__global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(Attn A) {
+  constexpr int kColTiles = col_tiles(D), kPromptRows = prompt_rows(D);
+  constexpr int kPieces = D / 64, kTiles = D / 16;
+  constexpr int kBytes = kChunk * D;                       // of a chunk's keys, and of its values
+  constexpr int kLoads = kBytes / 1024 / kPromptWaves;     // direct loads of a wave for each
+  __shared__ __attribute__((aligned(1024))) uint8_t lds_mem[2][2 * kBytes];
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int col = lane & 15, quarter = lane >> 4;
+  const Work W = work_of(A, blockIdx.x);
+  const int split = blockIdx.y, page_tokens = 1 << A.shift;
+  const int64_t head_codes = (int64_t)page_tokens * D, q_heads = (int64_t)A.heads * A.group;
+  // the run of 16 tokens that this lane's value loads are of (a KiB of values is 16 channels of
+  // four runs, run j of channel d at place j ^ (d / 4 mod 4))
+  const uint32_t v_run = (lane & 3) ^ (quarter & 3);
+
+  const int64_t tiles = (W.rows + kPromptRows - 1) / kPromptRows;
+  for (int64_t turn = blockIdx.z; turn < tiles; turn += gridDim.z) {
+    const int64_t tile = tiles - 1 - turn;   // the longest rows of a causal request first
+    const int64_t tile_first = tile * kPromptRows, wave_first = tile_first + 16 * kColTiles * wave;
+    const Span first = span_of(A, W, tile_first), last = span_of(A, W, min(tile_first + kPromptRows - 1, W.rows - 1));
+    const int share = split * A.split_tokens;
+    const int begin = max(share, first.low & ~(kChunk - 1));
+    const int end = split == A.splits - 1 ? last.high : min(share + A.split_tokens, last.high);
+    // keys [wave_a.low, wave_end) are seen by some row of this wave, [wave_b.low, wave_a.high) by all
+    const Span wave_a = span_of(A, W, min(wave_first, W.rows - 1)),
+               wave_b = span_of(A, W, min(wave_first + 16 * kColTiles - 1, W.rows - 1));
+    const int wave_end = wave_first < W.rows ? wave_b.high : 0;
+
+    Span span[kColTiles];
+    float row_scale[kColTiles], top[kColTiles], total[kColTiles];
+    v8h q[kColTiles][kPieces][2];
+    v4f o[kTiles][kColTiles];
+#pragma unroll
+    for (int n = 0; n < kColTiles; n++) {
+      const int64_t row = min(wave_first + 16 * n + col, W.rows - 1);
+      span[n] = span_of(A, W, row);
+      row_scale[n] = load_query<D, FP16>(A, W, row, quarter, q[n]);
+      top[n] = minus_inf();
+      total[n] = 0.0f;
+#pragma unroll
+      for (int t = 0; t < kTiles; t++) o[t][n] = v4f{};
+    }
+    float ref = 0.0f;
+
+    // Direct loads of chunk t0, whose run `quarter` lies in `page`: this wave takes every fourth KiB
+    // of the keys and of the values.  Runs with nothing to fetch take page 0, whose scores are
+    // masked and whose codes are cleaned.
+    auto fetch = [&](int t0, int32_t page, uint32_t stage) {
+      lds_u8* const dst = (lds_u8*)lds_mem[stage] + 1024 * wave;
+      const int32_t in = max(page, 0);
+#pragma unroll
+      for (int i = 0; i < kLoads; i++) {
+        const uint32_t at = 1024 * (kPromptWaves * i + wave), run = at / (16 * D);   // the same in all lanes
+        const int64_t p = __builtin_amdgcn_readlane(in, 16 * run);
+        const uint8_t* const src = A.k + (p * A.heads + W.h) * head_codes + ((t0 + 16 * run) & (page_tokens - 1)) * D;
+        const uint32_t r = (at + 16 * lane) / D, off = r % 16 * D + 16 * key_place<D>((at + 16 * lane) % D / 16, r);
+        __builtin_amdgcn_global_load_lds((global_u8*)(src + off), dst + 1024 * kPromptWaves * i, 16, 0, 0);
+      }
+      const int32_t p0 = __builtin_amdgcn_readlane(in, 0), p1 = __builtin_amdgcn_readlane(in, 16),
+                    p2 = __builtin_amdgcn_readlane(in, 32), p3 = __builtin_amdgcn_readlane(in, 48);
+      const int32_t pv = v_run & 2 ? (v_run & 1 ? p3 : p2) : (v_run & 1 ? p1 : p0);
+      const uint8_t* const src = A.v + ((int64_t)pv * A.heads + W.h) * head_codes + ((t0 + 16 * v_run) & (page_tokens - 1)) +
+                                 (16 * wave + (lane >> 2)) * page_tokens;
+#pragma unroll
+      for (int i = 0; i < kLoads; i++)
+        __builtin_amdgcn_global_load_lds((global_u8*)(src + 16 * kPromptWaves * i * page_tokens),
+                                         dst + kBytes + 1024 * kPromptWaves * i, 16, 0, 0);
+    };
+
+    auto chunk = [&](int t0, uint32_t stage, int32_t page, float ks, float vs, auto cut_c) {
+      constexpr bool CUT = decltype(cut_c)::value;
+      const lds_u8* const keys = (const lds_u8*)lds_mem[stage];
+      const lds_u8* const values = keys + kBytes;
+      const int tv = t0 + 16 * quarter;
+      v4f s[4][kColTiles];
+#pragma unroll
+      for (int t = 0; t < 4; t++) {
+#pragma unroll
+        for (int n = 0; n < kColTiles; n++) s[t][n] = v4f{};
+        const uint32_t r = 16 * (col >> 2) + 4 * t + (col & 3);
+#pragma unroll
+        for (int p = 0; p < kPieces; p++) {
+          const v4u c = *reinterpret_cast<const __attribute__((address_space(3))) v4u*>(
+              keys + r * D + 16 * key_place<D>(4 * p + quarter, r));
+          const v8h a = widen8<INT8>(c[0], c[1]), b = widen8<INT8>(c[2], c[3]);
+#pragma unroll
+          for (int n = 0; n < kColTiles; n++) {
+            s[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, q[n][p][0], s[t][n], 0, 0, 0);
+            s[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, q[n][p][1], s[t][n], 0, 0, 0);
+          }
+        }
+      }
+      // ref to the power of two above the largest finite scale, if that is larger
+      const float most = swap_max4(vs < __builtin_inff() ? vs : 0.0f);
+      if (__any(most > ref)) {
+        const float now = __uint_as_float(min((__float_as_uint(most) >> 23) + 1, 254u) << 23);
+        const float keep = ref / now;
+        ref = now;
+#pragma unroll
+        for (int t = 0; t < kTiles; t++)
+#pragma unroll
+          for (int n = 0; n < kColTiles; n++) o[t][n] *= keep;
+      }
+      const float part = ref > 0.0f ? vs / ref : vs;
+      v8h w[2][kColTiles];
+#pragma unroll
+      for (int n = 0; n < kColTiles; n++) {
+        const float f = ks * row_scale[n];
+        if (CUT) {
+#pragma unroll
+          for (int t = 0; t < 4; t++)
+#pragma unroll
+            for (int r = 0; r < 4; r++) {
+              const int at = tv + 4 * t + r;
+              s[t][n][r] = page >= 0 && at < span[n].high && at >= span[n].low ? s[t][n][r] * f : minus_inf();
+            }
+        }
+        float mx = fmaxf(fmaxf(s[0][n][0], s[0][n][1]), s[0][n][2]);
+        mx = fmaxf(mx, s[0][n][3]);
+#pragma unroll
+        for (int t = 1; t < 4; t++) {
+          mx = fmaxf(fmaxf(mx, s[t][n][0]), s[t][n][1]);
+          mx = fmaxf(fmaxf(mx, s[t][n][2]), s[t][n][3]);
+        }
+        if (!CUT) mx *= f;
+        mx = swap_max4(mx);
+        if (__any(mx > top[n] + kSlack)) {
+          const float now = mx > top[n] + kSlack ? mx : top[n];
+          const float keep = exp2_from(top[n], now);
+          total[n] *= keep;
+#pragma unroll
+          for (int t = 0; t < kTiles; t++) o[t][n] *= keep;
+          top[n] = now;
+        }
+        const float base = kLift - (top[n] == minus_inf() ? 0.0f : top[n]);
+        float sum = 0.0f;
+#pragma unroll
+        for (int t = 0; t < 4; t++)
+#pragma unroll
+          for (int r = 0; r < 4; r++) {
+            const float e = __builtin_amdgcn_exp2f(CUT ? s[t][n][r] + base : __builtin_fmaf(s[t][n][r], f, base));
+            sum += e;
+            // a masked weight is zero whatever its page's scale is
+            w[t >> 1][n][4 * (t & 1) + r] = (_Float16)(CUT && s[t][n][r] == minus_inf() ? 0.0f : e * part);
+          }
+        total[n] += sum;
+      }
+#pragma unroll
+      for (int t = 0; t < kTiles; t++) {
+        const uint32_t d = 16 * t + col;
+        v4u c = *reinterpret_cast<const __attribute__((address_space(3))) v4u*>(
+            values + d * kChunk + 16 * (quarter ^ ((d >> 2) & 3)));
+        if (CUT && !INT8) {
+#pragma unroll
+          for (int i = 0; i < 4; i++) c[i] = without_nans(c[i]);
+        }
+        const v8h a = widen8<INT8>(c[0], c[1]), b = widen8<INT8>(c[2], c[3]);
+#pragma unroll
+        for (int n = 0; n < kColTiles; n++) {
+          o[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, w[0][n], o[t][n], 0, 0, 0);
+          o[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, w[1][n], o[t][n], 0, 0, 0);
+        }
+      }
+    };
+
+    // this chunk's page and scales, and the next one's page, of the lane's run of 16 tokens: loaded
+    // a chunk ahead of their use, as the codes are
+    int32_t page = page_at(A, W, begin + 16 * quarter), next = page_at(A, W, begin + kChunk + 16 * quarter);
+    float ks = 0.0f, vs = 0.0f;
+    auto scales = [&](int32_t p, float& k, float& v) {
+      const int64_t at = (int64_t)max(p, 0) * A.heads + W.h;
+      k = A.k_scale[at];
+      v = A.v_scale[at];
+    };
+    if (begin < end) {
+      fetch(begin, page, 0);
+      scales(page, ks, vs);
+    }
+    uint32_t stage = 0;
+    for (int t0 = begin; t0 < end; t0 += kChunk) {
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_waitcnt(0x70);   // vmcnt(0) lgkmcnt(0): this chunk has landed, the last one is read
+      __builtin_amdgcn_s_barrier();
+      __builtin_amdgcn_sched_barrier(0);
+      int32_t after = -1;
+      float next_ks = 0.0f, next_vs = 0.0f;
+      if (t0 + kChunk < end) {
+        fetch(t0 + kChunk, next, stage ^ 1);
+        scales(next, next_ks, next_vs);
+        after = page_at(A, W, t0 + 2 * kChunk + 16 * quarter);
+      }
+      if (t0 < wave_end && t0 + kChunk > wave_a.low) {
+        const float v = page < 0 ? 0.0f : vs;
+        if (t0 + kChunk > wave_a.high || t0 < wave_b.low || __any(page < 0)) chunk(t0, stage, page, ks, v, std::true_type{});
+        else chunk(t0, stage, page, ks, v, std::false_type{});
+      }
+      page = next;
+      next = after;
+      ks = next_ks;
+      vs = next_vs;
+      stage ^= 1;
+    }
+    __syncthreads();   // before the next tile's loads
+
+#pragma unroll
+    for (int n = 0; n < kColTiles; n++) {
+      const int64_t row = wave_first + 16 * n + col;
+      const float l = sum4(total[n]);
+      if (row >= W.rows) continue;
+      const float inv = l == 0.0f ? 0.0f : ref / l;
+      const float lse2 = l == 0.0f ? minus_inf() : top[n] - kLift + __builtin_amdgcn_logf(l);
+      const int64_t token = W.q0 + row / A.group, head = W.h * A.group + row % A.group;
+      if (A.splits > 1) {
+        const int64_t at = ((int64_t)split * A.total_q + token) * q_heads + head;
+#pragma unroll
+        for (int t = 0; t < kTiles; t++)
+          *reinterpret_cast<v4f*>(A.part_out + at * D + 16 * t + 4 * quarter) = o[t][n] * inv;
+        if (quarter == 0) A.part_lse[at] = lse2;
+      } else {
+        uint16_t* const dst = A.out + token * A.out_row + head * D + 4 * quarter;
+#pragma unroll
+        for (int t = 0; t < kTiles; t++) {
+          typedef uint16_t v4s __attribute__((ext_vector_type(4)));
+          v4s x;
+#pragma unroll
+          for (int r = 0; r < 4; r++) x[r] = narrow<FP16>(o[t][n][r] * inv);
+          *reinterpret_cast<v4s*>(dst + 16 * t) = x;
+        }
+        if (quarter == 0 && A.lse) A.lse[token * q_heads + head] = lse2 * kLn2;
+      }
+    }
   }
 }
 
@@ -390,6 +680,7 @@ const char* call_fault(const ep_kv8_cache* c, const ep_kv8_attn* a) {
   if (a->table_ld <= 0 || a->table_ld > 0x7FFFFFFF) return "table_ld outside 1 .. 2^31 - 1";
   if (a->total_q < 0 || a->total_q > 0x7FFFFFFF) return "total_q outside 0 .. 2^31 - 1";
   if (a->window < 0 || (a->window && !a->causal)) return "a window needs causal, and must not be negative";
+  if (!(a->scale >= 0.0f && a->scale < __builtin_inff())) return "scale must be finite and not negative";
   if (a->max_q <= 0 || a->max_len < 0) return "max_q must be positive and max_len not negative";
   const int64_t width = (int64_t)a->q_heads * c->head_dim;
   if ((a->q_row && a->q_row < width) || (a->out_row && a->out_row < width) || a->q_row % 8 || a->out_row % 8)
@@ -400,23 +691,24 @@ const char* call_fault(const ep_kv8_cache* c, const ep_kv8_attn* a) {
   return nullptr;
 }
 
-// How a call's keys are shared out.  Workgroups are (row tile, request and head, split).
+// How a call's keys are shared out.  Workgroups are (request and head, split, row tile).
 struct Plan {
   int64_t tiles, splits, split_tokens, max_q;
+  bool prompt;
 };
-
-constexpr int64_t kWantGroups = 4096;
-constexpr int64_t kLeastTokens = kChunk * kWaves;
 
 Plan plan_of(const ep_kv8_cache& c, const ep_kv8_attn& a) {
   Plan P;
-  const int64_t group = a.q_heads / c.kv_heads;
-  P.tiles = std::min<int64_t>((a.max_q * group + kRows - 1) / kRows, 65535);
+  const int64_t rows = a.max_q * (int64_t)(a.q_heads / c.kv_heads);
   P.max_q = a.max_q;
-  const int64_t base = P.tiles * a.n_req * c.kv_heads;   // below 2^40
-  const int64_t most = std::max<int64_t>(1, (a.max_len + kLeastTokens - 1) / kLeastTokens);
-  P.splits = std::min<int64_t>({std::max<int64_t>(1, kWantGroups / base), most, 256});
-  P.split_tokens = (std::max<int64_t>(a.max_len, 1) + P.splits - 1) / P.splits;
+  P.prompt = rows > 32;
+  const int64_t tile = P.prompt ? prompt_rows(c.head_dim) : kRows, want = P.prompt ? 1024 : 4096, least = P.prompt ? 512 : 256;
+  P.tiles = std::min<int64_t>((rows + tile - 1) / tile, 65535);
+  const int64_t base = P.tiles * a.n_req * c.kv_heads;
+  const int64_t max_len = std::min(std::max(a.max_len, 1), 1 << 30);   // the last split takes what is past it
+  const int64_t most = (max_len + least - 1) / least;
+  P.splits = std::min<int64_t>({std::max<int64_t>(1, want / base), most, 256});
+  P.split_tokens = (max_len + P.splits - 1) / P.splits;
   P.split_tokens = (P.split_tokens + kChunk - 1) / kChunk * kChunk;
   return P;
 }
@@ -428,9 +720,11 @@ uint64_t plan_bytes(const Plan& P, const ep_kv8_cache& c, const ep_kv8_attn& a) 
 
 template <int D, bool INT8, bool FP16>
 void attention_launch(const Attn& A, const Plan& P, int64_t n_req, hipStream_t stream) {
-  hipLaunchKernelGGL((attention_rows_kernel<D, INT8, FP16>),
-                     dim3((uint32_t)(n_req * A.heads), (uint32_t)P.splits, (uint32_t)P.tiles), dim3(64 * kWaves), 0,
-                     stream, A);
+  const dim3 grid((uint32_t)(n_req * A.heads), (uint32_t)P.splits, (uint32_t)P.tiles);
+  if (P.prompt)
+    hipLaunchKernelGGL((attention_prompt_kernel<D, INT8, FP16>), grid, dim3(64 * kPromptWaves), 0, stream, A);
+  else
+    hipLaunchKernelGGL((attention_rows_kernel<D, INT8, FP16>), grid, dim3(64 * kWaves), 0, stream, A);
   if (P.splits > 1) {
     const int64_t rows = P.max_q * A.heads * A.group, per = 256 / (D / 4);
     hipLaunchKernelGGL((attention_join_kernel<D, FP16>),
