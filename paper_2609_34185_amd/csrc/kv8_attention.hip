@@ -137,8 +137,9 @@ __device__ __forceinline__ float exp2_from(float x, float m) {
 // request fit 32 bits.
 struct Work {
   const int32_t* table;
-  int64_t q0, rows;      // first query; (query, head of the group) pairs
+  int64_t q0;            // first query
   int32_t len, m, h;
+  uint32_t rows;         // (query, head of the group) pairs
 };
 
 __device__ __forceinline__ Work work_of(const Attn& A, uint32_t pair) {
@@ -148,7 +149,7 @@ __device__ __forceinline__ Work work_of(const Attn& A, uint32_t pair) {
   W.len = (int32_t)min((int64_t)max(A.len[b], 0), min(A.table_ld << A.shift, (int64_t)0x7FFFFF00));
   W.q0 = min((int64_t)max(A.cu[b], 0), A.total_q);
   W.m = (int32_t)max(min((int64_t)max(A.cu[b + 1], 0), A.total_q) - W.q0, (int64_t)0);
-  W.rows = (int64_t)W.m * A.group;
+  W.rows = (uint32_t)W.m * A.group;      // total_q * q_heads is below 2^31
   W.table = A.table + b * A.table_ld;
   return W;
 }
@@ -164,18 +165,18 @@ struct Span {
   int32_t low, high;
 };
 
-__device__ __forceinline__ Span span_of(const Attn& A, const Work& W, int64_t row) {
+__device__ __forceinline__ Span span_of(const Attn& A, const Work& W, uint32_t row) {
   if (!A.causal) return {0, W.len};
-  const int32_t high = max(W.len - W.m + (int32_t)(row / A.group) + 1, 0);   // at most len
+  const int32_t high = max(W.len - W.m + (int32_t)(row / (uint32_t)A.group) + 1, 0);   // at most len
   return {A.window > 0 ? max(high - A.window, 0) : 0, high};
 }
 
 // A query row in FP16 at its own power of two: 16 channels of each 64 for a lane, those that its
 // key pieces hold.  Returns what a score is to be multiplied with.
 template <int D, bool FP16>
-__device__ __forceinline__ float load_query(const Attn& A, const Work& W, int64_t row, int quarter,
+__device__ __forceinline__ float load_query(const Attn& A, const Work& W, uint32_t row, int quarter,
                                             v8h (&q)[D / 64][2]) {
-  const int64_t i = row / A.group, g = row % A.group;
+  const uint32_t i = row / (uint32_t)A.group, g = row - i * A.group;
   const uint16_t* const src = A.q + (W.q0 + i) * A.q_row + ((int64_t)W.h * A.group + g) * D + 16 * quarter;
   v4u w[D / 64][2];
   uint32_t top = 0;
@@ -219,11 +220,12 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
   const int col = lane & 15, quarter = lane >> 4;
   const Work W = work_of(A, blockIdx.x);
   const int split = blockIdx.y, page_tokens = 1 << A.shift;
-  const int64_t rows = W.rows, head_codes = (int64_t)page_tokens * D;
+  const uint32_t rows = W.rows;
+  const int64_t head_codes = (int64_t)page_tokens * D;
   const int64_t q_heads = (int64_t)A.heads * A.group;
 
-  for (int64_t tile = blockIdx.z; tile * kRows < rows; tile += gridDim.z) {
-    const int64_t row = min(tile * kRows + col, rows - 1);
+  for (uint32_t tile = blockIdx.z; tile * kRows < rows; tile += gridDim.z) {
+    const uint32_t row = min(tile * kRows + col, rows - 1);
     const Span mine = span_of(A, W, row), first = span_of(A, W, tile * kRows),
                last = span_of(A, W, min(tile * kRows + kRows - 1, rows - 1));
     // the split's share of the keys [first.low, last.high) that some row sees
@@ -344,7 +346,7 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
     __syncthreads();
     constexpr int kPer = kRows * D / (64 * kWaves);   // outputs of a thread, in one row
     const int r = threadIdx.x / (D / kPer), c0 = threadIdx.x % (D / kPer) * kPer;
-    const int64_t out_row = tile * kRows + r;
+    const uint32_t out_row = tile * kRows + r;
     if (out_row < rows) {
       float all = minus_inf(), l = 0.0f, v[kPer] = {};
 #pragma unroll
@@ -358,7 +360,7 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
       }
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
       const float lse2 = l == 0.0f ? minus_inf() : all + __builtin_amdgcn_logf(l);
-      const int64_t token = W.q0 + out_row / A.group, head = W.h * A.group + out_row % A.group;
+      const int64_t token = W.q0 + out_row / (uint32_t)A.group, head = W.h * A.group + out_row % (uint32_t)A.group;
       if (A.splits > 1) {
         const int64_t at = ((int64_t)split * A.total_q + token) * q_heads + head;
 #pragma unroll
@@ -392,12 +394,17 @@ constexpr float kLift = 12.0f, kSlack = 3.0f;
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 typedef __attribute__((address_space(1))) const uint8_t global_u8;
 
+// One instruction, without the steps that quiet an operand first; a NaN stays one.
+__device__ __forceinline__ float max3(float a, float b, float c) {
+  return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c);
+}
+
 // The largest over the four lanes that share a query, without LDS.
 __device__ __forceinline__ float swap_max4(float x) {
   auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  x = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  x = max3(__uint_as_float(a[0]), __uint_as_float(a[1]), __uint_as_float(a[1]));
   a = __builtin_amdgcn_permlane32_swap(__float_as_uint(x), __float_as_uint(x), false, false);
-  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  return max3(__uint_as_float(a[0]), __uint_as_float(a[1]), __uint_as_float(a[1]));
 }
 
 // Place of the 16-byte chunk j of token row r among its row's chunks: 16 lanes that read one chunk
@@ -426,10 +433,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
   // four runs, run j of channel d at place j ^ (d / 4 mod 4))
   const uint32_t v_run = (lane & 3) ^ (quarter & 3);
 
-  const int64_t tiles = (W.rows + kPromptRows - 1) / kPromptRows;
-  for (int64_t turn = blockIdx.z; turn < tiles; turn += gridDim.z) {
-    const int64_t tile = tiles - 1 - turn;   // the longest rows of a causal request first
-    const int64_t tile_first = tile * kPromptRows, wave_first = tile_first + 16 * kColTiles * wave;
+  const uint32_t tiles = (W.rows + kPromptRows - 1) / kPromptRows;
+  for (uint32_t turn = blockIdx.z; turn < tiles; turn += gridDim.z) {
+    const uint32_t tile = tiles - 1 - turn;   // the longest rows of a causal request first
+    const uint32_t tile_first = tile * kPromptRows, wave_first = tile_first + 16 * kColTiles * wave;
     const Span first = span_of(A, W, tile_first), last = span_of(A, W, min(tile_first + kPromptRows - 1, W.rows - 1));
     const int share = split * A.split_tokens;
     const int begin = max(share, first.low & ~(kChunk - 1));
@@ -445,7 +452,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
     v4f o[kTiles][kColTiles];
 #pragma unroll
     for (int n = 0; n < kColTiles; n++) {
-      const int64_t row = min(wave_first + 16 * n + col, W.rows - 1);
+      const uint32_t row = min(wave_first + 16 * n + col, W.rows - 1);
       span[n] = span_of(A, W, row);
       row_scale[n] = load_query<D, FP16>(A, W, row, quarter, q[n]);
       top[n] = minus_inf();
@@ -480,11 +487,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
                                          dst + kBytes + 1024 * kPromptWaves * i, 16, 0, 0);
     };
 
-    auto chunk = [&](int t0, uint32_t stage, int32_t page, float ks, float vs, auto cut_c) {
-      constexpr bool CUT = decltype(cut_c)::value;
+    // One chunk.  cut: some row of the wave does not see all of it.
+    auto chunk = [&](int t0, uint32_t stage, int32_t page, float ks, float vs, bool cut) {
       const lds_u8* const keys = (const lds_u8*)lds_mem[stage];
       const lds_u8* const values = keys + kBytes;
-      const int tv = t0 + 16 * quarter;
       v4f s[4][kColTiles];
 #pragma unroll
       for (int t = 0; t < 4; t++) {
@@ -503,6 +509,26 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
           }
         }
       }
+      float f[kColTiles];
+#pragma unroll
+      for (int n = 0; n < kColTiles; n++) f[n] = ks * row_scale[n];
+      if (cut) {
+        // scores as they are, -infinity where unseen; a value scale that is not finite makes the
+        // rows that see its page not-a-number, and no others
+        const int tv = t0 + 16 * quarter;
+        const bool bad = !(fabsf(vs) < __builtin_inff());
+#pragma unroll
+        for (int n = 0; n < kColTiles; n++) {
+          const int low = page >= 0 ? span[n].low - tv : 16, high = span[n].high - tv;
+#pragma unroll
+          for (int e = 0; e < 16; e++) {
+            const float x = bad ? __builtin_nanf("") : s[e >> 2][n][e & 3] * f[n];
+            s[e >> 2][n][e & 3] = e >= low && e < high ? x : minus_inf();
+          }
+          f[n] = 1.0f;
+        }
+        if (bad) vs = 0.0f;
+      }
       // ref to the power of two above the largest finite scale, if that is larger
       const float most = swap_max4(vs < __builtin_inff() ? vs : 0.0f);
       if (__any(most > ref)) {
@@ -514,29 +540,22 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
 #pragma unroll
           for (int n = 0; n < kColTiles; n++) o[t][n] *= keep;
       }
-      const float part = ref > 0.0f ? vs / ref : vs;
+      // the page's share of ref goes into the exponent, and out of the sum of weights again; what is
+      // below 2^-100 (zero among it) is nothing in FP16 either way
+      float part = ref > 0.0f ? vs / ref : vs;
+      part = part < 0x1p-100f ? 0x1p-100f : part;
+      const float lift = kLift + __builtin_amdgcn_logf(part), back = __builtin_amdgcn_rcpf(part);
       v8h w[2][kColTiles];
 #pragma unroll
       for (int n = 0; n < kColTiles; n++) {
-        const float f = ks * row_scale[n];
-        if (CUT) {
-#pragma unroll
-          for (int t = 0; t < 4; t++)
-#pragma unroll
-            for (int r = 0; r < 4; r++) {
-              const int at = tv + 4 * t + r;
-              s[t][n][r] = page >= 0 && at < span[n].high && at >= span[n].low ? s[t][n][r] * f : minus_inf();
-            }
-        }
-        float mx = fmaxf(fmaxf(s[0][n][0], s[0][n][1]), s[0][n][2]);
-        mx = fmaxf(mx, s[0][n][3]);
-#pragma unroll
-        for (int t = 1; t < 4; t++) {
-          mx = fmaxf(fmaxf(mx, s[t][n][0]), s[t][n][1]);
-          mx = fmaxf(fmaxf(mx, s[t][n][2]), s[t][n][3]);
-        }
-        if (!CUT) mx *= f;
-        mx = swap_max4(mx);
+        float mx = max3(s[0][n][0], s[0][n][1], s[0][n][2]);
+        mx = max3(mx, s[0][n][3], s[1][n][0]);
+        mx = max3(mx, s[1][n][1], s[1][n][2]);
+        mx = max3(mx, s[1][n][3], s[2][n][0]);
+        mx = max3(mx, s[2][n][1], s[2][n][2]);
+        mx = max3(mx, s[2][n][3], s[3][n][0]);
+        mx = max3(mx, s[3][n][1], s[3][n][2]);
+        mx = swap_max4(max3(mx, s[3][n][3], s[3][n][3]) * f[n]);
         if (__any(mx > top[n] + kSlack)) {
           const float now = mx > top[n] + kSlack ? mx : top[n];
           const float keep = exp2_from(top[n], now);
@@ -545,25 +564,24 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
           for (int t = 0; t < kTiles; t++) o[t][n] *= keep;
           top[n] = now;
         }
-        const float base = kLift - (top[n] == minus_inf() ? 0.0f : top[n]);
+        const float base = lift - (top[n] == minus_inf() ? 0.0f : top[n]);
         float sum = 0.0f;
 #pragma unroll
         for (int t = 0; t < 4; t++)
 #pragma unroll
           for (int r = 0; r < 4; r++) {
-            const float e = __builtin_amdgcn_exp2f(CUT ? s[t][n][r] + base : __builtin_fmaf(s[t][n][r], f, base));
+            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][n][r], f[n], base));
             sum += e;
-            // a masked weight is zero whatever its page's scale is
-            w[t >> 1][n][4 * (t & 1) + r] = (_Float16)(CUT && s[t][n][r] == minus_inf() ? 0.0f : e * part);
+            w[t >> 1][n][4 * (t & 1) + r] = (_Float16)e;
           }
-        total[n] += sum;
+        total[n] = __builtin_fmaf(sum, back, total[n]);
       }
 #pragma unroll
       for (int t = 0; t < kTiles; t++) {
         const uint32_t d = 16 * t + col;
         v4u c = *reinterpret_cast<const __attribute__((address_space(3))) v4u*>(
             values + d * kChunk + 16 * (quarter ^ ((d >> 2) & 3)));
-        if (CUT && !INT8) {
+        if (cut && !INT8) {
 #pragma unroll
           for (int i = 0; i < 4; i++) c[i] = without_nans(c[i]);
         }
@@ -603,9 +621,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
         after = page_at(A, W, t0 + 2 * kChunk + 16 * quarter);
       }
       if (t0 < wave_end && t0 + kChunk > wave_a.low) {
-        const float v = page < 0 ? 0.0f : vs;
-        if (t0 + kChunk > wave_a.high || t0 < wave_b.low || __any(page < 0)) chunk(t0, stage, page, ks, v, std::true_type{});
-        else chunk(t0, stage, page, ks, v, std::false_type{});
+        const bool cut = t0 + kChunk > wave_a.high || t0 < wave_b.low || __any(page < 0);
+        chunk(t0, stage, page, page < 0 ? 0.0f : ks, page < 0 ? 0.0f : vs, cut);
       }
       page = next;
       next = after;
@@ -617,12 +634,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
 
 #pragma unroll
     for (int n = 0; n < kColTiles; n++) {
-      const int64_t row = wave_first + 16 * n + col;
+      const uint32_t row = wave_first + 16 * n + col;
       const float l = sum4(total[n]);
       if (row >= W.rows) continue;
       const float inv = l == 0.0f ? 0.0f : ref / l;
       const float lse2 = l == 0.0f ? minus_inf() : top[n] - kLift + __builtin_amdgcn_logf(l);
-      const int64_t token = W.q0 + row / A.group, head = W.h * A.group + row % A.group;
+      const int64_t token = W.q0 + row / (uint32_t)A.group, head = W.h * A.group + row % (uint32_t)A.group;
       if (A.splits > 1) {
         const int64_t at = ((int64_t)split * A.total_q + token) * q_heads + head;
 #pragma unroll
@@ -679,6 +696,7 @@ const char* call_fault(const ep_kv8_cache* c, const ep_kv8_attn* a) {
   if (a->n_req <= 0 || a->n_req > 0xFFFFFF / c->kv_heads) return "n_req * kv_heads outside 1 .. 2^24 - 1";
   if (a->table_ld <= 0 || a->table_ld > 0x7FFFFFFF) return "table_ld outside 1 .. 2^31 - 1";
   if (a->total_q < 0 || a->total_q > 0x7FFFFFFF) return "total_q outside 0 .. 2^31 - 1";
+  if (a->total_q * a->q_heads > 0x7FFFFFFF) return "total_q * q_heads above 2^31 - 1";
   if (a->window < 0 || (a->window && !a->causal)) return "a window needs causal, and must not be negative";
   if (!(a->scale >= 0.0f && a->scale < __builtin_inff())) return "scale must be finite and not negative";
   if (a->max_q <= 0 || a->max_len < 0) return "max_q must be positive and max_len not negative";
