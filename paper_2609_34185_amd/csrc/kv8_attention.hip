@@ -154,10 +154,14 @@ __device__ __forceinline__ Work work_of(const Attn& A, uint32_t pair) {
   return W;
 }
 
-// Page of token t, -1 where there is none to be seen.
-__device__ __forceinline__ int32_t page_at(const Attn& A, const Work& W, int32_t t) {
-  const int32_t p = t < W.len ? W.table[t >> A.shift] : -1;
-  return (int64_t)(uint32_t)p < A.n_pages ? p : -1;
+// The table's entry for token t of a request that has tokens (past the last one, the last one's),
+// and the page that it stands for: -1 where there is none to be seen.  Apart, so that an entry can
+// be on its way while something else is done.
+__device__ __forceinline__ int32_t entry_at(const Attn& A, const Work& W, int32_t t) {
+  return W.table[min(t, W.len - 1) >> A.shift];
+}
+__device__ __forceinline__ int32_t page_of(const Attn& A, const Work& W, int32_t t, int32_t entry) {
+  return t < W.len && (uint32_t)entry < (uint32_t)A.n_pages ? entry : -1;
 }
 
 // Keys [low, high) are seen by query row `row`; 0 <= low, high <= len.
@@ -244,7 +248,7 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
     for (int t0 = begin + kChunk * wave; t0 < end; t0 += kChunk * kWaves) {
       // pages of the tokens whose keys this lane loads, and of the tokens whose scores it holds
       const int tk = t0 + 16 * (col >> 2), tv = t0 + 16 * quarter;
-      const int32_t pk = page_at(A, W, tk), pv = page_at(A, W, tv);
+      const int32_t pk = page_of(A, W, tk, entry_at(A, W, tk)), pv = page_of(A, W, tv, entry_at(A, W, tv));
       float ks = 0.0f, vs = 0.0f;
       v4u kc[4][kPieces], vc[kTiles];
       if (pk >= 0) {
@@ -460,7 +464,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
 #pragma unroll
       for (int t = 0; t < kTiles; t++) o[t][n] = v4f{};
     }
-    float ref = 0.0f;
+    float ref = 0.0f, per_ref = 1.0f;   // and 1 / ref
 
     // Direct loads of chunk t0, whose run `quarter` lies in `page`: this wave takes every fourth KiB
     // of the keys and of the values.  Runs with nothing to fetch take page 0, whose scores are
@@ -532,9 +536,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
       // ref to the power of two above the largest finite scale, if that is larger
       const float most = swap_max4(vs < __builtin_inff() ? vs : 0.0f);
       if (__any(most > ref)) {
-        const float now = __uint_as_float(min((__float_as_uint(most) >> 23) + 1, 254u) << 23);
-        const float keep = ref / now;
-        ref = now;
+        const uint32_t ex = min((__float_as_uint(most) >> 23) + 1, 253u);
+        per_ref = __uint_as_float((254 - ex) << 23);
+        const float keep = ref * per_ref;
+        ref = __uint_as_float(ex << 23);
 #pragma unroll
         for (int t = 0; t < kTiles; t++)
 #pragma unroll
@@ -542,7 +547,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
       }
       // the page's share of ref goes into the exponent, and out of the sum of weights again; what is
       // below 2^-100 (zero among it) is nothing in FP16 either way
-      float part = ref > 0.0f ? vs / ref : vs;
+      float part = vs * per_ref;
       part = part < 0x1p-100f ? 0x1p-100f : part;
       const float lift = kLift + __builtin_amdgcn_logf(part), back = __builtin_amdgcn_rcpf(part);
       v8h w[2][kColTiles];
@@ -594,9 +599,9 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
       }
     };
 
-    // this chunk's page and scales, and the next one's page, of the lane's run of 16 tokens: loaded
-    // a chunk ahead of their use, as the codes are
-    int32_t page = page_at(A, W, begin + 16 * quarter), next = page_at(A, W, begin + kChunk + 16 * quarter);
+    // page and scales of the lane's run of 16 tokens, and the table's entry of the next chunk's:
+    // loaded a chunk before they are used, as the codes are
+    int32_t page = -1, entry = -1;
     float ks = 0.0f, vs = 0.0f;
     auto scales = [&](int32_t p, float& k, float& v) {
       const int64_t at = (int64_t)max(p, 0) * A.heads + W.h;
@@ -604,8 +609,10 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
       v = A.v_scale[at];
     };
     if (begin < end) {
+      page = page_of(A, W, begin + 16 * quarter, entry_at(A, W, begin + 16 * quarter));
       fetch(begin, page, 0);
       scales(page, ks, vs);
+      entry = entry_at(A, W, begin + kChunk + 16 * quarter);
     }
     uint32_t stage = 0;
     for (int t0 = begin; t0 < end; t0 += kChunk) {
@@ -613,19 +620,20 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
       __builtin_amdgcn_s_waitcnt(0x70);   // vmcnt(0) lgkmcnt(0): this chunk has landed, the last one is read
       __builtin_amdgcn_s_barrier();
       __builtin_amdgcn_sched_barrier(0);
-      int32_t after = -1;
+      int32_t next = -1, after = -1;
       float next_ks = 0.0f, next_vs = 0.0f;
       if (t0 + kChunk < end) {
+        next = page_of(A, W, t0 + kChunk + 16 * quarter, entry);
         fetch(t0 + kChunk, next, stage ^ 1);
         scales(next, next_ks, next_vs);
-        after = page_at(A, W, t0 + 2 * kChunk + 16 * quarter);
+        after = entry_at(A, W, t0 + 2 * kChunk + 16 * quarter);
       }
       if (t0 < wave_end && t0 + kChunk > wave_a.low) {
         const bool cut = t0 + kChunk > wave_a.high || t0 < wave_b.low || __any(page < 0);
         chunk(t0, stage, page, page < 0 ? 0.0f : ks, page < 0 ? 0.0f : vs, cut);
       }
       page = next;
-      next = after;
+      entry = after;
       ks = next_ks;
       vs = next_vs;
       stage ^= 1;
