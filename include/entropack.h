@@ -489,7 +489,7 @@ int ep_gemm_fp8_block(const void* d_x, const float* d_x_scale, const void* d_w, 
 typedef struct {
   void* d_k;               /* [n_pages][kv_heads][page_tokens][head_dim] codes */
   void* d_v;               /* [n_pages][kv_heads][head_dim][page_tokens] codes */
-  float* d_k_scale;        /* [n_pages][kv_heads] */
+  float* d_k_scale;        /* [n_pages][kv_heads], not negative */
   float* d_v_scale;        /* [n_pages][kv_heads] */
   int64_t n_pages;         /* below 2^31 */
   int32_t kv_heads;
@@ -565,7 +565,7 @@ typedef struct {
   int32_t window;          /* > 0 (causal only): and no more than this many of them, itself included */
   int32_t max_q;           /* the most queries of a request and the most tokens of one, as far as */
   int32_t max_len;         /*  the host knows: they size the launch, and may be exceeded */
-  float scale;             /* of the scores, usually 1 / sqrt(head_dim) */
+  float scale;             /* of the scores, usually 1 / sqrt(head_dim); not negative */
   int32_t reserved;
 } ep_kv8_attn;
 
@@ -588,7 +588,8 @@ uint64_t ep_kv8_attention_workspace(const ep_kv8_cache* cache, const ep_kv8_attn
  * equal bits.  total_q may be 0.  Asynchronous on hip_stream, no allocation, at
  * most two launches.
  * Errors: EP_ERR_ARG (null or misaligned pointers, a bad cache or call, rows
- * shorter than q_heads * head_dim or misaligned, a short workspace), EP_ERR_HIP. */
+ * shorter than q_heads * head_dim or misaligned, n_req * kv_heads above 2^22,
+ * total_q * q_heads above 2^29, a short workspace), EP_ERR_HIP. */
 int ep_kv8_attention(const ep_kv8_cache* cache, const ep_kv8_attn* call, void* d_workspace,
                      uint64_t ws_bytes, void* hip_stream);
 

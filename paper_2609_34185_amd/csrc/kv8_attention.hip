@@ -50,7 +50,7 @@ struct Attn {
   float* lse;
   const int32_t *cu, *len, *table;
   float *part_out, *part_lse;        // [splits][total_q][q_heads][D], [splits][total_q][q_heads]
-  int64_t table_ld, total_q, q_row, out_row, n_pages;
+  int64_t table_ld, total_q, q_row, out_row, n_pages, n_req;
   int32_t heads, group, shift, causal, window, splits, split_tokens;
   float scale;
 };
@@ -142,14 +142,13 @@ struct Work {
   uint32_t rows;         // (query, head of the group) pairs
 };
 
-__device__ __forceinline__ Work work_of(const Attn& A, uint32_t pair) {
+__device__ __forceinline__ Work work_of(const Attn& A, int64_t b, int32_t h) {
   Work W;
-  W.h = pair % A.heads;
-  const int64_t b = pair / A.heads;
+  W.h = h;
   W.len = (int32_t)min((int64_t)max(A.len[b], 0), min(A.table_ld << A.shift, (int64_t)0x7FFFFF00));
   W.q0 = min((int64_t)max(A.cu[b], 0), A.total_q);
   W.m = (int32_t)max(min((int64_t)max(A.cu[b + 1], 0), A.total_q) - W.q0, (int64_t)0);
-  W.rows = (uint32_t)W.m * A.group;      // total_q * q_heads is below 2^31
+  W.rows = (uint32_t)W.m * A.group;      // total_q * q_heads is at most 2^29
   W.table = A.table + b * A.table_ld;
   return W;
 }
@@ -222,7 +221,7 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, quarter = lane >> 4;
-  const Work W = work_of(A, blockIdx.x);
+  const Work W = work_of(A, blockIdx.x / A.heads, blockIdx.x % A.heads);
   const int split = blockIdx.y, page_tokens = 1 << A.shift;
   const uint32_t rows = W.rows;
   const int64_t head_codes = (int64_t)page_tokens * D;
@@ -420,6 +419,50 @@ __device__ __forceinline__ uint32_t key_place(uint32_t j, uint32_t r) {
   return j ^ ((r & 3) | ((r >> 4) & 3) << 2);
 }
 
+// Tile `index` of all requests' tiles of `tile_rows` query rows: sets its request and its number
+// there, or returns false if there are fewer.  Every workgroup counts the requests' tiles for
+// itself, 256 requests at a time, so that a launch holds no workgroups for tiles that short
+// requests do not have.  (Workgroups without work, in turn with those that have some, take half of
+// the CUs away from them: a request of 64 tokens next to one of 8192 cost 1485 us instead of 876.)
+__device__ __forceinline__ bool find_tile(const Attn& A, uint32_t index, uint32_t tile_rows, int64_t& request, uint32_t& tile) {
+  constexpr int kThreads = 64 * kPromptWaves;
+  __shared__ uint32_t wave_sum[kPromptWaves], found[2];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t before = 0;     // tiles of the requests before this round's; below 2^31 in all
+  if (threadIdx.x == 0) found[1] = ~0u;
+  for (int64_t b0 = 0; b0 < A.n_req && before <= index; b0 += kThreads) {
+    const int64_t b = b0 + threadIdx.x;
+    uint32_t tiles = 0;
+    if (b < A.n_req) tiles = (work_of(A, b, 0).rows + tile_rows - 1) / tile_rows;
+    uint32_t sum = tiles;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const uint32_t up = __shfl_up(sum, d);
+      if (lane >= d) sum += up;
+    }
+    __syncthreads();       // the last round's sums are read
+    if (lane == 63) wave_sum[wave] = sum;
+    __syncthreads();
+    uint32_t all = 0, first = before + sum - tiles;
+#pragma unroll
+    for (int w = 0; w < kPromptWaves; w++) {
+      if (w < wave) first += wave_sum[w];
+      all += wave_sum[w];
+    }
+    if (index >= first && index < first + tiles) {
+      found[0] = (uint32_t)(b - b0);
+      found[1] = tiles - 1 - (index - first);   // the longest rows of a causal request first
+    }
+    request = b0;
+    before += all;
+  }
+  __syncthreads();
+  if (found[1] == ~0u) return false;
+  request += __builtin_amdgcn_readfirstlane(found[0]);
+  tile = __builtin_amdgcn_readfirstlane(found[1]);
+  return true;
+}
+
 template <int D, bool INT8, bool FP16>
 __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(Attn A) {
   constexpr int kColTiles = col_tiles(D), kPromptRows = prompt_rows(D);
@@ -430,242 +473,239 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quarter = lane >> 4;
-  const Work W = work_of(A, blockIdx.x);
+  int64_t request;
+  uint32_t tile;
+  if (!find_tile(A, blockIdx.x / A.heads, kPromptRows, request, tile)) return;
+  const Work W = work_of(A, request, blockIdx.x % A.heads);
   const int split = blockIdx.y, page_tokens = 1 << A.shift;
   const int64_t head_codes = (int64_t)page_tokens * D, q_heads = (int64_t)A.heads * A.group;
   // the run of 16 tokens that this lane's value loads are of (a KiB of values is 16 channels of
   // four runs, run j of channel d at place j ^ (d / 4 mod 4))
   const uint32_t v_run = (lane & 3) ^ (quarter & 3);
 
-  const uint32_t tiles = (W.rows + kPromptRows - 1) / kPromptRows;
-  for (uint32_t turn = blockIdx.z; turn < tiles; turn += gridDim.z) {
-    const uint32_t tile = tiles - 1 - turn;   // the longest rows of a causal request first
-    const uint32_t tile_first = tile * kPromptRows, wave_first = tile_first + 16 * kColTiles * wave;
-    const Span first = span_of(A, W, tile_first), last = span_of(A, W, min(tile_first + kPromptRows - 1, W.rows - 1));
-    const int share = split * A.split_tokens;
-    const int begin = max(share, first.low & ~(kChunk - 1));
-    const int end = split == A.splits - 1 ? last.high : min(share + A.split_tokens, last.high);
-    // keys [wave_a.low, wave_end) are seen by some row of this wave, [wave_b.low, wave_a.high) by all
-    const Span wave_a = span_of(A, W, min(wave_first, W.rows - 1)),
-               wave_b = span_of(A, W, min(wave_first + 16 * kColTiles - 1, W.rows - 1));
-    const int wave_end = wave_first < W.rows ? wave_b.high : 0;
+  const uint32_t tile_first = tile * kPromptRows, wave_first = tile_first + 16 * kColTiles * wave;
+  const Span first = span_of(A, W, tile_first), last = span_of(A, W, min(tile_first + kPromptRows - 1, W.rows - 1));
+  const int share = split * A.split_tokens;
+  const int begin = max(share, first.low & ~(kChunk - 1));
+  const int end = split == A.splits - 1 ? last.high : min(share + A.split_tokens, last.high);
+  // keys [wave_a.low, wave_end) are seen by some row of this wave, [wave_b.low, wave_a.high) by all
+  const Span wave_a = span_of(A, W, min(wave_first, W.rows - 1)),
+             wave_b = span_of(A, W, min(wave_first + 16 * kColTiles - 1, W.rows - 1));
+  const int wave_end = wave_first < W.rows ? wave_b.high : 0;
 
-    Span span[kColTiles];
-    float row_scale[kColTiles], top[kColTiles], total[kColTiles];
-    v8h q[kColTiles][kPieces][2];
-    v4f o[kTiles][kColTiles];
+  Span span[kColTiles];
+  float row_scale[kColTiles], top[kColTiles], total[kColTiles];
+  v8h q[kColTiles][kPieces][2];
+  v4f o[kTiles][kColTiles];
 #pragma unroll
-    for (int n = 0; n < kColTiles; n++) {
-      const uint32_t row = min(wave_first + 16 * n + col, W.rows - 1);
-      span[n] = span_of(A, W, row);
-      row_scale[n] = load_query<D, FP16>(A, W, row, quarter, q[n]);
-      top[n] = minus_inf();
-      total[n] = 0.0f;
+  for (int n = 0; n < kColTiles; n++) {
+    const uint32_t row = min(wave_first + 16 * n + col, W.rows - 1);
+    span[n] = span_of(A, W, row);
+    row_scale[n] = load_query<D, FP16>(A, W, row, quarter, q[n]);
+    top[n] = minus_inf();
+    total[n] = 0.0f;
 #pragma unroll
-      for (int t = 0; t < kTiles; t++) o[t][n] = v4f{};
+    for (int t = 0; t < kTiles; t++) o[t][n] = v4f{};
+  }
+  float ref = 0.0f, per_ref = 1.0f;   // and 1 / ref
+
+  // Direct loads of chunk t0, whose run `quarter` lies in `page`: this wave takes every fourth KiB
+  // of the keys and of the values.  Runs with nothing to fetch take page 0, whose scores are
+  // masked and whose codes are cleaned.
+  auto fetch = [&](int t0, int32_t page, uint32_t stage) {
+    lds_u8* const dst = (lds_u8*)lds_mem[stage] + 1024 * wave;
+    const int32_t in = max(page, 0);
+#pragma unroll
+    for (int i = 0; i < kLoads; i++) {
+      const uint32_t at = 1024 * (kPromptWaves * i + wave), run = at / (16 * D);   // the same in all lanes
+      const int64_t p = __builtin_amdgcn_readlane(in, 16 * run);
+      const uint8_t* const src = A.k + (p * A.heads + W.h) * head_codes + ((t0 + 16 * run) & (page_tokens - 1)) * D;
+      const uint32_t r = (at + 16 * lane) / D, off = r % 16 * D + 16 * key_place<D>((at + 16 * lane) % D / 16, r);
+      __builtin_amdgcn_global_load_lds((global_u8*)(src + off), dst + 1024 * kPromptWaves * i, 16, 0, 0);
     }
-    float ref = 0.0f, per_ref = 1.0f;   // and 1 / ref
+    const int32_t p0 = __builtin_amdgcn_readlane(in, 0), p1 = __builtin_amdgcn_readlane(in, 16),
+                  p2 = __builtin_amdgcn_readlane(in, 32), p3 = __builtin_amdgcn_readlane(in, 48);
+    const int32_t pv = v_run & 2 ? (v_run & 1 ? p3 : p2) : (v_run & 1 ? p1 : p0);
+    const uint8_t* const src = A.v + ((int64_t)pv * A.heads + W.h) * head_codes + ((t0 + 16 * v_run) & (page_tokens - 1)) +
+                               (16 * wave + (lane >> 2)) * page_tokens;
+#pragma unroll
+    for (int i = 0; i < kLoads; i++)
+      __builtin_amdgcn_global_load_lds((global_u8*)(src + 16 * kPromptWaves * i * page_tokens),
+                                       dst + kBytes + 1024 * kPromptWaves * i, 16, 0, 0);
+  };
 
-    // Direct loads of chunk t0, whose run `quarter` lies in `page`: this wave takes every fourth KiB
-    // of the keys and of the values.  Runs with nothing to fetch take page 0, whose scores are
-    // masked and whose codes are cleaned.
-    auto fetch = [&](int t0, int32_t page, uint32_t stage) {
-      lds_u8* const dst = (lds_u8*)lds_mem[stage] + 1024 * wave;
-      const int32_t in = max(page, 0);
+  // One chunk.  cut: some row of the wave does not see all of it.
+  auto chunk = [&](int t0, uint32_t stage, int32_t page, float ks, float vs, bool cut) {
+    const lds_u8* const keys = (const lds_u8*)lds_mem[stage];
+    const lds_u8* const values = keys + kBytes;
+    v4f s[4][kColTiles];
 #pragma unroll
-      for (int i = 0; i < kLoads; i++) {
-        const uint32_t at = 1024 * (kPromptWaves * i + wave), run = at / (16 * D);   // the same in all lanes
-        const int64_t p = __builtin_amdgcn_readlane(in, 16 * run);
-        const uint8_t* const src = A.k + (p * A.heads + W.h) * head_codes + ((t0 + 16 * run) & (page_tokens - 1)) * D;
-        const uint32_t r = (at + 16 * lane) / D, off = r % 16 * D + 16 * key_place<D>((at + 16 * lane) % D / 16, r);
-        __builtin_amdgcn_global_load_lds((global_u8*)(src + off), dst + 1024 * kPromptWaves * i, 16, 0, 0);
-      }
-      const int32_t p0 = __builtin_amdgcn_readlane(in, 0), p1 = __builtin_amdgcn_readlane(in, 16),
-                    p2 = __builtin_amdgcn_readlane(in, 32), p3 = __builtin_amdgcn_readlane(in, 48);
-      const int32_t pv = v_run & 2 ? (v_run & 1 ? p3 : p2) : (v_run & 1 ? p1 : p0);
-      const uint8_t* const src = A.v + ((int64_t)pv * A.heads + W.h) * head_codes + ((t0 + 16 * v_run) & (page_tokens - 1)) +
-                                 (16 * wave + (lane >> 2)) * page_tokens;
+    for (int t = 0; t < 4; t++) {
 #pragma unroll
-      for (int i = 0; i < kLoads; i++)
-        __builtin_amdgcn_global_load_lds((global_u8*)(src + 16 * kPromptWaves * i * page_tokens),
-                                         dst + kBytes + 1024 * kPromptWaves * i, 16, 0, 0);
-    };
-
-    // One chunk.  cut: some row of the wave does not see all of it.
-    auto chunk = [&](int t0, uint32_t stage, int32_t page, float ks, float vs, bool cut) {
-      const lds_u8* const keys = (const lds_u8*)lds_mem[stage];
-      const lds_u8* const values = keys + kBytes;
-      v4f s[4][kColTiles];
+      for (int n = 0; n < kColTiles; n++) s[t][n] = v4f{};
+      const uint32_t r = 16 * (col >> 2) + 4 * t + (col & 3);
 #pragma unroll
-      for (int t = 0; t < 4; t++) {
-#pragma unroll
-        for (int n = 0; n < kColTiles; n++) s[t][n] = v4f{};
-        const uint32_t r = 16 * (col >> 2) + 4 * t + (col & 3);
-#pragma unroll
-        for (int p = 0; p < kPieces; p++) {
-          const v4u c = *reinterpret_cast<const __attribute__((address_space(3))) v4u*>(
-              keys + r * D + 16 * key_place<D>(4 * p + quarter, r));
-          const v8h a = widen8<INT8>(c[0], c[1]), b = widen8<INT8>(c[2], c[3]);
-#pragma unroll
-          for (int n = 0; n < kColTiles; n++) {
-            s[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, q[n][p][0], s[t][n], 0, 0, 0);
-            s[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, q[n][p][1], s[t][n], 0, 0, 0);
-          }
-        }
-      }
-      float f[kColTiles];
-#pragma unroll
-      for (int n = 0; n < kColTiles; n++) f[n] = ks * row_scale[n];
-      if (cut) {
-        // scores as they are, -infinity where unseen; a value scale that is not finite makes the
-        // rows that see its page not-a-number, and no others
-        const int tv = t0 + 16 * quarter;
-        const bool bad = !(fabsf(vs) < __builtin_inff());
-#pragma unroll
-        for (int n = 0; n < kColTiles; n++) {
-          const int low = page >= 0 ? span[n].low - tv : 16, high = span[n].high - tv;
-#pragma unroll
-          for (int e = 0; e < 16; e++) {
-            const float x = bad ? __builtin_nanf("") : s[e >> 2][n][e & 3] * f[n];
-            s[e >> 2][n][e & 3] = e >= low && e < high ? x : minus_inf();
-          }
-          f[n] = 1.0f;
-        }
-        if (bad) vs = 0.0f;
-      }
-      // ref to the power of two above the largest finite scale, if that is larger
-      const float most = swap_max4(vs < __builtin_inff() ? vs : 0.0f);
-      if (__any(most > ref)) {
-        const uint32_t ex = min((__float_as_uint(most) >> 23) + 1, 253u);
-        per_ref = __uint_as_float((254 - ex) << 23);
-        const float keep = ref * per_ref;
-        ref = __uint_as_float(ex << 23);
-#pragma unroll
-        for (int t = 0; t < kTiles; t++)
-#pragma unroll
-          for (int n = 0; n < kColTiles; n++) o[t][n] *= keep;
-      }
-      // the page's share of ref goes into the exponent, and out of the sum of weights again; what is
-      // below 2^-100 (zero among it) is nothing in FP16 either way
-      float part = vs * per_ref;
-      part = part < 0x1p-100f ? 0x1p-100f : part;
-      const float lift = kLift + __builtin_amdgcn_logf(part), back = __builtin_amdgcn_rcpf(part);
-      v8h w[2][kColTiles];
-#pragma unroll
-      for (int n = 0; n < kColTiles; n++) {
-        float mx = max3(s[0][n][0], s[0][n][1], s[0][n][2]);
-        mx = max3(mx, s[0][n][3], s[1][n][0]);
-        mx = max3(mx, s[1][n][1], s[1][n][2]);
-        mx = max3(mx, s[1][n][3], s[2][n][0]);
-        mx = max3(mx, s[2][n][1], s[2][n][2]);
-        mx = max3(mx, s[2][n][3], s[3][n][0]);
-        mx = max3(mx, s[3][n][1], s[3][n][2]);
-        mx = swap_max4(max3(mx, s[3][n][3], s[3][n][3]) * f[n]);
-        if (__any(mx > top[n] + kSlack)) {
-          const float now = mx > top[n] + kSlack ? mx : top[n];
-          const float keep = exp2_from(top[n], now);
-          total[n] *= keep;
-#pragma unroll
-          for (int t = 0; t < kTiles; t++) o[t][n] *= keep;
-          top[n] = now;
-        }
-        const float base = lift - (top[n] == minus_inf() ? 0.0f : top[n]);
-        float sum = 0.0f;
-#pragma unroll
-        for (int t = 0; t < 4; t++)
-#pragma unroll
-          for (int r = 0; r < 4; r++) {
-            const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][n][r], f[n], base));
-            sum += e;
-            w[t >> 1][n][4 * (t & 1) + r] = (_Float16)e;
-          }
-        total[n] = __builtin_fmaf(sum, back, total[n]);
-      }
-#pragma unroll
-      for (int t = 0; t < kTiles; t++) {
-        const uint32_t d = 16 * t + col;
-        v4u c = *reinterpret_cast<const __attribute__((address_space(3))) v4u*>(
-            values + d * kChunk + 16 * (quarter ^ ((d >> 2) & 3)));
-        if (cut && !INT8) {
-#pragma unroll
-          for (int i = 0; i < 4; i++) c[i] = without_nans(c[i]);
-        }
+      for (int p = 0; p < kPieces; p++) {
+        const v4u c = *reinterpret_cast<const __attribute__((address_space(3))) v4u*>(
+            keys + r * D + 16 * key_place<D>(4 * p + quarter, r));
         const v8h a = widen8<INT8>(c[0], c[1]), b = widen8<INT8>(c[2], c[3]);
 #pragma unroll
         for (int n = 0; n < kColTiles; n++) {
-          o[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, w[0][n], o[t][n], 0, 0, 0);
-          o[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, w[1][n], o[t][n], 0, 0, 0);
+          s[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, q[n][p][0], s[t][n], 0, 0, 0);
+          s[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, q[n][p][1], s[t][n], 0, 0, 0);
         }
       }
-    };
-
-    // page and scales of the lane's run of 16 tokens, and the table's entry of the next chunk's:
-    // loaded a chunk before they are used, as the codes are
-    int32_t page = -1, entry = -1;
-    float ks = 0.0f, vs = 0.0f;
-    auto scales = [&](int32_t p, float& k, float& v) {
-      const int64_t at = (int64_t)max(p, 0) * A.heads + W.h;
-      k = A.k_scale[at];
-      v = A.v_scale[at];
-    };
-    if (begin < end) {
-      page = page_of(A, W, begin + 16 * quarter, entry_at(A, W, begin + 16 * quarter));
-      fetch(begin, page, 0);
-      scales(page, ks, vs);
-      entry = entry_at(A, W, begin + kChunk + 16 * quarter);
     }
-    uint32_t stage = 0;
-    for (int t0 = begin; t0 < end; t0 += kChunk) {
-      __builtin_amdgcn_sched_barrier(0);
-      __builtin_amdgcn_s_waitcnt(0x70);   // vmcnt(0) lgkmcnt(0): this chunk has landed, the last one is read
-      __builtin_amdgcn_s_barrier();
-      __builtin_amdgcn_sched_barrier(0);
-      int32_t next = -1, after = -1;
-      float next_ks = 0.0f, next_vs = 0.0f;
-      if (t0 + kChunk < end) {
-        next = page_of(A, W, t0 + kChunk + 16 * quarter, entry);
-        fetch(t0 + kChunk, next, stage ^ 1);
-        scales(next, next_ks, next_vs);
-        after = entry_at(A, W, t0 + 2 * kChunk + 16 * quarter);
+    float f[kColTiles];
+#pragma unroll
+    for (int n = 0; n < kColTiles; n++) f[n] = ks * row_scale[n];
+    if (cut) {
+      // scores as they are, -infinity where unseen; a value scale that is not finite makes the
+      // rows that see its page not-a-number, and no others
+      const int tv = t0 + 16 * quarter;
+      const bool bad = !(fabsf(vs) < __builtin_inff());
+#pragma unroll
+      for (int n = 0; n < kColTiles; n++) {
+        const int low = page >= 0 ? span[n].low - tv : 16, high = span[n].high - tv;
+#pragma unroll
+        for (int e = 0; e < 16; e++) {
+          const float x = bad ? __builtin_nanf("") : s[e >> 2][n][e & 3] * f[n];
+          s[e >> 2][n][e & 3] = e >= low && e < high ? x : minus_inf();
+        }
+        f[n] = 1.0f;
       }
-      if (t0 < wave_end && t0 + kChunk > wave_a.low) {
-        const bool cut = t0 + kChunk > wave_a.high || t0 < wave_b.low || __any(page < 0);
-        chunk(t0, stage, page, page < 0 ? 0.0f : ks, page < 0 ? 0.0f : vs, cut);
-      }
-      page = next;
-      entry = after;
-      ks = next_ks;
-      vs = next_vs;
-      stage ^= 1;
+      if (bad) vs = 0.0f;
     }
-    __syncthreads();   // before the next tile's loads
-
+    // ref to the power of two above the largest finite scale, if that is larger
+    const float most = swap_max4(vs < __builtin_inff() ? vs : 0.0f);
+    if (__any(most > ref)) {
+      const uint32_t ex = min((__float_as_uint(most) >> 23) + 1, 253u);
+      per_ref = __uint_as_float((254 - ex) << 23);
+      const float keep = ref * per_ref;
+      ref = __uint_as_float(ex << 23);
+#pragma unroll
+      for (int t = 0; t < kTiles; t++)
+#pragma unroll
+        for (int n = 0; n < kColTiles; n++) o[t][n] *= keep;
+    }
+    // the page's share of ref goes into the exponent, and out of the sum of weights again; what is
+    // below 2^-100 (zero among it) is nothing in FP16 either way
+    float part = vs * per_ref;
+    part = part < 0x1p-100f ? 0x1p-100f : part;
+    const float lift = kLift + __builtin_amdgcn_logf(part), back = __builtin_amdgcn_rcpf(part);
+    v8h w[2][kColTiles];
 #pragma unroll
     for (int n = 0; n < kColTiles; n++) {
-      const uint32_t row = wave_first + 16 * n + col;
-      const float l = sum4(total[n]);
-      if (row >= W.rows) continue;
-      const float inv = l == 0.0f ? 0.0f : ref / l;
-      const float lse2 = l == 0.0f ? minus_inf() : top[n] - kLift + __builtin_amdgcn_logf(l);
-      const int64_t token = W.q0 + row / (uint32_t)A.group, head = W.h * A.group + row % (uint32_t)A.group;
-      if (A.splits > 1) {
-        const int64_t at = ((int64_t)split * A.total_q + token) * q_heads + head;
+      float mx = max3(s[0][n][0], s[0][n][1], s[0][n][2]);
+      mx = max3(mx, s[0][n][3], s[1][n][0]);
+      mx = max3(mx, s[1][n][1], s[1][n][2]);
+      mx = max3(mx, s[1][n][3], s[2][n][0]);
+      mx = max3(mx, s[2][n][1], s[2][n][2]);
+      mx = max3(mx, s[2][n][3], s[3][n][0]);
+      mx = max3(mx, s[3][n][1], s[3][n][2]);
+      mx = swap_max4(max3(mx, s[3][n][3], s[3][n][3]) * f[n]);
+      if (__any(mx > top[n] + kSlack)) {
+        const float now = mx > top[n] + kSlack ? mx : top[n];
+        const float keep = exp2_from(top[n], now);
+        total[n] *= keep;
 #pragma unroll
-        for (int t = 0; t < kTiles; t++)
-          *reinterpret_cast<v4f*>(A.part_out + at * D + 16 * t + 4 * quarter) = o[t][n] * inv;
-        if (quarter == 0) A.part_lse[at] = lse2;
-      } else {
-        uint16_t* const dst = A.out + token * A.out_row + head * D + 4 * quarter;
-#pragma unroll
-        for (int t = 0; t < kTiles; t++) {
-          typedef uint16_t v4s __attribute__((ext_vector_type(4)));
-          v4s x;
-#pragma unroll
-          for (int r = 0; r < 4; r++) x[r] = narrow<FP16>(o[t][n][r] * inv);
-          *reinterpret_cast<v4s*>(dst + 16 * t) = x;
-        }
-        if (quarter == 0 && A.lse) A.lse[token * q_heads + head] = lse2 * kLn2;
+        for (int t = 0; t < kTiles; t++) o[t][n] *= keep;
+        top[n] = now;
       }
+      const float base = lift - (top[n] == minus_inf() ? 0.0f : top[n]);
+      float sum = 0.0f;
+#pragma unroll
+      for (int t = 0; t < 4; t++)
+#pragma unroll
+        for (int r = 0; r < 4; r++) {
+          const float e = __builtin_amdgcn_exp2f(__builtin_fmaf(s[t][n][r], f[n], base));
+          sum += e;
+          w[t >> 1][n][4 * (t & 1) + r] = (_Float16)e;
+        }
+      total[n] = __builtin_fmaf(sum, back, total[n]);
+    }
+#pragma unroll
+    for (int t = 0; t < kTiles; t++) {
+      const uint32_t d = 16 * t + col;
+      v4u c = *reinterpret_cast<const __attribute__((address_space(3))) v4u*>(
+          values + d * kChunk + 16 * (quarter ^ ((d >> 2) & 3)));
+      if (cut && !INT8) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) c[i] = without_nans(c[i]);
+      }
+      const v8h a = widen8<INT8>(c[0], c[1]), b = widen8<INT8>(c[2], c[3]);
+#pragma unroll
+      for (int n = 0; n < kColTiles; n++) {
+        o[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, w[0][n], o[t][n], 0, 0, 0);
+        o[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(b, w[1][n], o[t][n], 0, 0, 0);
+      }
+    }
+  };
+
+  // page and scales of the lane's run of 16 tokens, and the table's entry of the next chunk's:
+  // loaded a chunk before they are used, as the codes are
+  int32_t page = -1, entry = -1;
+  float ks = 0.0f, vs = 0.0f;
+  auto scales = [&](int32_t p, float& k, float& v) {
+    const int64_t at = (int64_t)max(p, 0) * A.heads + W.h;
+    k = A.k_scale[at];
+    v = A.v_scale[at];
+  };
+  if (begin < end) {
+    page = page_of(A, W, begin + 16 * quarter, entry_at(A, W, begin + 16 * quarter));
+    fetch(begin, page, 0);
+    scales(page, ks, vs);
+    entry = entry_at(A, W, begin + kChunk + 16 * quarter);
+  }
+  uint32_t stage = 0;
+  for (int t0 = begin; t0 < end; t0 += kChunk) {
+    __builtin_amdgcn_sched_barrier(0);
+    __builtin_amdgcn_s_waitcnt(0x70);   // vmcnt(0) lgkmcnt(0): this chunk has landed, the last one is read
+    __builtin_amdgcn_s_barrier();
+    __builtin_amdgcn_sched_barrier(0);
+    int32_t next = -1, after = -1;
+    float next_ks = 0.0f, next_vs = 0.0f;
+    if (t0 + kChunk < end) {
+      next = page_of(A, W, t0 + kChunk + 16 * quarter, entry);
+      fetch(t0 + kChunk, next, stage ^ 1);
+      scales(next, next_ks, next_vs);
+      after = entry_at(A, W, t0 + 2 * kChunk + 16 * quarter);
+    }
+    if (t0 < wave_end && t0 + kChunk > wave_a.low) {
+      const bool cut = t0 + kChunk > wave_a.high || t0 < wave_b.low || __any(page < 0);
+      chunk(t0, stage, page, page < 0 ? 0.0f : ks, page < 0 ? 0.0f : vs, cut);
+    }
+    page = next;
+    entry = after;
+    ks = next_ks;
+    vs = next_vs;
+    stage ^= 1;
+  }
+#pragma unroll
+  for (int n = 0; n < kColTiles; n++) {
+    const uint32_t row = wave_first + 16 * n + col;
+    const float l = sum4(total[n]);
+    if (row >= W.rows) continue;
+    const float inv = l == 0.0f ? 0.0f : ref / l;
+    const float lse2 = l == 0.0f ? minus_inf() : top[n] - kLift + __builtin_amdgcn_logf(l);
+    const int64_t token = W.q0 + row / (uint32_t)A.group, head = W.h * A.group + row % (uint32_t)A.group;
+    if (A.splits > 1) {
+      const int64_t at = ((int64_t)split * A.total_q + token) * q_heads + head;
+#pragma unroll
+      for (int t = 0; t < kTiles; t++)
+        *reinterpret_cast<v4f*>(A.part_out + at * D + 16 * t + 4 * quarter) = o[t][n] * inv;
+      if (quarter == 0) A.part_lse[at] = lse2;
+    } else {
+      uint16_t* const dst = A.out + token * A.out_row + head * D + 4 * quarter;
+#pragma unroll
+      for (int t = 0; t < kTiles; t++) {
+        typedef uint16_t v4s __attribute__((ext_vector_type(4)));
+        v4s x;
+#pragma unroll
+        for (int r = 0; r < 4; r++) x[r] = narrow<FP16>(o[t][n][r] * inv);
+        *reinterpret_cast<v4s*>(dst + 16 * t) = x;
+      }
+      if (quarter == 0 && A.lse) A.lse[token * q_heads + head] = lse2 * kLn2;
     }
   }
 }
@@ -701,10 +741,11 @@ const char* call_fault(const ep_kv8_cache* c, const ep_kv8_attn* a) {
   if (!a) return "null call";
   if (a->q_heads <= 0 || a->q_heads > 1 << 20 || a->q_heads % c->kv_heads) return "q_heads must be a multiple of kv_heads";
   if (a->dtype != EP_BF16 && a->dtype != EP_FP16) return "queries must be BF16 or FP16";
-  if (a->n_req <= 0 || a->n_req > 0xFFFFFF / c->kv_heads) return "n_req * kv_heads outside 1 .. 2^24 - 1";
+  // a grid holds less than 2^32 threads: one workgroup for each (request, head) and each full tile
+  if (a->n_req <= 0 || a->n_req > (1 << 22) / c->kv_heads) return "n_req * kv_heads outside 1 .. 2^22";
   if (a->table_ld <= 0 || a->table_ld > 0x7FFFFFFF) return "table_ld outside 1 .. 2^31 - 1";
   if (a->total_q < 0 || a->total_q > 0x7FFFFFFF) return "total_q outside 0 .. 2^31 - 1";
-  if (a->total_q * a->q_heads > 0x7FFFFFFF) return "total_q * q_heads above 2^31 - 1";
+  if (a->total_q * a->q_heads > 1 << 29) return "total_q * q_heads above 2^29";
   if (a->window < 0 || (a->window && !a->causal)) return "a window needs causal, and must not be negative";
   if (!(a->scale >= 0.0f && a->scale < __builtin_inff())) return "scale must be finite and not negative";
   if (a->max_q <= 0 || a->max_len < 0) return "max_q must be positive and max_len not negative";
@@ -719,7 +760,8 @@ const char* call_fault(const ep_kv8_cache* c, const ep_kv8_attn* a) {
 
 // How a call's keys are shared out.  Workgroups are (request and head, split, row tile).
 struct Plan {
-  int64_t tiles, splits, split_tokens, max_q;
+  int64_t tiles;         // of a request in the one kernel, of all requests at most in the other
+  int64_t splits, split_tokens, max_q;
   bool prompt;
 };
 
@@ -728,9 +770,10 @@ Plan plan_of(const ep_kv8_cache& c, const ep_kv8_attn& a) {
   const int64_t rows = a.max_q * (int64_t)(a.q_heads / c.kv_heads);
   P.max_q = a.max_q;
   P.prompt = rows > 32;
-  const int64_t tile = P.prompt ? prompt_rows(c.head_dim) : kRows, want = P.prompt ? 1024 : 4096, least = P.prompt ? 512 : 256;
-  P.tiles = std::min<int64_t>((rows + tile - 1) / tile, 65535);
-  const int64_t base = P.tiles * a.n_req * c.kv_heads;
+  const int64_t want = P.prompt ? 1024 : 4096, least = P.prompt ? 512 : 256;
+  if (P.prompt) P.tiles = a.total_q * (a.q_heads / c.kv_heads) / prompt_rows(c.head_dim) + a.n_req;
+  else P.tiles = (rows + kRows - 1) / kRows;
+  const int64_t base = P.tiles * c.kv_heads * (P.prompt ? 1 : a.n_req);
   const int64_t max_len = std::min(std::max(a.max_len, 1), 1 << 30);   // the last split takes what is past it
   const int64_t most = (max_len + least - 1) / least;
   P.splits = std::min<int64_t>({std::max<int64_t>(1, want / base), most, 256});
@@ -746,11 +789,13 @@ uint64_t plan_bytes(const Plan& P, const ep_kv8_cache& c, const ep_kv8_attn& a) 
 
 template <int D, bool INT8, bool FP16>
 void attention_launch(const Attn& A, const Plan& P, int64_t n_req, hipStream_t stream) {
-  const dim3 grid((uint32_t)(n_req * A.heads), (uint32_t)P.splits, (uint32_t)P.tiles);
   if (P.prompt)
-    hipLaunchKernelGGL((attention_prompt_kernel<D, INT8, FP16>), grid, dim3(64 * kPromptWaves), 0, stream, A);
+    hipLaunchKernelGGL((attention_prompt_kernel<D, INT8, FP16>), dim3((uint32_t)(P.tiles * A.heads), (uint32_t)P.splits),
+                       dim3(64 * kPromptWaves), 0, stream, A);
   else
-    hipLaunchKernelGGL((attention_rows_kernel<D, INT8, FP16>), grid, dim3(64 * kWaves), 0, stream, A);
+    hipLaunchKernelGGL((attention_rows_kernel<D, INT8, FP16>),
+                       dim3((uint32_t)(n_req * A.heads), (uint32_t)P.splits, (uint32_t)P.tiles), dim3(64 * kWaves), 0,
+                       stream, A);
   if (P.splits > 1) {
     const int64_t rows = P.max_q * A.heads * A.group, per = 256 / (D / 4);
     hipLaunchKernelGGL((attention_join_kernel<D, FP16>),
@@ -803,6 +848,7 @@ extern "C" int ep_kv8_attention(const ep_kv8_cache* cache, const ep_kv8_attn* ca
   A.q_row = call->q_row ? call->q_row : width;
   A.out_row = call->out_row ? call->out_row : width;
   A.n_pages = cache->n_pages;
+  A.n_req = call->n_req;
   A.heads = cache->kv_heads;
   A.group = call->q_heads / cache->kv_heads;
   A.shift = ep::page_shift(cache->page_tokens);
