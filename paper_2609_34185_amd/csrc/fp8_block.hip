@@ -8,6 +8,7 @@
 
 #include "../../include/entropack.h"
 #include "common.h"
+#include "scaled.h"
 #include "tile_order.h"
 
 namespace ep {
@@ -26,9 +27,6 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 constexpr float kE4m3Max = 448.0f;
 
 // ---- element types -------------------------------------------------------------
-struct Bf16 { uint16_t bits; };
-struct Fp16 { _Float16 h; };
-
 // Eight consecutive elements as floats.
 __device__ __forceinline__ void load8(const Bf16* p, float (&v)[8]) {
   const v4u w = *reinterpret_cast<const v4u*>(p);
@@ -68,32 +66,13 @@ __device__ __forceinline__ float scale_of(uint32_t top) {
   return s == 0.0f ? 1.0f : s;
 }
 
-// E4M3(x / s) of eight values.  x / s rounded to FP32 is formed from the correctly rounded
-// r = 1 / s as q0 = x r, q = q0 + r (x - q0 s): one correction of a quotient that is within
-// one unit gives the correctly rounded one (Markstein), as long as neither r nor the residual
-// leaves the normal range.  Outside it the quotient is divided out, and clamped since a
-// subnormal scale may be off by half.  A NaN stays one.
-__device__ __forceinline__ v2u codes8(const float (&v)[8], float s) {
-  float q[8];
-  if (s >= 0x1p-60f && s < 0x1p126f) {
-    const float r = 1.0f / s;
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      const float q0 = v[i] * r;
-      q[i] = __builtin_fmaf(__builtin_fmaf(-q0, s, v[i]), r, q0);
-    }
-  } else {
-#pragma unroll
-    for (int i = 0; i < 8; i++) {
-      const float d = v[i] / s;
-      q[i] = d > kE4m3Max ? kE4m3Max : d < -kE4m3Max ? -kE4m3Max : d;
-    }
-  }
+// E4M3(x / s) of eight values.
+__device__ __forceinline__ v2u codes8(const float (&v)[8], const Divider& by) {
   v2u out;
 #pragma unroll
   for (int i = 0; i < 2; i++) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i], q[4 * i + 1], 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(q[4 * i + 2], q[4 * i + 3], w, true);
+    int w = __builtin_amdgcn_cvt_pk_fp8_f32(by(v[4 * i]), by(v[4 * i + 1]), 0, false);
+    w = __builtin_amdgcn_cvt_pk_fp8_f32(by(v[4 * i + 2]), by(v[4 * i + 3]), w, true);
     out[i] = (uint32_t)w;
   }
   return out;
@@ -118,7 +97,7 @@ __global__ __launch_bounds__(kQuantThreads) void quant_rows_kernel(const T* __re
 #pragma unroll
   for (int d = 1; d < kLanes; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
   const float s = scale_of(top);
-  if (col < k) *reinterpret_cast<v2u*>(q + row * k + col) = codes8(v, s);
+  if (col < k) *reinterpret_cast<v2u*>(q + row * k + col) = codes8(v, Divider(s, kE4m3Max));
   if (threadIdx.x % kLanes == 0) scale[unit] = s;
 }
 
@@ -147,10 +126,11 @@ __global__ __launch_bounds__(kQuantThreads) void quant_blocks_kernel(const T* __
 #pragma unroll
   for (int w = 0; w < kQuantThreads / 64; w++) top = max(top, wave_top[w]);
   const float s = scale_of(top);
+  const Divider by(s, kE4m3Max);
 #pragma unroll
   for (int p = 0; p < kPasses; p++)
     if (col < k && r0 + kRows * p < m)
-      *reinterpret_cast<v2u*>(q + (r0 + kRows * p) * k + col) = codes8(v[p], s);
+      *reinterpret_cast<v2u*>(q + (r0 + kRows * p) * k + col) = codes8(v[p], by);
   if (threadIdx.x == 0) scale[blockIdx.x] = s;
 }
 

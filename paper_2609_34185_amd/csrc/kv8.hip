@@ -9,6 +9,7 @@
 #include "../../include/entropack.h"
 #include "common.h"
 #include "kv8.h"
+#include "scaled.h"
 
 namespace ep {
 namespace {
@@ -148,12 +149,6 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(Slots S) {
 }
 
 // ---- append --------------------------------------------------------------------------
-struct Bf16 { uint16_t bits; };
-struct Fp16 { _Float16 h; };
-__device__ __forceinline__ float as_float(Bf16 x) { return __uint_as_float((uint32_t)x.bits << 16); }
-__device__ __forceinline__ float as_float(Fp16 x) { return (float)x.h; }
-__device__ __forceinline__ float as_float(float x) { return x; }
-
 struct Append {
   uint8_t *k, *v;
   float *k_scale, *v_scale;
@@ -163,76 +158,346 @@ struct Append {
   int heads, shift;
 };
 
-// Nearest code of x / s (0 where s is 0).
+// Codes of two values in the low bytes.  Rounding to nearest even; INT8's NaN becomes 0, and shows
+// in the scale.
 template <bool INT8>
-__device__ __forceinline__ uint8_t code_of(float x, float s) {
-  const float top = INT8 ? 127.0f : 448.0f;
-  float q = s == 0.0f ? 0.0f : x / s;
-  q = q > top ? top : q < -top ? -top : q;   // a NaN stays one
-  if (INT8) return (uint8_t)(int8_t)(int)rintf(q);
-  return (uint8_t)(__builtin_amdgcn_cvt_pk_fp8_f32(q, q, 0, false) & 0xFF);
+__device__ __forceinline__ uint32_t codes2(float a, float b) {
+  if (INT8) return ((uint32_t)(int)rintf(a) & 0xFFu) | ((uint32_t)(int)rintf(b) & 0xFFu) << 8;
+  return (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(a, b, 0, false) & 0xFFFFu;
 }
 
+// The values of the four codes of a word, carried over from one scale to another.
 template <bool INT8>
-__device__ __forceinline__ float value_of(uint8_t c) {
-  if (INT8) return (float)(int8_t)c;
-  return __builtin_amdgcn_cvt_f32_fp8(c, 0);
+__device__ __forceinline__ uint32_t rescaled4(uint32_t c, float before, const Divider& by) {
+  float x[4];
+  if (INT8) {
+#pragma unroll
+    for (int i = 0; i < 4; i++) x[i] = (float)(int8_t)(c >> (8 * i));
+  } else {
+    x[0] = __builtin_amdgcn_cvt_f32_fp8((int)c, 0);
+    x[1] = __builtin_amdgcn_cvt_f32_fp8((int)c, 1);
+    x[2] = __builtin_amdgcn_cvt_f32_fp8((int)c, 2);
+    x[3] = __builtin_amdgcn_cvt_f32_fp8((int)c, 3);
+  }
+#pragma unroll
+  for (int i = 0; i < 4; i++) x[i] = by(x[i] * before);
+  return codes2<INT8>(x[0], x[1]) | codes2<INT8>(x[2], x[3]) << 16;
 }
 
-// One workgroup for each token, head and array (keys, values); those whose token is not the
-// first of its page's tokens have nothing to do.
-constexpr int kAppendThreads = 256;
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
+// Element e of a lane's channels of one token, from the words that hold them.
+__device__ __forceinline__ float element(const Bf16*, const uint32_t* w, int e) {
+  return __uint_as_float(e & 1 ? w[e >> 1] & 0xFFFF0000u : w[e >> 1] << 16);
+}
+__device__ __forceinline__ float element(const Fp16*, const uint32_t* w, int e) {
+  return (float)__builtin_bit_cast(_Float16, (uint16_t)(e & 1 ? w[e >> 1] >> 16 : w[e >> 1]));
+}
+__device__ __forceinline__ float element(const float*, const uint32_t* w, int e) { return __uint_as_float(w[e]); }
+
+// W words (2, 4, 8 or 16) from an address aligned to as many bytes as a load takes.
+template <int W>
+__device__ __forceinline__ void load_words(const void* p, uint32_t* w) {
+  if (W == 2) {
+    const uint2 x = *static_cast<const uint2*>(p);
+    w[0] = x.x;
+    w[1] = x.y;
+  } else {
+#pragma unroll
+    for (int i = 0; i < W / 4; i++) {
+      const v4u x = static_cast<const v4u*>(p)[i];
+#pragma unroll
+      for (int j = 0; j < 4; j++) w[4 * i + j] = x[j];
+    }
+  }
+}
+
+// A run of tokens that take consecutive places of one page, for one head, keys or values.
+struct Run {
+  uint8_t* codes;
+  float* scale;
+  const void* x;       // the head's channels of the run's first token
+  int64_t row;         // elements from one token to the next
+  int at, count;       // first place, tokens
+  bool values;
+};
+
+template <typename T, int D>
+__device__ __forceinline__ Run run_of(const Append& A, int64_t t0, int64_t slot, int count, int item) {
+  const int head = item >> 1, tokens = 1 << A.shift;
+  Run R;
+  R.values = item & 1;
+  R.row = R.values ? A.v_row : A.k_row;
+  R.x = static_cast<const T*>(R.values ? A.new_v : A.new_k) + t0 * R.row + head * D;
+  const int64_t block = (slot >> A.shift) * A.heads + head;
+  R.codes = (R.values ? A.v : A.k) + block * ((int64_t)tokens * D);
+  R.scale = (R.values ? A.v_scale : A.k_scale) + block;
+  R.at = (int)(slot & (tokens - 1));
+  R.count = count;
+  return R;
+}
+
+// The page's scale with the new tokens' largest magnitude among it; a NaN of either side stays.
+template <bool INT8>
+__device__ __forceinline__ float grown(float before, uint32_t top) {
+  const float fresh = __uint_as_float(top) / (INT8 ? 127.0f : 448.0f);
+  return fresh > before || fresh != fresh ? fresh : before;
+}
+
+// Carry the codes of places 0 .. at - 1 over to another scale, 16 codes for a lane at a time; done by
+// one wave.
+template <int D, bool INT8>
+__device__ __forceinline__ void carry_over(uint8_t* codes, int at, bool values, int tokens, float before, const Divider& by) {
+  const int lane = threadIdx.x & 63, per = values ? (at + 15) >> 4 : D / 16, all = values ? D * per : at * per;
+#pragma unroll 4
+  for (int i = lane; i < all; i += 64) {
+    const int r = i / per, c = i - r * per;
+    v4u* const p = reinterpret_cast<v4u*>(codes + (values ? r * tokens + 16 * c : 16 * i));
+    const v4u old = *p;
+    v4u w;
+#pragma unroll
+    for (int k = 0; k < 4; k++) {
+      w[k] = rescaled4<INT8>(old[k], before, by);
+      if (values) {   // what is not the page's yet stays
+        const int mine = min(max(at - 16 * c - 4 * k, 0), 4);
+        const uint32_t mask = mine == 4 ? 0xFFFFFFFFu : (1u << (8 * mine)) - 1u;
+        w[k] = (w[k] & mask) | (old[k] & ~mask);
+      }
+    }
+    *p = w;
+  }
+}
+
+// C codes (a multiple of 4) of one token, four in a word.
+template <typename T, int C, bool INT8>
+__device__ __forceinline__ void codes_of(const uint32_t* w, const Divider& by, uint32_t (&q)[C / 4]) {
+#pragma unroll
+  for (int k = 0; k < C / 4; k++) {
+    float v[4];
+#pragma unroll
+    for (int e = 0; e < 4; e++) v[e] = by.s == 0.0f ? 0.0f : by(element(static_cast<const T*>(nullptr), w, 4 * k + e));
+    q[k] = codes2<INT8>(v[0], v[1]) | codes2<INT8>(v[2], v[3]) << 16;
+  }
+}
+
+// A long run, by one wave.  16 lanes hold a token's channels, D / 16 each, and the wave's four rows
+// of lanes take four tokens each of a block of 16 places, so that a value channel's 16 codes can
+// be gathered into one lane: bytes are transposed four by four within a lane, then words between
+// the rows of lanes.  Up to kBlocks blocks stay in registers between the maximum and the codes.
 template <typename T, int D, bool INT8>
-__global__ __launch_bounds__(kAppendThreads) void append_kernel(Append A) {
-  __shared__ uint32_t wave_top[kAppendThreads / 64];
-  const int64_t t0 = blockIdx.x;
-  const int head = blockIdx.y;
-  const bool values = blockIdx.z;
-  const int64_t slot = A.slots[t0];
-  if (slot < 0 || slot >= A.n_slots) return;
-  const int64_t page = slot >> A.shift;
-  const int tokens = 1 << A.shift, at = (int)(slot & (tokens - 1));
-  if (t0 > 0 && A.slots[t0 - 1] >= 0 && A.slots[t0 - 1] >> A.shift == page) return;
-  int count = 1;
-  while (at + count < tokens && t0 + count < A.n_tokens && A.slots[t0 + count] == slot + count) count++;
-
-  const T* const x = static_cast<const T*>(values ? A.new_v : A.new_k) + (int64_t)head * D;
-  const int64_t row = values ? A.v_row : A.k_row;
-  uint8_t* const codes = (values ? A.v : A.k) + (page * A.heads + head) * ((int64_t)tokens * D);
-  float* const scale = (values ? A.v_scale : A.k_scale) + page * A.heads + head;
+__device__ __forceinline__ void append_long(const Run& R, int tokens) {
+  constexpr int C = D / 16, W = C * (int)sizeof(T) / 4, kBlocks = 64 / (4 * W) > 0 ? 64 / (4 * W) : 1;
+  const int lane = threadIdx.x & 63, sub = lane & 15, quarter = lane >> 4;
+  const int first = R.at & ~15, last = R.at + R.count;
+  const bool once = last - first <= 16 * kBlocks;
+  const T* const x = static_cast<const T*>(R.x) + C * sub;
+  uint32_t w[kBlocks][4][W];
+  auto load = [&](int place0, int blocks) {
+#pragma unroll
+    for (int n = 0; n < kBlocks; n++)
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        const int place = place0 + 16 * n + 4 * quarter + i;
+#pragma unroll
+        for (int j = 0; j < W; j++) w[n][i][j] = 0;
+        if (n < blocks && place >= R.at && place < last) load_words<W>(x + (place - R.at) * R.row, w[n][i]);
+      }
+  };
   uint32_t top = 0;
-  for (int e = threadIdx.x; e < count * D; e += kAppendThreads)
-    top = max(top, __float_as_uint(as_float(x[(t0 + e / D) * row + e % D])) & 0x7FFFFFFFu);
+  for (int place0 = first; place0 < last; place0 += 16 * kBlocks) {
+    load(place0, kBlocks);
+#pragma unroll
+    for (int n = 0; n < kBlocks; n++)
+#pragma unroll
+      for (int i = 0; i < 4; i++)
+#pragma unroll
+        for (int e = 0; e < C; e++) top = max(top, __float_as_uint(element(x, w[n][i], e)) & 0x7FFFFFFFu);
+  }
+  const float before = R.at > 0 ? *R.scale : 0.0f;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-  if (threadIdx.x % 64 == 0) wave_top[threadIdx.x / 64] = top;
-  const float before = at > 0 ? *scale : 0.0f;
-  __syncthreads();
+  const float now = grown<INT8>(before, top);
+  const Divider by(now, INT8 ? 127.0f : 448.0f);
+  if (now != before && R.at > 0) carry_over<D, INT8>(R.codes, R.at, R.values, tokens, before, by);
+  if (lane == 0) *R.scale = now;
+  for (int place0 = first; place0 < last; place0 += 16 * kBlocks) {
+    if (!once) load(place0, kBlocks);
 #pragma unroll
-  for (int w = 0; w < kAppendThreads / 64; w++) top = max(top, wave_top[w]);
-  const float fresh = __uint_as_float(top) / (INT8 ? 127.0f : 448.0f);
-  // a NaN of either side stays
-  const float now = fresh > before || fresh != fresh ? fresh : before;
-  if (threadIdx.x == 0) *scale = now;
-  // code (p, c) lies at p D + c of a key page, c tokens + p of a value page
-  if (now != before)
-    for (int e = threadIdx.x; e < at * D; e += kAppendThreads) {
-      const int p = e / D, c = e % D;
-      uint8_t* const q = codes + (values ? c * tokens + p : p * D + c);
-      *q = code_of<INT8>(value_of<INT8>(*q) * before, now);
+    for (int n = 0; n < kBlocks; n++) {
+      const int p0 = place0 + 16 * n;
+      if (p0 >= last) break;
+      uint32_t q[4][C / 4];
+#pragma unroll
+      for (int i = 0; i < 4; i++) codes_of<T, C, INT8>(w[n][i], by, q[i]);
+      if (!R.values) {
+#pragma unroll
+        for (int i = 0; i < 4; i++) {
+          const int place = p0 + 4 * quarter + i;
+          if (place >= R.at && place < last) {
+            uint32_t* const dst = reinterpret_cast<uint32_t*>(R.codes + place * D + C * sub);
+#pragma unroll
+            for (int k = 0; k < C / 4; k++) dst[k] = q[i][k];
+          }
+        }
+        continue;
+      }
+#pragma unroll
+      for (int k = 0; k < C / 4; k++) {
+        // t[m]: the lane's four tokens of channel 4 k + m
+        const uint32_t a = __builtin_amdgcn_perm(q[1][k], q[0][k], 0x05010400u), b = __builtin_amdgcn_perm(q[3][k], q[2][k], 0x05010400u),
+                       c = __builtin_amdgcn_perm(q[1][k], q[0][k], 0x07030602u), d = __builtin_amdgcn_perm(q[3][k], q[2][k], 0x07030602u);
+        uint32_t t[4] = {__builtin_amdgcn_perm(b, a, 0x05040100u), __builtin_amdgcn_perm(b, a, 0x07060302u),
+                         __builtin_amdgcn_perm(d, c, 0x05040100u), __builtin_amdgcn_perm(d, c, 0x07060302u)};
+        // word m of row r of lanes to word r of row m
+#pragma unroll
+        for (int m = 0; m < 4; m += 2) {
+          const auto s = __builtin_amdgcn_permlane16_swap(t[m], t[m + 1], false, false);
+          t[m] = s[0];
+          t[m + 1] = s[1];
+        }
+#pragma unroll
+        for (int m = 0; m < 2; m++) {
+          const auto s = __builtin_amdgcn_permlane32_swap(t[m], t[m + 2], false, false);
+          t[m] = s[0];
+          t[m + 2] = s[1];
+        }
+        uint8_t* const dst = R.codes + (C * sub + 4 * k + quarter) * tokens + p0;
+        if (p0 >= R.at && p0 + 16 <= last) {
+          *reinterpret_cast<v4u*>(dst) = v4u{t[0], t[1], t[2], t[3]};
+        } else {
+#pragma unroll
+          for (int e = 0; e < 16; e++)
+            if (p0 + e >= R.at && p0 + e < last) dst[e] = (uint8_t)(t[e >> 2] >> (8 * (e & 3)));
+        }
+      }
     }
-  for (int e = threadIdx.x; e < count * D; e += kAppendThreads) {
-    const int p = e / D, c = e % D;
-    codes[values ? c * tokens + at + p : (at + p) * D + c] = code_of<INT8>(as_float(x[(t0 + p) * row + c]), now);
+  }
+}
+
+// Short runs, several at a time: D / 8 lanes hold a token's channels, eight each, and take the run's
+// tokens one after the other.  Lanes without a run have count 0.
+template <typename T, int D, bool INT8>
+__device__ __forceinline__ void append_short(const Run& R, int tokens) {
+  constexpr int kLanes = D / 8, W = 8 * (int)sizeof(T) / 4;
+  const int lane = threadIdx.x & 63, sub = lane % kLanes;
+  const T* const x = static_cast<const T*>(R.x) + 8 * sub;
+  uint32_t w[W], top = 0;
+  float before = 0.0f;
+  if (R.count && R.at > 0) before = *R.scale;
+  for (int i = 0; i < R.count; i++) {
+    load_words<W>(x + i * R.row, w);
+#pragma unroll
+    for (int e = 0; e < 8; e++) top = max(top, __float_as_uint(element(x, w, e)) & 0x7FFFFFFFu);
+  }
+#pragma unroll
+  for (int d = 1; d < kLanes; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
+  const float now = grown<INT8>(before, top);
+  const Divider by(now, INT8 ? 127.0f : 448.0f);
+  // pages whose scale grew, one after the other by the whole wave
+  uint64_t carry = __ballot(R.count && R.at > 0 && now != before && sub == 0);
+  while (carry) {
+    const int from = __builtin_ctzll(carry);
+    carry &= carry - 1;
+    const uint64_t p = (uint64_t)R.codes;
+    uint8_t* const codes = (uint8_t*)((uint64_t)__builtin_amdgcn_readlane((int)(p >> 32), from) << 32 |
+                                      (uint32_t)__builtin_amdgcn_readlane((int)p, from));
+    const Divider to(__uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(now), from)), by.top);
+    carry_over<D, INT8>(codes, __builtin_amdgcn_readlane(R.at, from), __builtin_amdgcn_readlane(R.values, from), tokens,
+                        __uint_as_float(__builtin_amdgcn_readlane(__float_as_uint(before), from)), to);
+  }
+  if (!R.count) return;
+  if (sub == 0) *R.scale = now;
+  for (int i = 0; i < R.count; i++) {
+    if (R.count > 1) load_words<W>(x + i * R.row, w);
+    uint32_t q[2];
+    codes_of<T, 8, INT8>(w, by, q);
+    const int place = R.at + i;
+    if (!R.values) {
+      *reinterpret_cast<uint2*>(R.codes + place * D + 8 * sub) = make_uint2(q[0], q[1]);
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; e++) R.codes[(8 * sub + e) * tokens + place] = (uint8_t)(q[e >> 2] >> (8 * (e & 3)));
+    }
+  }
+}
+
+// A workgroup takes, for kItems of the (head, keys or values) pairs, the runs that begin among
+// WINDOW tokens.  Every wave finds them by itself from the slots; no wave waits for another.
+constexpr int kAppendThreads = 256, kItems = 4;
+constexpr int kFew = 4;    // tokens of a run that a few lanes take one by one
+
+template <typename T, int D, bool INT8, int WINDOW>
+__global__ __launch_bounds__(kAppendThreads) void append_kernel(Append A) {
+  constexpr int kShort = 64 / (D / 8);            // short runs of a wave at a time
+  constexpr int kWaves = kAppendThreads / 64;
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), tokens = 1 << A.shift;
+  const int item0 = blockIdx.y * kItems, items = min(2 * A.heads - item0, kItems);
+  for (int64_t w0 = (int64_t)blockIdx.x * WINDOW; w0 < A.n_tokens; w0 += (int64_t)gridDim.x * WINDOW) {
+    // lane i: token w0 - 1 + i, as far as the longest run that begins here may reach
+    auto slot_at = [&](int64_t t) {   // -1: not a token of the cache
+      const int64_t s = t >= 0 && t < A.n_tokens ? A.slots[t] : -1;
+      return s >= 0 && s < A.n_slots ? s : (int64_t)-1;
+    };
+    const int64_t mine = slot_at(w0 + lane), prior = slot_at(w0 + lane - 1);
+    const int64_t next = slot_at(w0 + lane + 1);
+    const uint64_t in_window = WINDOW == 64 ? ~0ull : (1ull << WINDOW) - 1;
+    const uint64_t leaders = __ballot(mine >= 0 && (prior < 0 || prior >> A.shift != mine >> A.shift)) & in_window;
+    // lanes whose token is followed by the page's next place: a run ends at the first without
+    const uint64_t goes_on = __ballot(mine >= 0 && next == mine + 1 && (next & (tokens - 1)) != 0);
+    auto slot_of = [&](int from) {
+      return (int64_t)((uint64_t)__builtin_amdgcn_readlane((int)(mine >> 32), from) << 32 |
+                       (uint32_t)__builtin_amdgcn_readlane((int)mine, from));
+    };
+    // tokens of the run that begins at lane `from` of the window
+    auto count_of = [&](int from) {
+      const uint64_t ends = ~(goes_on >> from);
+      int count = ends ? 1 + (int)__builtin_ctzll(ends) : 64;
+      if (from + count < 64) return count;
+      const int64_t slot = slot_of(from);
+      const int most = (int)min((int64_t)(tokens - (int)(slot & (tokens - 1))), A.n_tokens - (w0 + from));
+      while (count < most) {
+        const uint64_t other = ~__ballot(count + lane < most && slot_at(w0 + from + count + lane) == slot + count + lane);
+        if (other) return count + (int)__builtin_ctzll(other);
+        count += 64;
+      }
+      return most;
+    };
+    uint64_t shorts = 0;
+    for (uint64_t left = leaders; left; left &= left - 1) {
+      const int from = __builtin_ctzll(left);
+      if (count_of(from) <= kFew) shorts |= 1ull << from;
+    }
+    const int units = __popcll(shorts) * items;
+    for (int u0 = wave * kShort; u0 < units; u0 += kWaves * kShort) {
+      const int u = u0 + lane / (D / 8);
+      Run R = {};
+      uint64_t left = shorts;   // the runs of this wave's lanes, one after the other
+      for (int v = 0; v * items < u0 + kShort && left; v++, left &= left - 1) {
+        if ((v + 1) * items <= u0) continue;
+        const int from = __builtin_ctzll(left);
+        const Run one = run_of<T, D>(A, w0 + from, slot_of(from), count_of(from), item0 + max(u - v * items, 0) % items);
+        if (u / items == v) R = one;
+      }
+      append_short<T, D, INT8>(R, tokens);
+    }
+    for (uint64_t left = leaders & ~shorts; left; left &= left - 1) {
+      const int from = __builtin_ctzll(left);
+      for (int i = wave; i < items; i += kWaves)
+        append_long<T, D, INT8>(run_of<T, D>(A, w0 + from, slot_of(from), count_of(from), item0 + i), tokens);
+    }
   }
 }
 
 template <typename T, int D>
 void append_launch(const Append& A, bool int8, hipStream_t stream) {
-  const dim3 grid((uint32_t)A.n_tokens, A.heads, 2);
-  if (int8) hipLaunchKernelGGL((append_kernel<T, D, true>), grid, dim3(kAppendThreads), 0, stream, A);
-  else hipLaunchKernelGGL((append_kernel<T, D, false>), grid, dim3(kAppendThreads), 0, stream, A);
+  // Few tokens spread over more workgroups: a step of 128 requests is 128 of them.
+  const bool few = A.n_tokens <= 1024;
+  const int64_t window = few ? 4 : 16;
+  const dim3 grid((uint32_t)std::min<int64_t>((A.n_tokens + window - 1) / window, 1 << 22), (2 * A.heads + kItems - 1) / kItems);
+  if (few && int8) hipLaunchKernelGGL((append_kernel<T, D, true, 4>), grid, dim3(kAppendThreads), 0, stream, A);
+  else if (few) hipLaunchKernelGGL((append_kernel<T, D, false, 4>), grid, dim3(kAppendThreads), 0, stream, A);
+  else if (int8) hipLaunchKernelGGL((append_kernel<T, D, true, 16>), grid, dim3(kAppendThreads), 0, stream, A);
+  else hipLaunchKernelGGL((append_kernel<T, D, false, 16>), grid, dim3(kAppendThreads), 0, stream, A);
 }
 
 template <typename T>
