@@ -15,9 +15,9 @@ namespace ep {
 namespace {
 
 // ---- block tables and slot maps ------------------------------------------------------
-constexpr int kSlotThreads = 1024;
-constexpr int kSlotWaves = kSlotThreads / 64;
-constexpr int kSlotTokens = 2048;    // slots that one workgroup writes
+constexpr int kSlotThreads = 512, kSlotWaves = kSlotThreads / 64;
+constexpr int kEach = 8, kTile = kSlotThreads * kEach;   // requests of a thread, and of a tile
+constexpr int kSlotTokens = 2048;                        // slots that one workgroup writes
 
 struct Slots {
   const int32_t *cached, *fresh, *free_pages, *n_free;
@@ -29,105 +29,112 @@ struct Slots {
   int shift;           // log2 of a page's tokens
 };
 
-// Sums of a and b over the threads before this one; ta and tb get the workgroup's.
-__device__ __forceinline__ void scan2(int64_t& a, int64_t& b, int64_t& ta, int64_t& tb,
-                                      int64_t (*wave_sums)[2]) {
+// Sum of x over the threads before this one; `all` gets the workgroup's.
+__device__ __forceinline__ int64_t scan(int64_t x, int64_t& all, int64_t* wave_sums) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int64_t a0 = a, b0 = b;
+  int64_t sum = x;
 #pragma unroll
   for (int d = 1; d < 64; d *= 2) {
-    const int64_t pa = __shfl_up(a, d), pb = __shfl_up(b, d);
-    if (lane >= d) {
-      a += pa;
-      b += pb;
-    }
+    const int64_t up = __shfl_up(sum, d);
+    if (lane >= d) sum += up;
   }
   __syncthreads();   // the last use of wave_sums is over
-  if (lane == 63) {
-    wave_sums[wave][0] = a;
-    wave_sums[wave][1] = b;
-  }
+  if (lane == 63) wave_sums[wave] = sum;
   __syncthreads();
-  a -= a0;
-  b -= b0;
-  ta = tb = 0;
+  int64_t before = sum - x;
+  all = 0;
 #pragma unroll
   for (int w = 0; w < kSlotWaves; w++) {
-    if (w == wave) {
-      a += ta;
-      b += tb;
-    }
-    ta += wave_sums[w][0];
-    tb += wave_sums[w][1];
+    if (w < wave) before += wave_sums[w];
+    all += wave_sums[w];
   }
+  return before;
 }
 
-// Every workgroup walks all requests in tiles of 1024, carrying the sums of their tokens and
-// pages, and writes the slots of its own 2048 tokens; tile t's lengths, table entries and sums
-// are written by workgroup t mod the grid's size.  Walking them again in every workgroup costs
-// eight bytes a request from the caches, and saves a second launch and any waiting between
-// workgroups: 256 requests are one tile.
+// Every workgroup walks all requests in tiles of 4096, carrying the sums of their tokens and pages,
+// and writes the slots of its own 2048 tokens; tile t's lengths and sums are written by workgroup
+// t mod the grid's size.  Walking them again in every workgroup costs eight bytes a request from
+// the caches, and saves a second launch and any waiting between workgroups.  What is left is
+// latency: the counts, two scans, a search in LDS and a page number.
 __global__ __launch_bounds__(kSlotThreads) void slots_kernel(Slots S) {
-  __shared__ int64_t wave_sums[kSlotWaves][2];
-  __shared__ int64_t first_tok[kSlotThreads + 1];   // of the tile's requests
-  __shared__ int32_t first_page[kSlotThreads], held[kSlotThreads];
-  __shared__ int32_t old_tokens[kSlotThreads];      // cached, or -1 of a refused request
+  __shared__ int64_t wave_sums[kSlotWaves];
+  __shared__ int32_t first_tok[kTile];      // of the tile's requests, from this workgroup's first on
+  __shared__ int32_t first_page[kTile], held[kTile];
+  __shared__ int32_t old_tokens[kTile];     // cached, or -1 of a refused request
   const int t = threadIdx.x;
-  const int64_t n_free = max(*S.n_free, 0);
+  const int64_t n_free = max(*S.n_free, 0), most = 0x7FFFFFFF;
   const int64_t lo = (int64_t)blockIdx.x * kSlotTokens;
   const int64_t hi = lo + kSlotTokens < S.n_slots ? lo + kSlotTokens : S.n_slots;
-  const int64_t page = (int64_t)1 << S.shift;
+  const int32_t page = 1 << S.shift;
   int64_t tok = 0, pages = 0;      // before the tile
   int32_t bits = 0;
-  for (int64_t tile = 0, b0 = 0; b0 < S.n_req; tile++, b0 += kSlotThreads) {
-    const int64_t b = b0 + t;
-    int64_t cached = 0, fresh = 0;
-    if (b < S.n_req) {
-      cached = max(S.cached[b], 0);
-      fresh = max(S.fresh[b], 0);
+  for (int64_t tile = 0, b0 = 0; b0 < S.n_req; tile++, b0 += kTile) {
+    const int64_t mine = b0 + (int64_t)t * kEach;
+    int32_t cached[kEach], fresh[kEach];
+    int64_t my_tok = 0;
+#pragma unroll
+    for (int i = 0; i < kEach; i++) {
+      const bool in = mine + i < S.n_req;
+      cached[i] = in ? max(S.cached[mine + i], 0) : 0;
+      fresh[i] = in ? max(S.fresh[mine + i], 0) : 0;
+      my_tok += fresh[i];
     }
-    const int64_t have = (cached + page - 1) >> S.shift, want = (cached + fresh + page - 1) >> S.shift;
-    // tokens first: a request whose tokens do not fit the slot map asks for no pages
-    int64_t my_tok = fresh, my_page = 0, tile_tok, tile_pages, none;
-    scan2(my_tok, my_page, tile_tok, none, wave_sums);
-    my_tok += tok;
-    const bool row_fits = want <= S.table_ld, slots_fit = my_tok + fresh <= S.n_slots;
-    const int64_t need = row_fits && slots_fit ? want - have : 0;
-    int64_t off = need, dummy = 0;
-    scan2(off, dummy, tile_pages, none, wave_sums);
-    off += pages;
-    const bool paged = need == 0 || off + need <= n_free;
-    const bool ok = row_fits && slots_fit && paged;
-    first_tok[t] = my_tok;
-    first_page[t] = (int32_t)(off < 0x7FFFFFFF ? off : 0x7FFFFFFF);
-    held[t] = (int32_t)have;
-    old_tokens[t] = ok ? (int32_t)cached : -1;
-    if (t == 0) first_tok[kSlotThreads] = tok + tile_tok;
-    const bool mine = tile % gridDim.x == blockIdx.x;
-    if (mine && b < S.n_req) {
-      S.len[b] = (int32_t)(ok ? cached + fresh : cached);
-      const int64_t most = 0x7FFFFFFF;
-      S.cu[b] = (int32_t)(my_tok < most ? my_tok : most);
-      if (b == S.n_req - 1) S.cu[b + 1] = (int32_t)(my_tok + fresh < most ? my_tok + fresh : most);
-      bits |= (row_fits ? 0 : EP_STATUS_TABLE_FULL) | (slots_fit ? 0 : EP_STATUS_SLOTS_FULL) |
-              (paged ? 0 : EP_STATUS_NO_PAGES);
-      // pages taken: all that is needed, or what is needed before the first request that they
-      // do not suffice for
-      if (need > 0 && off <= n_free && off + need > n_free) *S.used = (int32_t)off;
-      if (b == S.n_req - 1 && off + need <= n_free) *S.used = (int32_t)(off + need);
+    int64_t tile_tok, tile_pages;
+    my_tok = tok + scan(my_tok, tile_tok, wave_sums);
+    // pages that a request asks for: none if it does not fit its row of the table or the slot map
+    auto pages_of = [&](int i, int64_t first, bool& row_fits, bool& slots_fit, int64_t& have) {
+      have = ((int64_t)cached[i] + page - 1) >> S.shift;
+      const int64_t want = ((int64_t)cached[i] + fresh[i] + page - 1) >> S.shift;
+      row_fits = want <= S.table_ld;
+      slots_fit = first + fresh[i] <= S.n_slots;
+      return row_fits && slots_fit ? want - have : 0;
+    };
+    int64_t need = 0, first = my_tok, have;
+    bool row_fits, slots_fit;
+#pragma unroll
+    for (int i = 0; i < kEach; i++) {
+      need += pages_of(i, first, row_fits, slots_fit, have);
+      first += fresh[i];
+    }
+    int64_t off = pages + scan(need, tile_pages, wave_sums);
+    const bool owner = tile % gridDim.x == blockIdx.x;
+    first = my_tok;
+#pragma unroll
+    for (int i = 0; i < kEach; i++) {
+      const int64_t b = mine + i;
+      need = pages_of(i, first, row_fits, slots_fit, have);
+      const bool paged = need == 0 || off + need <= n_free, ok = row_fits && slots_fit && paged;
+      const int r = t * kEach + i;
+      first_tok[r] = (int32_t)min(first - lo, most);
+      first_page[r] = (int32_t)min(off, most);
+      held[r] = (int32_t)have;
+      old_tokens[r] = ok ? cached[i] : -1;
+      if (owner && b < S.n_req) {
+        S.len[b] = ok ? cached[i] + fresh[i] : cached[i];
+        S.cu[b] = (int32_t)min(first, most);
+        if (b == S.n_req - 1) S.cu[b + 1] = (int32_t)min(first + fresh[i], most);
+        bits |= (row_fits ? 0 : EP_STATUS_TABLE_FULL) | (slots_fit ? 0 : EP_STATUS_SLOTS_FULL) |
+                (paged ? 0 : EP_STATUS_NO_PAGES);
+        // pages taken: all that is needed, or what is needed before the first request that they
+        // do not suffice for
+        if (need > 0 && off <= n_free && off + need > n_free) *S.used = (int32_t)off;
+        if (b == S.n_req - 1 && off + need <= n_free) *S.used = (int32_t)(off + need);
+      }
+      first += fresh[i];
+      off += need;
     }
     __syncthreads();
     // the tile's tokens in this workgroup's range; a token at the start of a page that its
     // request did not hold puts the page into the table
-    const int64_t from = max(lo, tok), to = min(hi, tok + tile_tok);
-    for (int64_t at = from + t; at < to; at += kSlotThreads) {
+    const int from = (int)(max(lo, tok) - lo), to = (int)(min(hi, tok + tile_tok) - lo);
+    for (int at = from + t; at < to; at += kSlotThreads) {
       int r = 0;   // the last request of the tile whose first token is not after `at`
 #pragma unroll
-      for (int d = kSlotThreads / 2; d > 0; d /= 2)
+      for (int d = kTile / 2; d > 0; d /= 2)
         if (first_tok[r + d] <= at) r += d;
       int64_t slot = -1;
       if (old_tokens[r] >= 0) {
-        const int64_t pos = old_tokens[r] + (at - first_tok[r]), j = pos >> S.shift;
+        const int32_t pos = old_tokens[r] + (at - first_tok[r]), j = pos >> S.shift;
         int32_t* const entry = S.table + (b0 + r) * S.table_ld + j;
         int32_t p;
         if (j < held[r]) {
@@ -138,11 +145,11 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(Slots S) {
         }
         slot = (int64_t)p * page + (pos & (page - 1));
       }
-      S.slots[at] = slot;
+      S.slots[lo + at] = slot;
     }
     tok += tile_tok;
     pages += tile_pages;
-    __syncthreads();
+    if (b0 + kTile < S.n_req) __syncthreads();
   }
   for (int64_t at = max(lo, tok) + t; at < hi; at += kSlotThreads) S.slots[at] = -1;
   if (bits && S.status) __hip_atomic_fetch_or(S.status, bits, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
@@ -283,10 +290,12 @@ __device__ __forceinline__ void codes_of(const uint32_t* w, const Divider& by, u
 // A long run, by one wave.  16 lanes hold a token's channels, D / 16 each, and the wave's four rows
 // of lanes take four tokens each of a block of 16 places, so that a value channel's 16 codes can
 // be gathered into one lane: bytes are transposed four by four within a lane, then words between
-// the rows of lanes.  Up to kBlocks blocks stay in registers between the maximum and the codes.
+// the rows of lanes.  Up to kBlocks blocks stay in registers between the maximum and the codes;
+// twice as many cost a wave of occupancy (58 us for 52 at 26k tokens x 8 heads), and longer runs
+// read their values again from the caches.
 template <typename T, int D, bool INT8>
 __device__ __forceinline__ void append_long(const Run& R, int tokens) {
-  constexpr int C = D / 16, W = C * (int)sizeof(T) / 4, kBlocks = 64 / (4 * W) > 0 ? 64 / (4 * W) : 1;
+  constexpr int C = D / 16, W = C * (int)sizeof(T) / 4, kBlocks = 256 / D;
   const int lane = threadIdx.x & 63, sub = lane & 15, quarter = lane >> 4;
   const int first = R.at & ~15, last = R.at + R.count;
   const bool once = last - first <= 16 * kBlocks;
