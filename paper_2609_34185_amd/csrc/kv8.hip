@@ -19,6 +19,28 @@ constexpr int kSlotThreads = 512, kSlotWaves = kSlotThreads / 64;
 constexpr int kEach = 8, kTile = kSlotThreads * kEach;   // requests of a thread, and of a tile
 constexpr int kSlotTokens = 2048;                        // slots that one workgroup writes
 
+// Where request r of a tile is kept: a word is left out after each thread's, so that threads that
+// write theirs at once meet different banks.
+constexpr int kPlaces = kTile + kTile / kEach;
+__device__ __forceinline__ int place_of(int r) { return r + r / kEach; }
+
+// A thread's counts, negative ones and those past the end as 0.
+__device__ __forceinline__ void load_counts(const int32_t* p, int64_t first, int64_t n, int32_t (&v)[kEach]) {
+  if (first + kEach <= n && (reinterpret_cast<uintptr_t>(p) & 15) == 0) {
+#pragma unroll
+    for (int i = 0; i < kEach; i += 4) {
+      const int4 x = *reinterpret_cast<const int4*>(p + first + i);
+      v[i] = max(x.x, 0);
+      v[i + 1] = max(x.y, 0);
+      v[i + 2] = max(x.z, 0);
+      v[i + 3] = max(x.w, 0);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < kEach; i++) v[i] = first + i < n ? max(p[first + i], 0) : 0;
+  }
+}
+
 struct Slots {
   const int32_t *cached, *fresh, *free_pages, *n_free;
   int32_t* table;
@@ -58,9 +80,10 @@ __device__ __forceinline__ int64_t scan(int64_t x, int64_t& all, int64_t* wave_s
 // latency: the counts, two scans, a search in LDS and a page number.
 __global__ __launch_bounds__(kSlotThreads) void slots_kernel(Slots S) {
   __shared__ int64_t wave_sums[kSlotWaves];
-  __shared__ int32_t first_tok[kTile];      // of the tile's requests, from this workgroup's first on
-  __shared__ int32_t first_page[kTile], held[kTile];
-  __shared__ int32_t old_tokens[kTile];     // cached, or -1 of a refused request
+  // of the tile's requests, r at place_of(r)
+  __shared__ int32_t first_tok[kPlaces];      // from this workgroup's first on
+  __shared__ int32_t first_page[kPlaces], held[kPlaces];
+  __shared__ int32_t old_tokens[kPlaces];     // cached, or -1 of a refused request
   const int t = threadIdx.x;
   const int64_t n_free = max(*S.n_free, 0), most = 0x7FFFFFFF;
   const int64_t lo = (int64_t)blockIdx.x * kSlotTokens;
@@ -72,13 +95,10 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(Slots S) {
     const int64_t mine = b0 + (int64_t)t * kEach;
     int32_t cached[kEach], fresh[kEach];
     int64_t my_tok = 0;
+    load_counts(S.cached, mine, S.n_req, cached);
+    load_counts(S.fresh, mine, S.n_req, fresh);
 #pragma unroll
-    for (int i = 0; i < kEach; i++) {
-      const bool in = mine + i < S.n_req;
-      cached[i] = in ? max(S.cached[mine + i], 0) : 0;
-      fresh[i] = in ? max(S.fresh[mine + i], 0) : 0;
-      my_tok += fresh[i];
-    }
+    for (int i = 0; i < kEach; i++) my_tok += fresh[i];
     int64_t tile_tok, tile_pages;
     my_tok = tok + scan(my_tok, tile_tok, wave_sums);
     // pages that a request asks for: none if it does not fit its row of the table or the slot map
@@ -104,7 +124,7 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(Slots S) {
       const int64_t b = mine + i;
       need = pages_of(i, first, row_fits, slots_fit, have);
       const bool paged = need == 0 || off + need <= n_free, ok = row_fits && slots_fit && paged;
-      const int r = t * kEach + i;
+      const int r = place_of(t * kEach + i);
       first_tok[r] = (int32_t)min(first - lo, most);
       first_page[r] = (int32_t)min(off, most);
       held[r] = (int32_t)have;
@@ -127,25 +147,30 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(Slots S) {
     // the tile's tokens in this workgroup's range; a token at the start of a page that its
     // request did not hold puts the page into the table
     const int from = (int)(max(lo, tok) - lo), to = (int)(min(hi, tok + tile_tok) - lo);
-    for (int at = from + t; at < to; at += kSlotThreads) {
-      int r = 0;   // the last request of the tile whose first token is not after `at`
+    constexpr int kOwn = kSlotTokens / kSlotThreads;
+    int r[kOwn] = {};   // the last request of the tile whose first token is not after this thread's
 #pragma unroll
-      for (int d = kTile / 2; d > 0; d /= 2)
-        if (first_tok[r + d] <= at) r += d;
-      int64_t slot = -1;
-      if (old_tokens[r] >= 0) {
-        const int32_t pos = old_tokens[r] + (at - first_tok[r]), j = pos >> S.shift;
-        int32_t* const entry = S.table + (b0 + r) * S.table_ld + j;
-        int32_t p;
-        if (j < held[r]) {
-          p = *entry;
-        } else {
-          p = S.free_pages[first_page[r] + (j - held[r])];
-          if ((pos & (page - 1)) == 0) *entry = p;
-        }
-        slot = (int64_t)p * page + (pos & (page - 1));
+    for (int d = kTile / 2; d > 0; d /= 2)
+#pragma unroll
+      for (int u = 0; u < kOwn; u++)
+        if (first_tok[place_of(r[u] + d)] <= t + kSlotThreads * u) r[u] += d;
+    int32_t p[kOwn] = {}, in_page[kOwn], fill[kOwn];   // fill: the row's entry to write, or -1
+#pragma unroll
+    for (int u = 0; u < kOwn; u++) {
+      const int at = t + kSlotThreads * u, l = place_of(r[u]);
+      in_page[u] = fill[u] = -1;
+      if (at >= from && at < to && old_tokens[l] >= 0) {
+        const int32_t pos = old_tokens[l] + (at - first_tok[l]), j = pos >> S.shift;
+        in_page[u] = pos & (page - 1);
+        if (j >= held[l] && in_page[u] == 0) fill[u] = j;
+        p[u] = *(j < held[l] ? S.table + (b0 + r[u]) * S.table_ld + j : S.free_pages + first_page[l] + (j - held[l]));
       }
-      S.slots[lo + at] = slot;
+    }
+#pragma unroll
+    for (int u = 0; u < kOwn; u++) {
+      const int at = t + kSlotThreads * u;
+      if (fill[u] >= 0) S.table[(b0 + r[u]) * S.table_ld + fill[u]] = p[u];
+      if (at >= from && at < to) S.slots[lo + at] = in_page[u] < 0 ? -1 : (int64_t)p[u] * page + in_page[u];
     }
     tok += tile_tok;
     pages += tile_pages;
