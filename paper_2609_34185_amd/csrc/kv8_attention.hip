@@ -145,7 +145,7 @@ struct Work {
 __device__ __forceinline__ Work work_of(const Attn& A, int64_t b, int32_t h) {
   Work W;
   W.h = h;
-  W.len = (int32_t)min((int64_t)max(A.len[b], 0), min(A.table_ld << A.shift, (int64_t)0x7FFFFF00));
+  W.len = (int32_t)min((int64_t)max(A.len[b], 0), min(A.table_ld << A.shift, (int64_t)0x7FFFF000));
   W.q0 = min((int64_t)max(A.cu[b], 0), A.total_q);
   W.m = (int32_t)max(min((int64_t)max(A.cu[b + 1], 0), A.total_q) - W.q0, (int64_t)0);
   W.rows = (uint32_t)W.m * A.group;      // total_q * q_heads is at most 2^29
@@ -161,6 +161,57 @@ __device__ __forceinline__ int32_t entry_at(const Attn& A, const Work& W, int32_
 }
 __device__ __forceinline__ int32_t page_of(const Attn& A, const Work& W, int32_t t, int32_t entry) {
   return t < W.len && (uint32_t)entry < (uint32_t)A.n_pages ? entry : -1;
+}
+
+// Splits of a request's keys.
+__device__ __forceinline__ int splits_of(const Attn& A, int32_t len) {
+  return min(max((len + A.split_tokens - 1) / A.split_tokens, 1), A.splits);
+}
+
+// Item `index` of all requests' items, count(request) of them each: sets its request and its number
+// there, or returns false if there are fewer.  Every workgroup counts for itself, a request for
+// each of its 256 threads at a time, so that a launch holds no workgroups for items that short
+// requests do not have but at its end.  (Workgroups without work, in turn with those that have
+// some, take half of the CUs away from them: a prompt of 64 tokens next to one of 8192 cost
+// 1485 us instead of 876.)
+template <typename Count>
+__device__ __forceinline__ bool find_item(const Attn& A, uint32_t index, int64_t& request, uint32_t& item, uint32_t& items,
+                                          Count count) {
+  __shared__ uint32_t wave_sum[kWaves], found[3];
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  uint32_t before = 0;     // items of the requests before this round's; below 2^31 in all
+  if (threadIdx.x == 0) found[2] = 0;
+  for (int64_t b0 = 0; b0 < A.n_req && before <= index; b0 += 64 * kWaves) {
+    const int64_t b = b0 + threadIdx.x;
+    const uint32_t mine = b < A.n_req ? count(b) : 0;
+    uint32_t sum = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const uint32_t up = __shfl_up(sum, d);
+      if (lane >= d) sum += up;
+    }
+    __syncthreads();       // the last round's sums are read
+    if (lane == 63) wave_sum[wave] = sum;
+    __syncthreads();
+    uint32_t all = 0, first = before + sum - mine;
+#pragma unroll
+    for (int w = 0; w < kWaves; w++) {
+      if (w < wave) first += wave_sum[w];
+      all += wave_sum[w];
+    }
+    if (index >= first && index < first + mine) {
+      found[0] = (uint32_t)(b - b0);
+      found[1] = index - first;
+      found[2] = mine;
+    }
+    request = b0;
+    before += all;
+  }
+  __syncthreads();
+  items = __builtin_amdgcn_readfirstlane(found[2]);
+  request += __builtin_amdgcn_readfirstlane(found[0]);
+  item = __builtin_amdgcn_readfirstlane(found[1]);
+  return items != 0;
 }
 
 // Keys [low, high) are seen by query row `row`; 0 <= low, high <= len.
@@ -213,7 +264,7 @@ __device__ __forceinline__ float load_query(const Attn& A, const Work& W, uint32
 // A tile of 16 query rows of one request and kv head, against one share of its tokens.  The
 // workgroup's waves take chunks of 64 tokens in turn and join their results in LDS.
 template <int D, bool INT8, bool FP16>
-__global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
+__global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A, uint32_t tiles) {
   constexpr int kPieces = D / 64;    // 16-byte pieces of a key for each lane
   constexpr int kTiles = D / 16;     // tiles of 16 value channels
   __shared__ float join_m[kWaves][kRows], join_l[kWaves][kRows];
@@ -221,46 +272,75 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
 
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int col = lane & 15, quarter = lane >> 4;
-  const Work W = work_of(A, blockIdx.x / A.heads, blockIdx.x % A.heads);
-  const int split = blockIdx.y, page_tokens = 1 << A.shift;
-  const uint32_t rows = W.rows;
-  const int64_t head_codes = (int64_t)page_tokens * D;
-  const int64_t q_heads = (int64_t)A.heads * A.group;
+  // Up to 256 requests, one round of counting, a workgroup takes the item (tile of rows, split of
+  // keys) of that number.  With more there is work enough everywhere: a request has the workgroups
+  // of `tiles` row tiles and all splits, and they take every tiles-th tile.
+  int64_t request = blockIdx.x / A.heads;
+  uint32_t tile, split, stride = tiles;
+  const bool counted = A.n_req <= 64 * kWaves;
+  if (counted) {
+    uint32_t item, items;
+    if (!find_item(A, blockIdx.x / A.heads, request, item, items, [&](int64_t b) {
+          const Work W = work_of(A, b, 0);
+          return (W.rows + kRows - 1) / kRows * splits_of(A, W.len);
+        }))
+      return;
+    const uint32_t splits = splits_of(A, work_of(A, request, 0).len);
+    tile = item / splits;
+    split = item % splits;
+    stride = 1u << 27;         // more than there are
+  } else {
+    tile = blockIdx.y / (uint32_t)A.splits;
+    split = blockIdx.y % (uint32_t)A.splits;
+  }
+  const Work W = work_of(A, request, blockIdx.x % A.heads);
+  const uint32_t splits = splits_of(A, W.len), rows = W.rows;
+  if (split >= splits) return;
+  const int page_tokens = 1 << A.shift;
+  const int64_t head_codes = (int64_t)page_tokens * D, q_heads = (int64_t)A.heads * A.group;
 
-  for (uint32_t tile = blockIdx.z; tile * kRows < rows; tile += gridDim.z) {
+  for (; tile * kRows < rows; tile += stride) {
     const uint32_t row = min(tile * kRows + col, rows - 1);
     const Span mine = span_of(A, W, row), first = span_of(A, W, tile * kRows),
                last = span_of(A, W, min(tile * kRows + kRows - 1, rows - 1));
     // the split's share of the keys [first.low, last.high) that some row sees
-    const int share = split * A.split_tokens;
+    const int share = (int)split * A.split_tokens;
     const int begin = max(share, first.low & ~(kChunk - 1));
-    const int end = split == A.splits - 1 ? last.high : min(share + A.split_tokens, last.high);
+    const int end = split == splits - 1 ? last.high : min(share + A.split_tokens, last.high);
 
     v8h q[kPieces][2];
     const float row_scale = load_query<D, FP16>(A, W, row, quarter, q);
 
     v4f o[kTiles];
-#pragma unroll
+  #pragma unroll
     for (int t = 0; t < kTiles; t++) o[t] = v4f{};
     float top = minus_inf(), total = 0.0f;
 
+    // the table's entries for the tokens whose keys this lane loads and for those whose scores it
+    // holds, read a chunk ahead
+    int32_t entry_k = -1, entry_v = -1;
+    if (begin < end) {
+      entry_k = entry_at(A, W, begin + kChunk * wave + 16 * (col >> 2));
+      entry_v = entry_at(A, W, begin + kChunk * wave + 16 * quarter);
+    }
     for (int t0 = begin + kChunk * wave; t0 < end; t0 += kChunk * kWaves) {
-      // pages of the tokens whose keys this lane loads, and of the tokens whose scores it holds
       const int tk = t0 + 16 * (col >> 2), tv = t0 + 16 * quarter;
-      const int32_t pk = page_of(A, W, tk, entry_at(A, W, tk)), pv = page_of(A, W, tv, entry_at(A, W, tv));
+      const int32_t pk = page_of(A, W, tk, entry_k), pv = page_of(A, W, tv, entry_v);
+      entry_k = entry_at(A, W, tk + kChunk * kWaves);
+      entry_v = entry_at(A, W, tv + kChunk * kWaves);
       float ks = 0.0f, vs = 0.0f;
       v4u kc[4][kPieces], vc[kTiles];
       if (pk >= 0) {
         const uint8_t* const src = A.k + ((int64_t)pk * A.heads + W.h) * head_codes +
                                    ((tk & (page_tokens - 1)) + (col & 3)) * D + 16 * quarter;
-#pragma unroll
+  #pragma unroll
         for (int t = 0; t < 4; t++)
-#pragma unroll
+  #pragma unroll
           for (int p = 0; p < kPieces; p++) kc[t][p] = *reinterpret_cast<const v4u*>(src + 4 * t * D + 64 * p);
       } else {
-#pragma unroll
+  #pragma unroll
         for (int t = 0; t < 4; t++)
-#pragma unroll
+  #pragma unroll
           for (int p = 0; p < kPieces; p++) kc[t][p] = v4u{};
       }
       if (pv >= 0) {
@@ -268,24 +348,24 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
             A.v + ((int64_t)pv * A.heads + W.h) * head_codes + (tv & (page_tokens - 1)) + col * page_tokens;
         ks = A.k_scale[(int64_t)pv * A.heads + W.h];
         vs = A.v_scale[(int64_t)pv * A.heads + W.h];
-#pragma unroll
+  #pragma unroll
         for (int t = 0; t < kTiles; t++) vc[t] = *reinterpret_cast<const v4u*>(src + 16 * t * page_tokens);
       } else {
-#pragma unroll
+  #pragma unroll
         for (int t = 0; t < kTiles; t++) vc[t] = v4u{};
       }
 
       float s[16];
       const float f = ks * row_scale;
-#pragma unroll
+  #pragma unroll
       for (int t = 0; t < 4; t++) {
         v4f acc = {};
-#pragma unroll
+  #pragma unroll
         for (int p = 0; p < kPieces; p++) {
           acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8<INT8>(kc[t][p][0], kc[t][p][1]), q[p][0], acc, 0, 0, 0);
           acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(widen8<INT8>(kc[t][p][2], kc[t][p][3]), q[p][1], acc, 0, 0, 0);
         }
-#pragma unroll
+  #pragma unroll
         for (int r = 0; r < 4; r++) s[4 * t + r] = acc[r] * f;
       }
       // where a row of the tile does not see all of the chunk, or a page is missing
@@ -293,27 +373,27 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
       uint32_t seen = 0xFFFFu;
       if (cut) {
         seen = 0;
-#pragma unroll
+  #pragma unroll
         for (int e = 0; e < 16; e++) {
           const bool yes = pv >= 0 && tv + e < mine.high && tv + e >= mine.low;
           seen |= (uint32_t)yes << e;
           s[e] = yes ? s[e] : minus_inf();
         }
         if (!INT8) {
-#pragma unroll
+  #pragma unroll
           for (int t = 0; t < kTiles; t++)
-#pragma unroll
+  #pragma unroll
             for (int c = 0; c < 4; c++) vc[t][c] = without_nans(vc[t][c]);
         }
       }
       float mx = s[0];
-#pragma unroll
+  #pragma unroll
       for (int e = 1; e < 16; e++) mx = fmaxf(mx, s[e]);
       const float now = fmaxf(top, max4(mx));
       const float keep = exp2_from(top, now), base = now == minus_inf() ? 0.0f : now;
       float sum = 0.0f;
       v8b hi[2], lo[2];
-#pragma unroll
+  #pragma unroll
       for (int e = 0; e < 16; e++) {
         const float p = __builtin_amdgcn_exp2f(s[e] - base);
         sum += p;
@@ -325,10 +405,10 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
       }
       total = total * keep + sum;
       top = now;
-#pragma unroll
+  #pragma unroll
       for (int t = 0; t < kTiles; t++) {
         const v8b va = widen8_bf16<INT8>(vc[t][0], vc[t][1]), vb = widen8_bf16<INT8>(vc[t][2], vc[t][3]);
-#pragma unroll
+  #pragma unroll
         for (int r = 0; r < 4; r++) o[t][r] *= keep;
         o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(va, hi[0], o[t], 0, 0, 0);
         o[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vb, hi[1], o[t], 0, 0, 0);
@@ -343,7 +423,7 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
       join_m[wave][col] = top;
       join_l[wave][col] = total;
     }
-#pragma unroll
+  #pragma unroll
     for (int t = 0; t < kTiles; t++)
       *reinterpret_cast<v4f*>(&join_o[wave][col][16 * t + 4 * quarter]) = o[t];
     __syncthreads();
@@ -352,13 +432,13 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
     const uint32_t out_row = tile * kRows + r;
     if (out_row < rows) {
       float all = minus_inf(), l = 0.0f, v[kPer] = {};
-#pragma unroll
+  #pragma unroll
       for (int w = 0; w < kWaves; w++) all = fmaxf(all, join_m[w][r]);
-#pragma unroll
+  #pragma unroll
       for (int w = 0; w < kWaves; w++) {
         const float f = exp2_from(join_m[w][r], all);
         l += f * join_l[w][r];
-#pragma unroll
+  #pragma unroll
         for (int c = 0; c < kPer; c++) v[c] += f * join_o[w][r][c0 + c];
       }
       const float inv = l == 0.0f ? 0.0f : 1.0f / l;
@@ -366,17 +446,17 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
       const int64_t token = W.q0 + out_row / (uint32_t)A.group, head = W.h * A.group + out_row % (uint32_t)A.group;
       if (A.splits > 1) {
         const int64_t at = ((int64_t)split * A.total_q + token) * q_heads + head;
-#pragma unroll
+  #pragma unroll
         for (int c = 0; c < kPer; c++) A.part_out[at * D + c0 + c] = v[c] * inv;
         if (c0 == 0) A.part_lse[at] = lse2;
       } else {
         uint16_t* const dst = A.out + token * A.out_row + head * D + c0;
-#pragma unroll
+  #pragma unroll
         for (int c = 0; c < kPer; c++) dst[c] = narrow<FP16>(v[c] * inv);
         if (c0 == 0 && A.lse) A.lse[token * q_heads + head] = lse2 * kLn2;
       }
     }
-    __syncthreads();
+    __syncthreads();     // the joined results are read
   }
 }
 
@@ -389,7 +469,7 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A) {
 // multiplies them divided by `ref`, a power of two at least as large as every page's scale met so
 // far, so they stay inside FP16 whatever the scales are.  A row's maximum follows its scores only
 // when they pass it by more than 3 (weights stay below 2^15): the sums are rarely rescaled.
-constexpr int kPromptWaves = 4;
+constexpr int kPromptWaves = kWaves;
 constexpr int col_tiles(int dim) { return dim <= 128 ? 2 : 1; }   // what 256 registers hold
 constexpr int prompt_rows(int dim) { return kPromptWaves * col_tiles(dim) * 16; }
 constexpr float kLift = 12.0f, kSlack = 3.0f;
@@ -419,50 +499,6 @@ __device__ __forceinline__ uint32_t key_place(uint32_t j, uint32_t r) {
   return j ^ ((r & 3) | ((r >> 4) & 3) << 2);
 }
 
-// Tile `index` of all requests' tiles of `tile_rows` query rows: sets its request and its number
-// there, or returns false if there are fewer.  Every workgroup counts the requests' tiles for
-// itself, 256 requests at a time, so that a launch holds no workgroups for tiles that short
-// requests do not have.  (Workgroups without work, in turn with those that have some, take half of
-// the CUs away from them: a request of 64 tokens next to one of 8192 cost 1485 us instead of 876.)
-__device__ __forceinline__ bool find_tile(const Attn& A, uint32_t index, uint32_t tile_rows, int64_t& request, uint32_t& tile) {
-  constexpr int kThreads = 64 * kPromptWaves;
-  __shared__ uint32_t wave_sum[kPromptWaves], found[2];
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  uint32_t before = 0;     // tiles of the requests before this round's; below 2^31 in all
-  if (threadIdx.x == 0) found[1] = ~0u;
-  for (int64_t b0 = 0; b0 < A.n_req && before <= index; b0 += kThreads) {
-    const int64_t b = b0 + threadIdx.x;
-    uint32_t tiles = 0;
-    if (b < A.n_req) tiles = (work_of(A, b, 0).rows + tile_rows - 1) / tile_rows;
-    uint32_t sum = tiles;
-#pragma unroll
-    for (int d = 1; d < 64; d *= 2) {
-      const uint32_t up = __shfl_up(sum, d);
-      if (lane >= d) sum += up;
-    }
-    __syncthreads();       // the last round's sums are read
-    if (lane == 63) wave_sum[wave] = sum;
-    __syncthreads();
-    uint32_t all = 0, first = before + sum - tiles;
-#pragma unroll
-    for (int w = 0; w < kPromptWaves; w++) {
-      if (w < wave) first += wave_sum[w];
-      all += wave_sum[w];
-    }
-    if (index >= first && index < first + tiles) {
-      found[0] = (uint32_t)(b - b0);
-      found[1] = tiles - 1 - (index - first);   // the longest rows of a causal request first
-    }
-    request = b0;
-    before += all;
-  }
-  __syncthreads();
-  if (found[1] == ~0u) return false;
-  request += __builtin_amdgcn_readfirstlane(found[0]);
-  tile = __builtin_amdgcn_readfirstlane(found[1]);
-  return true;
-}
-
 template <int D, bool INT8, bool FP16>
 __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(Attn A) {
   constexpr int kColTiles = col_tiles(D), kPromptRows = prompt_rows(D);
@@ -474,8 +510,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quarter = lane >> 4;
   int64_t request;
-  uint32_t tile;
-  if (!find_tile(A, blockIdx.x / A.heads, kPromptRows, request, tile)) return;
+  uint32_t tile, tiles;
+  if (!find_item(A, blockIdx.x / A.heads, request, tile, tiles,
+                 [&](int64_t b) { return (work_of(A, b, 0).rows + kPromptRows - 1) / kPromptRows; }))
+    return;
+  tile = tiles - 1 - tile;     // the longest rows of a causal request first
   const Work W = work_of(A, request, blockIdx.x % A.heads);
   const int split = blockIdx.y, page_tokens = 1 << A.shift;
   const int64_t head_codes = (int64_t)page_tokens * D, q_heads = (int64_t)A.heads * A.group;
@@ -485,9 +524,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
 
   const uint32_t tile_first = tile * kPromptRows, wave_first = tile_first + 16 * kColTiles * wave;
   const Span first = span_of(A, W, tile_first), last = span_of(A, W, min(tile_first + kPromptRows - 1, W.rows - 1));
+  const int splits = splits_of(A, W.len);
+  if (split >= splits) return;
   const int share = split * A.split_tokens;
   const int begin = max(share, first.low & ~(kChunk - 1));
-  const int end = split == A.splits - 1 ? last.high : min(share + A.split_tokens, last.high);
+  const int end = split == splits - 1 ? last.high : min(share + A.split_tokens, last.high);
   // keys [wave_a.low, wave_end) are seen by some row of this wave, [wave_b.low, wave_a.high) by all
   const Span wave_a = span_of(A, W, min(wave_first, W.rows - 1)),
              wave_b = span_of(A, W, min(wave_first + 16 * kColTiles - 1, W.rows - 1));
@@ -714,15 +755,15 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
 template <int D, bool FP16>
 __global__ __launch_bounds__(256) void attention_join_kernel(Attn A) {
   constexpr int kLanes = D / 4, kPer = 256 / kLanes;
-  const int64_t b = blockIdx.x, q_heads = (int64_t)A.heads * A.group, all_rows = A.total_q * q_heads;
-  const int64_t q0 = min((int64_t)max(A.cu[b], 0), A.total_q), q1 = min((int64_t)max(A.cu[b + 1], 0), A.total_q);
-  const int c0 = threadIdx.x % kLanes * 4;
-  for (int64_t row = q0 * q_heads + blockIdx.y * kPer + threadIdx.x / kLanes; row < q1 * q_heads;
+  const int64_t q_heads = (int64_t)A.heads * A.group, all_rows = A.total_q * q_heads;
+  const Work W = work_of(A, blockIdx.x, 0);
+  const int c0 = threadIdx.x % kLanes * 4, splits = splits_of(A, W.len);
+  for (int64_t row = W.q0 * q_heads + blockIdx.y * kPer + threadIdx.x / kLanes; row < (W.q0 + W.m) * q_heads;
        row += (int64_t)gridDim.y * kPer) {
     float all = minus_inf(), l = 0.0f;
-    for (int s = 0; s < A.splits; s++) all = fmaxf(all, A.part_lse[s * all_rows + row]);
+    for (int s = 0; s < splits; s++) all = fmaxf(all, A.part_lse[s * all_rows + row]);
     v4f v = {};
-    for (int s = 0; s < A.splits; s++) {
+    for (int s = 0; s < splits; s++) {
       const float lse = A.part_lse[s * all_rows + row], f = exp2_from(lse, all);
       l += f;
       if (f != 0.0f) v += f * *reinterpret_cast<const v4f*>(A.part_out + (s * all_rows + row) * D + c0);
@@ -760,9 +801,9 @@ const char* call_fault(const ep_kv8_cache* c, const ep_kv8_attn* a) {
 
 // How a call's keys are shared out.  Workgroups are (request and head, split, row tile).
 struct Plan {
-  int64_t tiles;         // of a request in the one kernel, of all requests at most in the other
+  int64_t tiles;         // row tiles of a launch: of all requests, or (not counted) of each
   int64_t splits, split_tokens, max_q;
-  bool prompt;
+  bool prompt, counted;
 };
 
 Plan plan_of(const ep_kv8_cache& c, const ep_kv8_attn& a) {
@@ -771,9 +812,11 @@ Plan plan_of(const ep_kv8_cache& c, const ep_kv8_attn& a) {
   P.max_q = a.max_q;
   P.prompt = rows > 32;
   const int64_t want = P.prompt ? 1024 : 4096, least = P.prompt ? 512 : 256;
-  if (P.prompt) P.tiles = a.total_q * (a.q_heads / c.kv_heads) / prompt_rows(c.head_dim) + a.n_req;
-  else P.tiles = (rows + kRows - 1) / kRows;
-  const int64_t base = P.tiles * c.kv_heads * (P.prompt ? 1 : a.n_req);
+  // the tiles of all requests are at most those that total_q would fill, and one more for each
+  const int64_t tile_rows = P.prompt ? prompt_rows(c.head_dim) : kRows;
+  P.counted = P.prompt || a.n_req <= 64 * kWaves;
+  P.tiles = P.counted ? a.total_q * (a.q_heads / c.kv_heads) / tile_rows + a.n_req : std::min<int64_t>((rows + kRows - 1) / kRows, 64);
+  const int64_t base = (P.counted ? P.tiles : P.tiles * a.n_req) * c.kv_heads;
   const int64_t max_len = std::min(std::max(a.max_len, 1), 1 << 30);   // the last split takes what is past it
   const int64_t most = (max_len + least - 1) / least;
   P.splits = std::min<int64_t>({std::max<int64_t>(1, want / base), most, 256});
@@ -794,8 +837,9 @@ void attention_launch(const Attn& A, const Plan& P, int64_t n_req, hipStream_t s
                        dim3(64 * kPromptWaves), 0, stream, A);
   else
     hipLaunchKernelGGL((attention_rows_kernel<D, INT8, FP16>),
-                       dim3((uint32_t)(n_req * A.heads), (uint32_t)P.splits, (uint32_t)P.tiles), dim3(64 * kWaves), 0,
-                       stream, A);
+                       P.counted ? dim3((uint32_t)(P.tiles * P.splits * A.heads))
+                                 : dim3((uint32_t)(n_req * A.heads), (uint32_t)(P.splits * P.tiles)),
+                       dim3(64 * kWaves), 0, stream, A, (uint32_t)P.tiles);
   if (P.splits > 1) {
     const int64_t rows = P.max_q * A.heads * A.group, per = 256 / (D / 4);
     hipLaunchKernelGGL((attention_join_kernel<D, FP16>),

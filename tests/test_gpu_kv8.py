@@ -407,6 +407,16 @@ def test_attention_hints_size_the_launch_only(E, max_q, max_len):
     c.check(c.call(E, max_q=max_q, max_len=max_len))
 
 
+@pytest.mark.parametrize("max_q,max_len,window", [(1, 900, 0), (6, 900, 0), (2, 10, 40), (40, 5000, 0)])
+def test_attention_of_many_requests(E, max_q, max_len, window):
+    """More requests than a workgroup counts in one round, of all lengths from none on, with one to
+    six queries, or none."""
+    rng = np.random.default_rng(61)
+    requests = [(int(n), int(q)) for n, q in zip(rng.integers(0, 900, 700) * (rng.random(700) < 0.4), rng.integers(0, 7, 700))]
+    c = Case(requests, 8, 2, 64, 16, False, "bf16", seed=13, window=window)
+    c.check(c.call(E, max_q=max_q, max_len=max_len))
+
+
 def test_attention_wide_spread_of_scales(E):
     """Page scales over many powers of ten: weights stay inside their type, small pages count for
     what they are."""
