@@ -179,6 +179,21 @@ __device__ __forceinline__ bool find_item(const Attn& A, uint32_t index, int64_t
                                           Count count) {
   __shared__ uint32_t wave_sum[kWaves], found[3];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (A.n_req <= 64) {     // every wave by itself
+    const uint32_t mine = lane < A.n_req ? count(lane) : 0;
+    uint32_t sum = mine;
+#pragma unroll
+    for (int d = 1; d < 64; d *= 2) {
+      const uint32_t up = __shfl_up(sum, d);
+      if (lane >= d) sum += up;
+    }
+    const uint64_t hit = __ballot(index >= sum - mine && index < sum);
+    if (!hit) return false;
+    request = __builtin_ctzll(hit);
+    items = __builtin_amdgcn_readlane(mine, (int)request);
+    item = index - (__builtin_amdgcn_readlane(sum, (int)request) - items);
+    return true;
+  }
   uint32_t before = 0;     // items of the requests before this round's; below 2^31 in all
   if (threadIdx.x == 0) found[2] = 0;
   for (int64_t b0 = 0; b0 < A.n_req && before <= index; b0 += 64 * kWaves) {
@@ -285,13 +300,14 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A, uin
           return (W.rows + kRows - 1) / kRows * splits_of(A, W.len);
         }))
       return;
-    const uint32_t splits = splits_of(A, work_of(A, request, 0).len);
-    tile = item / splits;
-    split = item % splits;
+    // the tiles of one split follow each other: they read the same keys and values
+    const uint32_t row_tiles = (work_of(A, request, 0).rows + kRows - 1) / kRows;
+    tile = item % row_tiles;
+    split = item / row_tiles;
     stride = 1u << 27;         // more than there are
   } else {
-    tile = blockIdx.y / (uint32_t)A.splits;
-    split = blockIdx.y % (uint32_t)A.splits;
+    tile = blockIdx.y % tiles;
+    split = blockIdx.y / tiles;
   }
   const Work W = work_of(A, request, blockIdx.x % A.heads);
   const uint32_t splits = splits_of(A, W.len), rows = W.rows;
@@ -751,28 +767,46 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
   }
 }
 
-// Joins the splits of each query row: sum_s 2^(lse_s - max) o_s / sum_s 2^(lse_s - max).
+// Joins the splits of a query row, a workgroup for each: sum_s 2^(lse_s - max) o_s / sum_s 2^(lse_s -
+// max).  D / 4 lanes hold a row's channels, and the workgroup's groups of so many lanes take the
+// splits in turn; their sums meet in LDS in a fixed order.
 template <int D, bool FP16>
 __global__ __launch_bounds__(256) void attention_join_kernel(Attn A) {
-  constexpr int kLanes = D / 4, kPer = 256 / kLanes;
+  constexpr int kLanes = D / 4, kGroups = 256 / kLanes;
+  __shared__ float sums[kGroups][D + 4];     // a group's o, then its sum of weights
   const int64_t q_heads = (int64_t)A.heads * A.group, all_rows = A.total_q * q_heads;
   const Work W = work_of(A, blockIdx.x, 0);
-  const int c0 = threadIdx.x % kLanes * 4, splits = splits_of(A, W.len);
-  for (int64_t row = W.q0 * q_heads + blockIdx.y * kPer + threadIdx.x / kLanes; row < (W.q0 + W.m) * q_heads;
-       row += (int64_t)gridDim.y * kPer) {
+  const int group = threadIdx.x / kLanes, c0 = threadIdx.x % kLanes * 4, splits = splits_of(A, W.len);
+  for (int64_t row = W.q0 * q_heads + blockIdx.y; row < (W.q0 + W.m) * q_heads; row += gridDim.y) {
     float all = minus_inf(), l = 0.0f;
-    for (int s = 0; s < splits; s++) all = fmaxf(all, A.part_lse[s * all_rows + row]);
-    v4f v = {};
-    for (int s = 0; s < splits; s++) {
-      const float lse = A.part_lse[s * all_rows + row], f = exp2_from(lse, all);
-      l += f;
-      if (f != 0.0f) v += f * *reinterpret_cast<const v4f*>(A.part_out + (s * all_rows + row) * D + c0);
-    }
-    const float inv = l == 0.0f ? 0.0f : 1.0f / l;
-    uint16_t* const dst = A.out + row / q_heads * A.out_row + row % q_heads * D + c0;
+    for (int s = threadIdx.x & 63; s < splits; s += 64) all = fmaxf(all, A.part_lse[s * all_rows + row]);
 #pragma unroll
-    for (int c = 0; c < 4; c++) dst[c] = narrow<FP16>(v[c] * inv);
-    if (c0 == 0 && A.lse) A.lse[row] = l == 0.0f ? minus_inf() : (all + __builtin_amdgcn_logf(l)) * kLn2;
+    for (int d = 1; d < 64; d *= 2) all = fmaxf(all, __shfl_xor(all, d));
+    v4f v = {};
+#pragma unroll 4
+    for (int s = group; s < splits; s += kGroups) {
+      const float f = exp2_from(A.part_lse[s * all_rows + row], all);
+      const v4f o = *reinterpret_cast<const v4f*>(A.part_out + (s * all_rows + row) * D + c0);
+      l += f;
+#pragma unroll
+      for (int c = 0; c < 4; c++) v[c] += f == 0.0f ? 0.0f : f * o[c];
+    }
+    *reinterpret_cast<v4f*>(&sums[group][c0]) = v;
+    if (c0 == 0) sums[group][D] = l;
+    __syncthreads();
+    if (group == 0) {
+#pragma unroll
+      for (int g = 1; g < kGroups; g++) {
+        v += *reinterpret_cast<const v4f*>(&sums[g][c0]);
+        l += sums[g][D];
+      }
+      const float inv = l == 0.0f ? 0.0f : 1.0f / l;
+      uint16_t* const dst = A.out + row / q_heads * A.out_row + row % q_heads * D + c0;
+#pragma unroll
+      for (int c = 0; c < 4; c++) dst[c] = narrow<FP16>(v[c] * inv);
+      if (c0 == 0 && A.lse) A.lse[row] = l == 0.0f ? minus_inf() : (all + __builtin_amdgcn_logf(l)) * kLn2;
+    }
+    __syncthreads();
   }
 }
 
@@ -811,15 +845,18 @@ Plan plan_of(const ep_kv8_cache& c, const ep_kv8_attn& a) {
   const int64_t rows = a.max_q * (int64_t)(a.q_heads / c.kv_heads);
   P.max_q = a.max_q;
   P.prompt = rows > 32;
-  const int64_t want = P.prompt ? 1024 : 4096, least = P.prompt ? 512 : 256;
   // the tiles of all requests are at most those that total_q would fill, and one more for each
   const int64_t tile_rows = P.prompt ? prompt_rows(c.head_dim) : kRows;
   P.counted = P.prompt || a.n_req <= 64 * kWaves;
   P.tiles = P.counted ? a.total_q * (a.q_heads / c.kv_heads) / tile_rows + a.n_req : std::min<int64_t>((rows + kRows - 1) / kRows, 64);
-  const int64_t base = (P.counted ? P.tiles : P.tiles * a.n_req) * c.kv_heads;
   const int64_t max_len = std::min(std::max(a.max_len, 1), 1 << 30);   // the last split takes what is past it
-  const int64_t most = (max_len + least - 1) / least;
-  P.splits = std::min<int64_t>({std::max<int64_t>(1, want / base), most, 256});
+  // Up to ten workgroups for a CU of at least 1024 tokens (64 requests of up to 16384 tokens in 5
+  // splits: 150 us, in 2 168, in 10 158), but of 256 where that leaves less than four (3 requests
+  // of up to 1999 tokens, 8 kv heads: 11.3 us in 8 splits).  Of few rows, a request's tiles share
+  // what they read and count once.
+  const int64_t groups = (P.prompt ? P.tiles : a.n_req) * c.kv_heads;
+  P.splits = std::min(2560 / groups, std::max(max_len / 1024, std::min(1024 / groups, (max_len + 255) / 256)));
+  P.splits = std::min<int64_t>(std::max<int64_t>(P.splits, 1), 256);
   P.split_tokens = (max_len + P.splits - 1) / P.splits;
   P.split_tokens = (P.split_tokens + kChunk - 1) / kChunk * kChunk;
   return P;
@@ -841,9 +878,9 @@ void attention_launch(const Attn& A, const Plan& P, int64_t n_req, hipStream_t s
                                  : dim3((uint32_t)(n_req * A.heads), (uint32_t)(P.splits * P.tiles)),
                        dim3(64 * kWaves), 0, stream, A, (uint32_t)P.tiles);
   if (P.splits > 1) {
-    const int64_t rows = P.max_q * A.heads * A.group, per = 256 / (D / 4);
+    const int64_t rows = P.max_q * A.heads * A.group;
     hipLaunchKernelGGL((attention_join_kernel<D, FP16>),
-                       dim3((uint32_t)n_req, (uint32_t)std::min<int64_t>((rows + per - 1) / per, 65535)), dim3(256), 0,
+                       dim3((uint32_t)n_req, (uint32_t)std::min<int64_t>(rows, 65535)), dim3(256), 0,
                        stream, A);
   }
 }
