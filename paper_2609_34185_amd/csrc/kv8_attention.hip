@@ -521,7 +521,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
   constexpr int kPieces = D / 64, kTiles = D / 16;
   constexpr int kBytes = kChunk * D;                       // of a chunk's keys, and of its values
   constexpr int kLoads = kBytes / 1024 / kPromptWaves;     // direct loads of a wave for each
-  __shared__ __attribute__((aligned(1024))) uint8_t lds_mem[2][2 * kBytes];
+  constexpr int kPass = D <= 128 ? 2 : 1;                  // chunks between two barriers
+  __shared__ __attribute__((aligned(1024))) uint8_t lds_mem[2 * kPass][2 * kBytes];
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quarter = lane >> 4;
@@ -613,10 +614,24 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
         }
       }
     }
+    // the values' codes are on their way while the weights are made
+    v4u vc[kTiles];
+#pragma unroll
+    for (int t = 0; t < kTiles; t++) {
+      const uint32_t d = 16 * t + col;
+      vc[t] = *reinterpret_cast<const __attribute__((address_space(3))) v4u*>(
+          values + d * kChunk + 16 * (quarter ^ ((d >> 2) & 3)));
+    }
     float f[kColTiles];
 #pragma unroll
     for (int n = 0; n < kColTiles; n++) f[n] = ks * row_scale[n];
     if (cut) {
+      if (!INT8) {
+#pragma unroll
+        for (int t = 0; t < kTiles; t++)
+#pragma unroll
+          for (int i = 0; i < 4; i++) vc[t][i] = without_nans(vc[t][i]);
+      }
       // scores as they are, -infinity where unseen; a value scale that is not finite makes the
       // rows that see its page not-a-number, and no others
       const int tv = t0 + 16 * quarter;
@@ -683,14 +698,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
     }
 #pragma unroll
     for (int t = 0; t < kTiles; t++) {
-      const uint32_t d = 16 * t + col;
-      v4u c = *reinterpret_cast<const __attribute__((address_space(3))) v4u*>(
-          values + d * kChunk + 16 * (quarter ^ ((d >> 2) & 3)));
-      if (cut && !INT8) {
-#pragma unroll
-        for (int i = 0; i < 4; i++) c[i] = without_nans(c[i]);
-      }
-      const v8h a = widen8<INT8>(c[0], c[1]), b = widen8<INT8>(c[2], c[3]);
+      const v8h a = widen8<INT8>(vc[t][0], vc[t][1]), b = widen8<INT8>(vc[t][2], vc[t][3]);
 #pragma unroll
       for (int n = 0; n < kColTiles; n++) {
         o[t][n] = __builtin_amdgcn_mfma_f32_16x16x32_f16(a, w[0][n], o[t][n], 0, 0, 0);
@@ -699,44 +707,65 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
     }
   };
 
-  // page and scales of the lane's run of 16 tokens, and the table's entry of the next chunk's:
-  // loaded a chunk before they are used, as the codes are
-  int32_t page = -1, entry = -1;
-  float ks = 0.0f, vs = 0.0f;
+  // pages and scales of the lane's runs of 16 tokens, and the table's entries of the next pass's:
+  // loaded a pass before they are used, as the codes are
+  int32_t page[kPass], entry[kPass];
+  float ks[kPass], vs[kPass];
   auto scales = [&](int32_t p, float& k, float& v) {
     const int64_t at = (int64_t)max(p, 0) * A.heads + W.h;
     k = A.k_scale[at];
     v = A.v_scale[at];
   };
-  if (begin < end) {
-    page = page_of(A, W, begin + 16 * quarter, entry_at(A, W, begin + 16 * quarter));
-    fetch(begin, page, 0);
-    scales(page, ks, vs);
-    entry = entry_at(A, W, begin + kChunk + 16 * quarter);
+#pragma unroll
+  for (int g = 0; g < kPass; g++) {
+    const int t = begin + kChunk * g;
+    page[g] = entry[g] = -1;
+    ks[g] = vs[g] = 0.0f;
+    if (t < end) {
+      page[g] = page_of(A, W, t + 16 * quarter, entry_at(A, W, t + 16 * quarter));
+      fetch(t, page[g], g);
+      scales(page[g], ks[g], vs[g]);
+      entry[g] = entry_at(A, W, t + kChunk * kPass + 16 * quarter);
+    }
   }
   uint32_t stage = 0;
-  for (int t0 = begin; t0 < end; t0 += kChunk) {
+  for (int t0 = begin; t0 < end; t0 += kChunk * kPass) {
     __builtin_amdgcn_sched_barrier(0);
-    __builtin_amdgcn_s_waitcnt(0x70);   // vmcnt(0) lgkmcnt(0): this chunk has landed, the last one is read
+    __builtin_amdgcn_s_waitcnt(0x70);   // vmcnt(0) lgkmcnt(0): this pass has landed, the last one is read
     __builtin_amdgcn_s_barrier();
     __builtin_amdgcn_sched_barrier(0);
-    int32_t next = -1, after = -1;
-    float next_ks = 0.0f, next_vs = 0.0f;
-    if (t0 + kChunk < end) {
-      next = page_of(A, W, t0 + kChunk + 16 * quarter, entry);
-      fetch(t0 + kChunk, next, stage ^ 1);
-      scales(next, next_ks, next_vs);
-      after = entry_at(A, W, t0 + 2 * kChunk + 16 * quarter);
+    int32_t next[kPass], after[kPass];
+    float next_ks[kPass], next_vs[kPass];
+#pragma unroll
+    for (int g = 0; g < kPass; g++) {
+      const int t = t0 + kChunk * (kPass + g);
+      next[g] = after[g] = -1;
+      next_ks[g] = next_vs[g] = 0.0f;
+      if (t < end) {
+        next[g] = page_of(A, W, t + 16 * quarter, entry[g]);
+        fetch(t, next[g], (stage ^ kPass) + g);
+        scales(next[g], next_ks[g], next_vs[g]);
+        after[g] = entry_at(A, W, t + kChunk * kPass + 16 * quarter);
+      }
     }
-    if (t0 < wave_end && t0 + kChunk > wave_a.low) {
-      const bool cut = t0 + kChunk > wave_a.high || t0 < wave_b.low || __any(page < 0);
-      chunk(t0, stage, page, page < 0 ? 0.0f : ks, page < 0 ? 0.0f : vs, cut);
+#pragma unroll 1
+    for (int g = 0; g < kPass; g++) {
+      const int t = t0 + kChunk * g;
+      if (t < min(wave_end, end) && t + kChunk > wave_a.low) {
+        const int32_t p = kPass > 1 && g ? page[kPass - 1] : page[0];
+        const float k = kPass > 1 && g ? ks[kPass - 1] : ks[0], v = kPass > 1 && g ? vs[kPass - 1] : vs[0];
+        const bool cut = t + kChunk > wave_a.high || t < wave_b.low || __any(p < 0);
+        chunk(t, stage + g, p, p < 0 ? 0.0f : k, p < 0 ? 0.0f : v, cut);
+      }
     }
-    page = next;
-    entry = after;
-    ks = next_ks;
-    vs = next_vs;
-    stage ^= 1;
+#pragma unroll
+    for (int g = 0; g < kPass; g++) {
+      page[g] = next[g];
+      entry[g] = after[g];
+      ks[g] = next_ks[g];
+      vs[g] = next_vs[g];
+    }
+    stage ^= kPass;
   }
 #pragma unroll
   for (int n = 0; n < kColTiles; n++) {
