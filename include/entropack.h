@@ -491,7 +491,7 @@ typedef struct {
   void* d_v;               /* [n_pages][kv_heads][head_dim][page_tokens] codes */
   float* d_k_scale;        /* [n_pages][kv_heads], not negative */
   float* d_v_scale;        /* [n_pages][kv_heads] */
-  int64_t n_pages;         /* below 2^31 */
+  int64_t n_pages;         /* n_pages * kv_heads at most 2^30 */
   int32_t kv_heads;
   int32_t page_tokens;
   int32_t head_dim;        /* 64, 128 or 256 */

@@ -20,7 +20,8 @@ inline const char* cache_fault(const ep_kv8_cache* c) {
   if (c->head_dim != 64 && c->head_dim != 128 && c->head_dim != 256) return "head_dim must be 64, 128 or 256";
   if (c->dtype != EP_FP8_E4M3 && c->dtype != EP_INT8) return "the cache's dtype must be FP8_E4M3 or INT8";
   if (c->kv_heads <= 0 || c->kv_heads > 1 << 16) return "kv_heads outside 1 .. 65536";
-  if (c->n_pages <= 0 || c->n_pages > 0x7FFFFFFF) return "n_pages outside 1 .. 2^31 - 1";
+  if (c->n_pages <= 0) return "n_pages must be positive";
+  if (c->n_pages > (1 << 30) / c->kv_heads) return "n_pages * kv_heads above 2^30";
   if (!c->d_k || !c->d_v || !c->d_k_scale || !c->d_v_scale) return "null array of the cache";
   if ((reinterpret_cast<uintptr_t>(c->d_k) | reinterpret_cast<uintptr_t>(c->d_v)) & 15)
     return "codes must be 16-byte aligned";

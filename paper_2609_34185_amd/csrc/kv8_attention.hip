@@ -534,7 +534,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
   tile = tiles - 1 - tile;     // the longest rows of a causal request first
   const Work W = work_of(A, request, blockIdx.x % A.heads);
   const int split = blockIdx.y, page_tokens = 1 << A.shift;
-  const int64_t head_codes = (int64_t)page_tokens * D, q_heads = (int64_t)A.heads * A.group;
+  const int64_t q_heads = (int64_t)A.heads * A.group;
   // the run of 16 tokens that this lane's value loads are of (a KiB of values is 16 channels of
   // four runs, run j of channel d at place j ^ (d / 4 mod 4))
   const uint32_t v_run = (lane & 3) ^ (quarter & 3);
@@ -570,22 +570,33 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
   // Direct loads of chunk t0, whose run `quarter` lies in `page`: this wave takes every fourth KiB
   // of the keys and of the values.  Runs with nothing to fetch take page 0, whose scores are
   // masked and whose codes are cleaned.
+  uint32_t k_off[kLoads];    // of this lane's 16 bytes in a run of 16 tokens
+#pragma unroll
+  for (int i = 0; i < kLoads; i++) {
+    const uint32_t at = 1024 * (kPromptWaves * i + wave) + 16 * lane, r = at / D;
+    k_off[i] = r % 16 * D + 16 * key_place<D>(at % D / 16, r);
+  }
+  const uint32_t v_off = (16 * wave + (lane >> 2)) * page_tokens;
+  const int code_shift = A.shift + (D == 64 ? 6 : D == 128 ? 7 : 8);   // log2 of a page and head's codes
   auto fetch = [&](int t0, int32_t page, uint32_t stage) {
     lds_u8* const dst = (lds_u8*)lds_mem[stage] + 1024 * wave;
     const int32_t in = max(page, 0);
+    // of the four runs: where their page and head begins
+    int64_t from[4];
+#pragma unroll
+    for (int j = 0; j < 4; j++)
+      from[j] = (int64_t)((uint32_t)__builtin_amdgcn_readlane(in, 16 * j) * (uint32_t)A.heads + W.h) << code_shift;
 #pragma unroll
     for (int i = 0; i < kLoads; i++) {
-      const uint32_t at = 1024 * (kPromptWaves * i + wave), run = at / (16 * D);   // the same in all lanes
-      const int64_t p = __builtin_amdgcn_readlane(in, 16 * run);
-      const uint8_t* const src = A.k + (p * A.heads + W.h) * head_codes + ((t0 + 16 * run) & (page_tokens - 1)) * D;
-      const uint32_t r = (at + 16 * lane) / D, off = r % 16 * D + 16 * key_place<D>((at + 16 * lane) % D / 16, r);
-      __builtin_amdgcn_global_load_lds((global_u8*)(src + off), dst + 1024 * kPromptWaves * i, 16, 0, 0);
+      const uint32_t run = 1024 * (kPromptWaves * i + wave) / (16 * D);   // the same in all lanes
+      const int64_t at = run < 2 ? (run < 1 ? from[0] : from[1]) : (run < 3 ? from[2] : from[3]);
+      const uint8_t* const src = A.k + at + ((t0 + 16 * (int)run) & (page_tokens - 1)) * D;
+      __builtin_amdgcn_global_load_lds((global_u8*)(src + k_off[i]), dst + 1024 * kPromptWaves * i, 16, 0, 0);
     }
-    const int32_t p0 = __builtin_amdgcn_readlane(in, 0), p1 = __builtin_amdgcn_readlane(in, 16),
-                  p2 = __builtin_amdgcn_readlane(in, 32), p3 = __builtin_amdgcn_readlane(in, 48);
-    const int32_t pv = v_run & 2 ? (v_run & 1 ? p3 : p2) : (v_run & 1 ? p1 : p0);
-    const uint8_t* const src = A.v + ((int64_t)pv * A.heads + W.h) * head_codes + ((t0 + 16 * v_run) & (page_tokens - 1)) +
-                               (16 * wave + (lane >> 2)) * page_tokens;
+#pragma unroll
+    for (int j = 0; j < 4; j++) from[j] += (t0 + 16 * j) & (page_tokens - 1);
+    const int64_t at = v_run & 2 ? (v_run & 1 ? from[3] : from[2]) : (v_run & 1 ? from[1] : from[0]);
+    const uint8_t* const src = A.v + (at + v_off);
 #pragma unroll
     for (int i = 0; i < kLoads; i++)
       __builtin_amdgcn_global_load_lds((global_u8*)(src + 16 * kPromptWaves * i * page_tokens),
@@ -712,7 +723,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
   int32_t page[kPass], entry[kPass];
   float ks[kPass], vs[kPass];
   auto scales = [&](int32_t p, float& k, float& v) {
-    const int64_t at = (int64_t)max(p, 0) * A.heads + W.h;
+    const uint32_t at = (uint32_t)max(p, 0) * (uint32_t)A.heads + W.h;
     k = A.k_scale[at];
     v = A.v_scale[at];
   };
