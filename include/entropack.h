@@ -439,7 +439,7 @@ int ep_gemm_i8_nt(const int8_t* d_a, const int8_t* d_b, int32_t* d_y, int64_t m,
 /* Activations (or weights) to FP8 E4M3 with one FP32 scale for each block of
  * block_rows (1 or 128) rows and 128 columns; the last block of a row or column
  * may be partial.  With amax the block's largest magnitude:
- *   scale = fp32(amax / 448), or 1 where that is zero;
+ *   scale = fp32(amax * fp32(1 / 448)), or 1 where that is zero;
  *   q     = E4M3(fp32(x / scale)), round to nearest even.
  * A block that holds a NaN or an infinity gets a scale that is one, so its values
  * do not pass as finite.  d_x: m rows of k elements (x_dtype EP_BF16, EP_FP16 or
@@ -534,7 +534,7 @@ int ep_kv8_slots(const int32_t* d_cached, const int32_t* d_new, int64_t n_req, i
  * The tokens that fall into one page must be consecutive in d_slots and take
  * consecutive offsets.  With o the first one's offset and top = 448 or 127, each
  * page and head gets
- *   scale' = max(scale if o > 0 else 0, fp32(amax of the new values / top))
+ *   scale' = max(scale if o > 0 else 0, fp32(amax of the new values * fp32(1 / top)))
  * the tokens before o are carried over as code' = round(fp32(fp32(code * scale) /
  * scale')) (unchanged where the scale does not grow), the new ones are round(fp32(x
  * / scale')): to nearest even, saturating, and 0 where scale' is 0.  A NaN or

@@ -62,7 +62,7 @@ __device__ __forceinline__ uint32_t top_bits(const float (&v)[8]) {
 }
 
 __device__ __forceinline__ float scale_of(uint32_t top) {
-  const float s = __uint_as_float(top) / kE4m3Max;
+  const float s = __uint_as_float(top) * (1.0f / kE4m3Max);
   return s == 0.0f ? 1.0f : s;
 }
 

@@ -272,7 +272,7 @@ __device__ __forceinline__ Run run_of(const Append& A, int64_t t0, int64_t slot,
 // The page's scale with the new tokens' largest magnitude among it; a NaN of either side stays.
 template <bool INT8>
 __device__ __forceinline__ float grown(float before, uint32_t top) {
-  const float fresh = __uint_as_float(top) / (INT8 ? 127.0f : 448.0f);
+  const float fresh = __uint_as_float(top) * (INT8 ? 1.0f / 127.0f : 1.0f / 448.0f);
   return fresh > before || fresh != fresh ? fresh : before;
 }
 

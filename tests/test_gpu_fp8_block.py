@@ -52,7 +52,7 @@ def quant_ref(x, block_rows):
     m, k = x.shape
     pm, pk = -m % block_rows, -k % 128
     b = np.pad(x, ((0, pm), (0, pk))).reshape((m + pm) // block_rows, block_rows, (k + pk) // 128, 128)
-    s = (np.abs(b).max((1, 3)) / np.float32(448)).astype(np.float32)
+    s = (np.abs(b).max((1, 3)) * (np.float32(1) / np.float32(448))).astype(np.float32)
     s = np.where(s == 0, np.float32(1), s)
     q = e4m3_codes((b / s[:, None, :, None]).astype(np.float32))
     return q.reshape(m + pm, k + pk)[:m, :k], s

@@ -155,7 +155,7 @@ def append_ref(k_codes, scales, x, slots, page, int8, is_v):
             e += 1
         for h in range(codes.shape[1]):
             before = scales[p, h] if o else np.float32(0)
-            fresh = np.abs(x[t:e, h]).max().astype(np.float32) / top
+            fresh = np.abs(x[t:e, h]).max().astype(np.float32) * (np.float32(1) / top)
             now = max(before, fresh)
             if now != before:
                 old = e4m3_value(codes[p, h, :o]) if not int8 else codes[p, h, :o].view(np.int8).astype(np.float32)
@@ -231,7 +231,7 @@ def test_append_zero_tokens_and_zero_values(E):
     assert (vc[1, 0, :, :3] == 0).all() and (vc[1, 0, :, 3:] == 0x55).all() and ks[0] == 1
     one = torch.full((1, 64), 2.0, dtype=torch.bfloat16, device="cuda")
     run_append(E, kc, vc, ks, vs, one, one, E.BF16, [19], 16, 64, False)
-    assert (kc[1, 0, :3] == 0).all() and (kc[1, 0, 3] == 0x7E).all() and ks[1] == np.float32(2) / np.float32(448)
+    assert (kc[1, 0, :3] == 0).all() and (kc[1, 0, 3] == 0x7E).all() and ks[1] == np.float32(2) * (np.float32(1) / np.float32(448))
 
 
 @pytest.mark.parametrize("int8", [False, True])
