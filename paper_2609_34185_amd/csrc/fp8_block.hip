@@ -565,30 +565,39 @@ void ring_launch(const Product& P, uint32_t height, hipStream_t stream) {
                      stream, P, height, per_xcd);
 }
 
-// Time of a tiled launch on the busiest CU for each step along k, in ns, from its tiles: measured
-// with n = 5120 and 17408, k = 5120 and 17408, m = 64 .. 2048.  `half`: when it runs as half tiles
-// alone; `one`: a CU with one tile; `each`: with more, for each of them.
+// Time of a launch on its busiest CU, in ns: what a step along k takes, and what a workgroup takes
+// besides (its first loads, its stores).  Measured with n from 438 to 17408, k from 512 to 17408 and
+// m from 64 to 4441, for outputs of 16 bits (FP8 instructions) and FP32 (FP16 instructions).
+constexpr int kBesides = 1500;
+
+// Tiles: a CU with half a tile (of W's rows), with one, and with more, for each of them.
 struct TileCost {
   int rows_w, rows_x, half, one, each;
 };
-constexpr TileCost kSmallTile = {128, 64, 510, 750, 490}, kMidTile = {128, 128, 780, 1170, 720},
-                   kLargeTile = {256, 256, 1310, 1970, 1970};
+constexpr TileCost kSmallTile[2] = {{128, 64, 510, 750, 490}, {128, 64, 640, 900, 660}},
+                   kMidTile[2] = {{128, 128, 780, 1170, 850}, {128, 128, 900, 1400, 1090}},
+                   kLargeTile[2] = {{256, 256, 1310, 1970, 1970}, {256, 256, 2200, 3650, 3650}};
 
 int64_t tile_cost(const TileCost& c, const Product& P, int cus) {
   const int64_t tiles = (P.m + c.rows_x - 1) / c.rows_x * ((P.n + c.rows_w - 1) / c.rows_w);
-  if (2 * tiles <= cus) return c.half;
-  if (tiles <= cus) return c.one;
-  const int64_t last = tiles % cus;
-  return std::max<int64_t>(c.one, c.each * (tiles / cus) + (last == 0 ? 0 : 2 * last <= cus ? c.half : c.each));
+  const int64_t halves = (2 * tiles + cus - 1) / cus;     // of the busiest CU
+  const int64_t step = halves == 1 ? c.half : std::max<int64_t>(c.one, c.each * halves / 2);
+  return step * P.kb + kBesides * ((halves + 1) / 2);
+}
+
+// Workgroups of the streaming kernel, by rounds of the chip.
+int64_t ring_cost(int step, int64_t groups, const Product& P, int cus) {
+  return (step * (int64_t)P.kb + kBesides) * rounds(groups, cus);
 }
 
 // Up to 16 rows of X the launch is W's stream from memory: 1 x 17408 x 5120 in 15.6 us with four
 // waves a workgroup, 18.0 with eight; 1 x 5120 x 17408, which has too few strips for several
-// workgroups on a CU, in 27.2 and 16.6.  Beyond, workgroups of the streaming kernel take 210 ns a
-// step with 48 x 32 rows and 270 with 48 x 64, and the tiled kernels what is stated above; the
-// least wins.
+// workgroups on a CU, in 27.2 and 16.6.  Beyond, the kernel with the least estimate.  The streaming
+// ones read X again for every strip of W, and are left out where X is what there is most of (4441 x
+// 438 x 14800: 194 us for the small tile's 88).
 template <int WFMT, int OUT, int LAYOUT>
 void product_launch(const Product& P, int cus, hipStream_t stream) {
+  constexpr bool EXACT = OUT == EP_FP32;
   if (P.m <= 16) {
     const uint32_t h = ring_height<2, 1>(P, cus);
     if (rounds(ring_groups<1>(P, h), cus) > 1) ring_launch<WFMT, OUT, LAYOUT, 2, 1, 4, 2>(P, h, stream);
@@ -596,9 +605,11 @@ void product_launch(const Product& P, int cus, hipStream_t stream) {
     return;
   }
   const uint32_t h2 = ring_height<3, 2>(P, cus), h4 = ring_height<3, 4>(P, cus);
-  const int64_t ring2 = 210 * rounds(ring_groups<2>(P, h2), cus), ring4 = 270 * rounds(ring_groups<4>(P, h4), cus);
-  const int64_t small = tile_cost(kSmallTile, P, cus), mid = tile_cost(kMidTile, P, cus),
-                large = tile_cost(kLargeTile, P, cus);
+  const int64_t never = P.m > 512 ? INT64_MAX : 0;
+  const int64_t ring2 = std::max(never, ring_cost(210, ring_groups<2>(P, h2), P, cus)),
+                ring4 = std::max(never, ring_cost(EXACT ? 320 : 270, ring_groups<4>(P, h4), P, cus));
+  const int64_t small = tile_cost(kSmallTile[EXACT], P, cus), mid = tile_cost(kMidTile[EXACT], P, cus),
+                large = tile_cost(kLargeTile[EXACT], P, cus);
   const int64_t least = std::min({ring2, ring4, small, mid, large});
   if (least == large) tiles_launch<WFMT, OUT, LAYOUT, 8, 4, 2, 4, 2>(P, cus, stream);
   else if (least == mid) tiles_launch<WFMT, OUT, LAYOUT, 4, 4, 2, 2, 2>(P, cus, stream);
