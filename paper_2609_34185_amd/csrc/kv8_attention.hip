@@ -169,18 +169,19 @@ __device__ __forceinline__ int splits_of(const Attn& A, int32_t len) {
 }
 
 // Item `index` of all requests' items, count(request) of them each: sets its request and its number
-// there, or returns false if there are fewer.  Every workgroup counts for itself, a request for
+// there, or returns false if there are fewer.  The request's head is the caller's to set.  Every workgroup counts for itself, a request for
 // each of its 256 threads at a time, so that a launch holds no workgroups for items that short
 // requests do not have but at its end.  (Workgroups without work, in turn with those that have
 // some, take half of the CUs away from them: a prompt of 64 tokens next to one of 8192 cost
 // 1485 us instead of 876.)
 template <typename Count>
-__device__ __forceinline__ bool find_item(const Attn& A, uint32_t index, int64_t& request, uint32_t& item, uint32_t& items,
+__device__ __forceinline__ bool find_item(const Attn& A, uint32_t index, Work& request, uint32_t& item, uint32_t& items,
                                           Count count) {
   __shared__ uint32_t wave_sum[kWaves], found[3];
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (A.n_req <= 64) {     // every wave by itself
-    const uint32_t mine = lane < A.n_req ? count(lane) : 0;
+    Work W = work_of(A, min((int64_t)lane, A.n_req - 1), 0);
+    const uint32_t mine = lane < A.n_req ? count(W) : 0;
     uint32_t sum = mine;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
@@ -189,16 +190,23 @@ __device__ __forceinline__ bool find_item(const Attn& A, uint32_t index, int64_t
     }
     const uint64_t hit = __ballot(index >= sum - mine && index < sum);
     if (!hit) return false;
-    request = __builtin_ctzll(hit);
-    items = __builtin_amdgcn_readlane(mine, (int)request);
-    item = index - (__builtin_amdgcn_readlane(sum, (int)request) - items);
+    const int b = __builtin_ctzll(hit);
+    items = __builtin_amdgcn_readlane(mine, b);
+    item = index - (__builtin_amdgcn_readlane(sum, b) - items);
+    // what lane b has read
+    request.q0 = __builtin_amdgcn_readlane((int)W.q0, b);        // below 2^31
+    request.len = __builtin_amdgcn_readlane(W.len, b);
+    request.m = __builtin_amdgcn_readlane(W.m, b);
+    request.rows = __builtin_amdgcn_readlane(W.rows, b);
+    request.table = A.table + b * A.table_ld;
     return true;
   }
   uint32_t before = 0;     // items of the requests before this round's; below 2^31 in all
+  int64_t round = 0;
   if (threadIdx.x == 0) found[2] = 0;
   for (int64_t b0 = 0; b0 < A.n_req && before <= index; b0 += 64 * kWaves) {
     const int64_t b = b0 + threadIdx.x;
-    const uint32_t mine = b < A.n_req ? count(b) : 0;
+    const uint32_t mine = b < A.n_req ? count(work_of(A, b, 0)) : 0;
     uint32_t sum = mine;
 #pragma unroll
     for (int d = 1; d < 64; d *= 2) {
@@ -219,14 +227,15 @@ __device__ __forceinline__ bool find_item(const Attn& A, uint32_t index, int64_t
       found[1] = index - first;
       found[2] = mine;
     }
-    request = b0;
+    round = b0;
     before += all;
   }
   __syncthreads();
   items = __builtin_amdgcn_readfirstlane(found[2]);
-  request += __builtin_amdgcn_readfirstlane(found[0]);
+  if (items == 0) return false;
   item = __builtin_amdgcn_readfirstlane(found[1]);
-  return items != 0;
+  request = work_of(A, round + __builtin_amdgcn_readfirstlane(found[0]), 0);
+  return true;
 }
 
 // Keys [low, high) are seen by query row `row`; 0 <= low, high <= len.
@@ -290,26 +299,24 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A, uin
   // Up to 256 requests, one round of counting, a workgroup takes the item (tile of rows, split of
   // keys) of that number.  With more there is work enough everywhere: a request has the workgroups
   // of `tiles` row tiles and all splits, and they take every tiles-th tile.
-  int64_t request = blockIdx.x / A.heads;
+  Work W;
   uint32_t tile, split, stride = tiles;
-  const bool counted = A.n_req <= 64 * kWaves;
-  if (counted) {
+  if (A.n_req <= 64 * kWaves) {
     uint32_t item, items;
-    if (!find_item(A, blockIdx.x / A.heads, request, item, items, [&](int64_t b) {
-          const Work W = work_of(A, b, 0);
-          return (W.rows + kRows - 1) / kRows * splits_of(A, W.len);
-        }))
+    if (!find_item(A, blockIdx.x / A.heads, W, item, items,
+                   [&](const Work& R) { return (R.rows + kRows - 1) / kRows * splits_of(A, R.len); }))
       return;
     // the tiles of one split follow each other: they read the same keys and values
-    const uint32_t row_tiles = (work_of(A, request, 0).rows + kRows - 1) / kRows;
+    const uint32_t row_tiles = (W.rows + kRows - 1) / kRows;
     tile = item % row_tiles;
     split = item / row_tiles;
     stride = 1u << 27;         // more than there are
   } else {
+    W = work_of(A, blockIdx.x / A.heads, 0);
     tile = blockIdx.y % tiles;
     split = blockIdx.y / tiles;
   }
-  const Work W = work_of(A, request, blockIdx.x % A.heads);
+  W.h = blockIdx.x % A.heads;
   const uint32_t splits = splits_of(A, W.len), rows = W.rows;
   if (split >= splits) return;
   const int page_tokens = 1 << A.shift;
@@ -526,13 +533,12 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int col = lane & 15, quarter = lane >> 4;
-  int64_t request;
+  Work W;
   uint32_t tile, tiles;
-  if (!find_item(A, blockIdx.x / A.heads, request, tile, tiles,
-                 [&](int64_t b) { return (work_of(A, b, 0).rows + kPromptRows - 1) / kPromptRows; }))
+  if (!find_item(A, blockIdx.x / A.heads, W, tile, tiles, [&](const Work& R) { return (R.rows + kPromptRows - 1) / kPromptRows; }))
     return;
+  W.h = blockIdx.x % A.heads;
   tile = tiles - 1 - tile;     // the longest rows of a causal request first
-  const Work W = work_of(A, request, blockIdx.x % A.heads);
   const int split = blockIdx.y, page_tokens = 1 << A.shift;
   const int64_t q_heads = (int64_t)A.heads * A.group;
   // the run of 16 tokens that this lane's value loads are of (a KiB of values is 16 channels of
