@@ -256,7 +256,10 @@ template <int WFMT, int OUT, int LAYOUT, int NW, int NX, int KW, int NS>
 __global__ __launch_bounds__(64 * KW) void product_ring_kernel(Product P, uint32_t height, uint32_t per_xcd) {
   constexpr bool EXACT = OUT == EP_FP32;
   constexpr int TW = 16 * NW, TX = 16 * NX;
-  constexpr int kXScaleLoads = (TX + 63) / 64, kWScaleLoads = LAYOUT == EP_SCALE_ROW_BLOCK ? (TW + 63) / 64 : 0;
+  // scales come as the operands do: a row of X or W for a lane, or (blocks) the one or two blocks of
+  // 128 rows that the strip lies in
+  constexpr int kXScaleLoads = (TX + 63) / 64,
+                kWScaleLoads = LAYOUT == EP_SCALE_ROW ? 0 : LAYOUT == EP_SCALE_BLOCK ? 1 : (TW + 63) / 64;
   constexpr int kPerStep = (TW + TX) / 8 + kXScaleLoads + kWScaleLoads;
   constexpr int kScales = (TW + TX) * 128, kStage = kScales + 256 * (kXScaleLoads + kWScaleLoads);
   constexpr int kTiles = NW * NX;
@@ -273,7 +276,9 @@ __global__ __launch_bounds__(64 * KW) void product_ring_kernel(Product P, uint32
   const uint32_t k = (uint32_t)P.k, kb = P.kb;
   const __amdgpu_buffer_rsrc_t rx = rsrc_of(P.x + i0 * P.k, rows_x * P.k), rw = rsrc_of(P.w + j0 * P.k, rows_w * P.k);
   const __amdgpu_buffer_rsrc_t rxs = rsrc_of(P.x_scale + i0 * kb, rows_x * kb * 4);
-  const __amdgpu_buffer_rsrc_t rws = rsrc_of(P.w_scale + j0 * kb, LAYOUT == EP_SCALE_ROW_BLOCK ? rows_w * kb * 4 : 0);
+  const int64_t block0 = j0 / 128, blocks = (j0 + rows_w - 1) / 128 - block0 + 1;
+  const __amdgpu_buffer_rsrc_t rws = LAYOUT == EP_SCALE_BLOCK ? rsrc_of(P.w_scale + block0 * kb, blocks * kb * 4)
+                                                              : rsrc_of(P.w_scale + j0 * kb, LAYOUT == EP_SCALE_ROW ? 0 : rows_w * kb * 4);
 
   // direct loads: segments of 8 rows, lane l writing chunk (l mod 8) ^ swz(row) of row l / 8
   const uint32_t seg_row = lane >> 3;
@@ -319,11 +324,6 @@ __global__ __launch_bounds__(64 * KW) void product_ring_kernel(Product P, uint32
   for (uint32_t b = wave; b < kb; b += KW) {
     // the stage read last time is free: its reads have returned
     fetch(b + KW * (NS - 1), stage == 0 ? NS - 1 : stage - 1);
-    float w0 = 1.0f, w1 = 1.0f;   // of the strip's first rows, and of those past a multiple of 128
-    if (LAYOUT == EP_SCALE_BLOCK) {
-      w0 = P.w_scale[j0 / 128 * kb + b];
-      w1 = P.w_scale[(j0 + rows_w - 1) / 128 * kb + b];
-    }
     __builtin_amdgcn_sched_barrier(0);
     constexpr int kLater = (NS - 1) * kPerStep;   // loads of the stages after this one
     static_assert(kLater < 64, "vmcnt");
@@ -341,7 +341,7 @@ __global__ __launch_bounds__(64 * KW) void product_ring_kernel(Product P, uint32
 #pragma unroll
     for (int i = 0; i < NW; i++) {
       const v8i wf = fragment(p + TX * 128 + 2048 * i);
-      const float wblock = 16 * i + 4 * quarter < first_rows ? w0 : w1;
+      const float wblock = LAYOUT == EP_SCALE_BLOCK ? sc[64 * kXScaleLoads + (16 * i + 4 * quarter < first_rows ? 0 : 1)] : 1.0f;
       v4f ws;
       if (LAYOUT == EP_SCALE_ROW_BLOCK)
         ws = *reinterpret_cast<const __attribute__((address_space(3))) v4f*>(sc + 64 * kXScaleLoads + 16 * i + 4 * quarter);
