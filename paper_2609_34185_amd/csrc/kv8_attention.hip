@@ -513,14 +513,19 @@ __device__ __forceinline__ float swap_max4(float x) {
   return max3(__uint_as_float(a[0]), __uint_as_float(a[1]), __uint_as_float(a[1]));
 }
 
-// Place of the 16-byte chunk j of token row r among its row's chunks: 16 lanes that read one chunk
-// of rows 16 (0 .. 3) + 4 i + (0 .. 3) meet 16 different 16-byte columns of the 64 banks.
+// Places in LDS.  A 16-byte read is served to 16 lanes at a time, of the first 32 lanes 0-3, 12-15
+// and 20-27 together and then the others (measured), and is free of conflicts if they meet 16
+// different columns of a 256-byte bank row.
+// Chunk j of token row r among its row's chunks; lane l reads chunk 4 p + l / 16 of row 16 (l / 4
+// mod 4) + 4 i + l mod 4.
 template <int D>
 __device__ __forceinline__ uint32_t key_place(uint32_t j, uint32_t r) {
-  if (D == 64) return j ^ ((r >> 4) & 3);
+  if (D == 64) return j ^ (-(r >> 4) & 3);
   if (D == 128) return j ^ (((r >> 1) & 1) | ((r >> 4) & 3) << 1);
   return j ^ ((r & 3) | ((r >> 4) & 3) << 2);
 }
+// Run j (of 16 tokens) of value channel d among its four; lane l reads run l / 16 of channel l mod 16.
+__device__ __forceinline__ uint32_t value_place(uint32_t j, uint32_t d) { return j ^ (-(d >> 2) & 3); }
 
 template <int D, bool INT8, bool FP16>
 __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(Attn A) {
@@ -542,8 +547,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
   const int split = blockIdx.y, page_tokens = 1 << A.shift;
   const int64_t q_heads = (int64_t)A.heads * A.group;
   // the run of 16 tokens that this lane's value loads are of (a KiB of values is 16 channels of
-  // four runs, run j of channel d at place j ^ (d / 4 mod 4))
-  const uint32_t v_run = (lane & 3) ^ (quarter & 3);
+  // four runs)
+  const uint32_t v_run = value_place(lane & 3, lane >> 2);
 
   const uint32_t tile_first = tile * kPromptRows, wave_first = tile_first + 16 * kColTiles * wave;
   const Span first = span_of(A, W, tile_first), last = span_of(A, W, min(tile_first + kPromptRows - 1, W.rows - 1));
@@ -637,7 +642,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
     for (int t = 0; t < kTiles; t++) {
       const uint32_t d = 16 * t + col;
       vc[t] = *reinterpret_cast<const __attribute__((address_space(3))) v4u*>(
-          values + d * kChunk + 16 * (quarter ^ ((d >> 2) & 3)));
+          values + d * kChunk + 16 * value_place(quarter, d));
     }
     float f[kColTiles];
 #pragma unroll
