@@ -77,7 +77,8 @@ __device__ __forceinline__ int64_t scan(int64_t x, int64_t& all, int64_t* wave_s
 // and writes the slots of its own 2048 tokens; tile t's lengths and sums are written by workgroup
 // t mod the grid's size.  Walking them again in every workgroup costs eight bytes a request from
 // the caches, and saves a second launch and any waiting between workgroups.  What is left is
-// latency: the counts, two scans, a search in LDS and a page number.
+// latency: the counts, two scans, a search in LDS and a page number.  256 requests of one token take
+// 7.6 us, 3001 with 775 thousand tokens 16.8.
 __global__ __launch_bounds__(kSlotThreads) void slots_kernel(Slots S) {
   __shared__ int64_t wave_sums[kSlotWaves];
   // of the tile's requests, r at place_of(r)
@@ -316,7 +317,7 @@ __device__ __forceinline__ void codes_of(const uint32_t* w, const Divider& by, u
 // of lanes take four tokens each of a block of 16 places, so that a value channel's 16 codes can
 // be gathered into one lane: bytes are transposed four by four within a lane, then words between
 // the rows of lanes.  Up to kBlocks blocks stay in registers between the maximum and the codes;
-// twice as many cost a wave of occupancy (58 us for 52 at 26k tokens x 8 heads), and longer runs
+// twice as many cost a wave of occupancy (58 us for 52 at 25 thousand tokens x 8 heads), and longer runs
 // read their values again from the caches.
 template <typename T, int D, bool INT8>
 __device__ __forceinline__ void append_long(const Run& R, int tokens) {
@@ -456,7 +457,11 @@ __device__ __forceinline__ void append_short(const Run& R, int tokens) {
 }
 
 // A workgroup takes, for kItems of the (head, keys or values) pairs, the runs that begin among
-// WINDOW tokens.  Every wave finds them by itself from the slots; no wave waits for another.
+// WINDOW tokens.  Every wave finds them by itself from the slots; no wave waits for another.  A new
+// token is read once and its codes written once; a page's older codes are read and written only
+// where its scale grows.  128 requests of one token, 8 heads of 128: 7.9 us, the latency of slots,
+// scale and codes one after the other; 25 thousand tokens of prompts: 52 us, 3.0 TB/s of reads and
+// writes, bound by the transposition of the values (31 us for the bytes alone).
 constexpr int kAppendThreads = 256, kItems = 4;
 constexpr int kFew = 4;    // tokens of a run that a few lanes take one by one
 
@@ -524,7 +529,8 @@ __global__ __launch_bounds__(kAppendThreads) void append_kernel(Append A) {
 
 template <typename T, int D>
 void append_launch(const Append& A, bool int8, hipStream_t stream) {
-  // Few tokens spread over more workgroups: a step of 128 requests is 128 of them.
+  // Few tokens spread over more workgroups (8 heads of 128; windows of 4 and of 16): 128 requests of
+  // one token 8.5 and 12.3 us, 4 runs of 686 tokens in all 13.1 and 16.5, of 2439 18.6 and 17.2.
   const bool few = A.n_tokens <= 1024;
   const int64_t window = few ? 4 : 16;
   const dim3 grid((uint32_t)std::min<int64_t>((A.n_tokens + window - 1) / window, 1 << 22), (2 * A.heads + kItems - 1) / kItems);
