@@ -471,8 +471,8 @@ enum ep_scale_layout {
  * instructions, which carry fewer bits than FP32 (measured: off by 1.4e-5 of a
  * block of Gaussian codes, 5e-5 of uniform ones, well below those types' own
  * rounding).  FP32 outputs take FP16 instructions with FP32 sums, into which both
- * FP8 types widen exactly, at half the rate.  m may be 0 (nothing is done).  Asynchronous on hip_stream, no allocation,
- * no workspace, one launch.
+ * FP8 types widen exactly, at half the rate.  m may be 0 (nothing is done).
+ * Asynchronous on hip_stream, no allocation, no workspace, one launch.
  * Errors: EP_ERR_ARG (null or misaligned pointers, m < 0, n <= 0, k <= 0,
  * k % 16, m or n above 2^24, k above 2^22, another dtype or layout), EP_ERR_HIP. */
 int ep_gemm_fp8_block(const void* d_x, const float* d_x_scale, const void* d_w, int w_dtype,
@@ -582,7 +582,9 @@ uint64_t ep_kv8_attention_workspace(const ep_kv8_cache* cache, const ep_kv8_attn
  * cache count as unseen.  Scores, softmax statistics and sums are FP32; the codes
  * enter the matrix instructions exactly, a query with all 11 bits of FP16 (scaled
  * by a power of two for each row, its sums scaled back), a weight p rounded to
- * 11 bits (22 where a call has few query rows).  Outputs round to nearest even.
+ * 11 bits (16 where a call has few query rows).  Outputs round to nearest even.
+ * A value code that is E4M3's not-a-number under a finite scale, which
+ * ep_kv8_append never writes, may count as 0.
  * d_workspace: >= ep_kv8_attention_workspace bytes of device memory (nullable if
  * that is 0), 16-byte aligned, not shared by calls that overlap.  Equal calls give
  * equal bits.  total_q may be 0.  Asynchronous on hip_stream, no allocation, at
