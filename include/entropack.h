@@ -504,8 +504,8 @@ typedef struct {
  * page_tokens, have = ceil(cached / T) and want = ceil((cached + new) / T), it
  * needs want - have pages.  Requests take them from d_free (page numbers, *d_n_free
  * of them) in order: request b's are d_free[off .. off + need), off the need of
- * the requests before it.  A request is refused if want > table_ld
- * (EP_STATUS_TABLE_FULL), if its tokens end past n_slots (EP_STATUS_SLOTS_FULL; such
+ * the requests before it.  A request is refused if want > table_ld or cached + new
+ * passes 2^31 - 1 (EP_STATUS_TABLE_FULL), if its tokens end past n_slots (EP_STATUS_SLOTS_FULL; such
  * requests need no pages) or if off + need passes *d_n_free with need > 0
  * (EP_STATUS_NO_PAGES).  Written:
  *   d_table [n_req][table_ld] : entries have .. want - 1 of each admitted row; the

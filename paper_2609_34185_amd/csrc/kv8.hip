@@ -106,7 +106,7 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(Slots S) {
     auto pages_of = [&](int i, int64_t first, bool& row_fits, bool& slots_fit, int64_t& have) {
       have = ((int64_t)cached[i] + page - 1) >> S.shift;
       const int64_t want = ((int64_t)cached[i] + fresh[i] + page - 1) >> S.shift;
-      row_fits = want <= S.table_ld;
+      row_fits = want <= S.table_ld && (int64_t)cached[i] + fresh[i] <= most;
       slots_fit = first + fresh[i] <= S.n_slots;
       return row_fits && slots_fit ? want - have : 0;
     };
@@ -147,7 +147,7 @@ __global__ __launch_bounds__(kSlotThreads) void slots_kernel(Slots S) {
     __syncthreads();
     // the tile's tokens in this workgroup's range; a token at the start of a page that its
     // request did not hold puts the page into the table
-    const int from = (int)(max(lo, tok) - lo), to = (int)(min(hi, tok + tile_tok) - lo);
+    const int from = (int)min(max(tok - lo, (int64_t)0), (int64_t)kSlotTokens), to = (int)(min(hi, tok + tile_tok) - lo);
     constexpr int kOwn = kSlotTokens / kSlotThreads;
     int r[kOwn] = {};   // the last request of the tile whose first token is not after this thread's
 #pragma unroll

@@ -125,6 +125,28 @@ def test_slots_huge_counts_are_refused_not_wrapped(E):
     assert a[1] == [0, 0] and a[3] == [-1] * 7 and a[4] == 0 and a[5] == E.STATUS_NO_PAGES
 
 
+def test_slots_of_earlier_requests_stay_when_the_sums_pass_32_bits(E):
+    n = 9000     # several tiles of requests, the later ones past 2^32 - 2 tokens
+    cached, new = [0] * n, [1] * n
+    new[0], new[7], new[9] = 5, 2 ** 31 - 1, 2 ** 31 - 1
+    table = np.full((n, 1), -1, np.int32)
+    free = list(range(n))
+    got = slots_gpu(E, cached, new, 16, free, n, table, 4000)
+    want = slots_ref(E, cached, new, 16, free, n, table, 4000)
+    for g, w in zip(got, want):
+        assert np.array_equal(g, w)
+    assert got[3][:11] == [0, 1, 2, 3, 4, 16, 32, 48, 64, 80, 96] and got[3][11:] == [-1] * 3989
+
+
+def test_slots_refuse_requests_of_2_to_the_31_tokens(E):
+    width = 2 ** 23 + 1
+    table = np.zeros((1, width), np.int32)
+    table[0, width - 2] = 77
+    full, over = slots_gpu(E, [2 ** 31 - 2], [1], 256, [1], 1, table, 3), slots_gpu(E, [2 ** 31 - 1], [2], 256, [1], 1, table, 3)
+    assert full[1:] == ([2 ** 31 - 1], [0, 1], [77 * 256 + 254, -1, -1], 0, 0)
+    assert over[1:] == ([2 ** 31 - 1], [0, 2], [-1, -1, -1], 0, E.STATUS_TABLE_FULL) and np.array_equal(over[0], table)
+
+
 # ---- append ----------------------------------------------------------------------------------
 def e4m3_value(c):
     return torch.from_numpy(np.ascontiguousarray(c)).view(torch.float8_e4m3fn).float().numpy()
