@@ -461,7 +461,9 @@ __device__ __forceinline__ void append_short(const Run& R, int tokens) {
 // token is read once and its codes written once; a page's older codes are read and written only
 // where its scale grows.  128 requests of one token, 8 heads of 128: 7.9 us, the latency of slots,
 // scale and codes one after the other; 25 thousand tokens of prompts: 52 us, 3.0 TB/s of reads and
-// writes, bound by the transposition of the values (31 us for the bytes alone).
+// writes, bound by the latency of a long run in its wave: loads, maximum, transposition, stores (31 us
+// for the bytes alone).  Windows of a page's tokens instead of 16 took 45 us for 48 with pages of 32,
+// 62 for 57 with pages of 64, and 25 for 16 at 100 prompts of up to 40 tokens.
 constexpr int kAppendThreads = 256, kItems = 4;
 constexpr int kFew = 4;    // tokens of a run that a few lanes take one by one
 

@@ -169,9 +169,9 @@ __device__ __forceinline__ int splits_of(const Attn& A, int32_t len) {
 }
 
 // Item `index` of all requests' items, count(request) of them each: sets its request and its number
-// there, or returns false if there are fewer.  The request's head is the caller's to set.  Every workgroup counts for itself, a request for
-// each of its 256 threads at a time, so that a launch holds no workgroups for items that short
-// requests do not have but at its end.  (Workgroups without work, in turn with those that have
+// there, or returns false if there are fewer.  The request's head is the caller's to set.  Every
+// workgroup counts for itself, a request for each of its 256 threads at a time, so that a launch
+// holds no workgroups for items that short requests do not have but at its end.  (Workgroups without work, in turn with those that have
 // some, take half of the CUs away from them: a prompt of 64 tokens next to one of 8192 cost
 // 1485 us instead of 876.)
 template <typename Count>
