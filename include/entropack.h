@@ -581,8 +581,11 @@ uint64_t ep_kv8_attention_workspace(const ep_kv8_cache* cache, const ep_kv8_attn
  * pages beyond a request's length may hold anything.  Table entries outside the
  * cache count as unseen.  Scores, softmax statistics and sums are FP32; the codes
  * enter the matrix instructions exactly, a query with all 11 bits of FP16 (scaled
- * by a power of two for each row, its sums scaled back), a weight p rounded to
- * 11 bits (16 where a call has few query rows).  Outputs round to nearest even.
+ * by a power of two for each row, its sums scaled back).  A weight times its page's
+ * value scale is rounded to 16 bits where max_q is small (the kernel for few query
+ * rows), and else to 11 bits or to within 2^-37 of the largest such product that
+ * the row sees, whichever is coarser: a key that counts for less than that in its
+ * row may count as 0.  Outputs round to nearest even.
  * A value code that is E4M3's not-a-number under a finite scale, which
  * ep_kv8_append never writes, may count as 0.
  * d_workspace: >= ep_kv8_attention_workspace bytes of device memory (nullable if

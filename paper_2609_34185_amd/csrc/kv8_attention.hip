@@ -492,10 +492,14 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A, uin
 // tokens, which direct loads bring to LDS as they lie in the cache, one chunk ahead.  Every wave
 // widens the codes it reads, so LDS and its bandwidth hold 8 bits a value.
 //
-// The weights enter the second product as FP16, lifted by 2^12.  The scale of a value page
-// multiplies them divided by `ref`, a power of two at least as large as every page's scale met so
-// far, so they stay inside FP16 whatever the scales are.  A row's maximum follows its scores only
-// when they pass it by more than 3 (weights stay below 2^15): the sums are rarely rescaled.
+// A weight enters the second product with its page's value scale in the exponent, as FP16 of
+//   2^(s + log2 vs - peak + 12),
+// where a row's peak follows the largest s + log2 vs among the keys that it sees, whatever the scales
+// of others are: 11 bits down to 2^-26 of the row's largest product of weight and scale, 0 below
+// 2^-37 of it.  (Two BF16 numbers, as in the kernel for few rows, would keep those too, for half as
+// many matrix instructions again.)  The peak moves only when it is passed by more than 3, so that the
+// sums are rarely rescaled and FP16 holds 2^15.  The sum of the weights themselves, which pages of
+// small values and of zeros count in all the same, is kept apart by each lane, at a maximum of its own.
 //
 // Bound by the vector unit, which widens codes and makes weights while the matrix unit works for
 // another wave: busy 67 % of the cycles, the matrix unit 35 %.  Two causal prompts of up to 8192
@@ -505,7 +509,7 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A, uin
 constexpr int kPromptWaves = kWaves;
 constexpr int col_tiles(int dim) { return dim <= 128 ? 2 : 1; }   // what 256 registers hold
 constexpr int prompt_rows(int dim) { return kPromptWaves * col_tiles(dim) * 16; }
-constexpr float kLift = 12.0f, kSlack = 3.0f;
+constexpr float kLift = 12.0f, kSlack = 3.0f, kSumSlack = 40.0f, kNothing = -40.0f;
 
 typedef __attribute__((address_space(3))) uint8_t lds_u8;
 typedef __attribute__((address_space(1))) const uint8_t global_u8;
@@ -573,7 +577,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
   const int wave_end = wave_first < W.rows ? wave_b.high : 0;
 
   Span span[kColTiles];
-  float row_scale[kColTiles], top[kColTiles], total[kColTiles];
+  // peak: of s + log2 vs, the row's; sums of weights 2^(s - top): this lane's tokens'
+  float row_scale[kColTiles], peak[kColTiles], top[kColTiles], total[kColTiles];
   v8h q[kColTiles][kPieces][2];
   v4f o[kTiles][kColTiles];
 #pragma unroll
@@ -581,12 +586,11 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
     const uint32_t row = min(wave_first + 16 * n + col, W.rows - 1);
     span[n] = span_of(A, W, row);
     row_scale[n] = load_query<D, FP16>(A, W, row, quarter, q[n]);
-    top[n] = minus_inf();
+    peak[n] = top[n] = minus_inf();
     total[n] = 0.0f;
 #pragma unroll
     for (int t = 0; t < kTiles; t++) o[t][n] = v4f{};
   }
-  float ref = 0.0f, per_ref = 1.0f;   // and 1 / ref
 
   // Direct loads of chunk t0, whose run `quarter` lies in `page`: this wave takes every fourth KiB
   // of the keys and of the values.  Runs with nothing to fetch take page 0, whose scores are
@@ -680,23 +684,8 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
       }
       if (bad) vs = 0.0f;
     }
-    // ref to the power of two above the largest finite scale, if that is larger
-    const float most = swap_max4(vs < __builtin_inff() ? vs : 0.0f);
-    if (__any(most > ref)) {
-      const uint32_t ex = min((__float_as_uint(most) >> 23) + 1, 253u);
-      per_ref = __uint_as_float((254 - ex) << 23);
-      const float keep = ref * per_ref;
-      ref = __uint_as_float(ex << 23);
-#pragma unroll
-      for (int t = 0; t < kTiles; t++)
-#pragma unroll
-        for (int n = 0; n < kColTiles; n++) o[t][n] *= keep;
-    }
-    // the page's share of ref goes into the exponent, and out of the sum of weights again; what is
-    // below 2^-100 (zero among it) is nothing in FP16 either way
-    float part = vs * per_ref;
-    part = part < 0x1p-100f ? 0x1p-100f : part;
-    const float lift = kLift + __builtin_amdgcn_logf(part), back = __builtin_amdgcn_rcpf(part);
+    // log2 of the page's value scale, -infinity for one of zeros
+    const float log_vs = vs < 0x1p-100f ? __builtin_amdgcn_logf(vs * 0x1p100f) - 100.0f : __builtin_amdgcn_logf(vs);
     v8h w[2][kColTiles];
 #pragma unroll
     for (int n = 0; n < kColTiles; n++) {
@@ -707,16 +696,26 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
       mx = max3(mx, s[2][n][1], s[2][n][2]);
       mx = max3(mx, s[2][n][3], s[3][n][0]);
       mx = max3(mx, s[3][n][1], s[3][n][2]);
-      mx = swap_max4(max3(mx, s[3][n][3], s[3][n][3]) * f[n]);
-      if (__any(mx > top[n] + kSlack)) {
-        const float now = mx > top[n] + kSlack ? mx : top[n];
-        const float keep = exp2_from(top[n], now);
-        total[n] *= keep;
+      mx = max3(mx, s[3][n][3], s[3][n][3]) * f[n];
+      const float high = swap_max4(mx + log_vs);
+      if (__any(high > peak[n] + kSlack)) {
+        const float now = high > peak[n] + kSlack ? high : peak[n];
+        const float keep = exp2_from(peak[n], now);
 #pragma unroll
         for (int t = 0; t < kTiles; t++) o[t][n] *= keep;
+        peak[n] = now;
+      }
+      if (__any(mx > top[n] + kSumSlack)) {
+        const float now = mx > top[n] + kSumSlack ? mx : top[n];
+        total[n] *= exp2_from(top[n], now);
         top[n] = now;
       }
-      const float base = lift - (top[n] == minus_inf() ? 0.0f : top[n]);
+      // where the lane's weights are nothing in FP16 (as those of a page of zeros are) they still have
+      // to be summed, and are lifted until the largest is 2^-40
+      const float lift = log_vs + (kLift - (peak[n] == minus_inf() ? 0.0f : peak[n]));
+      const float least = kNothing - max3(mx, -0x1p126f, -0x1p126f);
+      const float base = max3(lift, least, least);
+      const float back = __builtin_amdgcn_exp2f(-(top[n] == minus_inf() ? 0.0f : top[n]) - base);
       float sum = 0.0f;
 #pragma unroll
       for (int t = 0; t < 4; t++)
@@ -802,16 +801,18 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
 #pragma unroll
   for (int n = 0; n < kColTiles; n++) {
     const uint32_t row = wave_first + 16 * n + col;
-    const float l = sum4(total[n]);
+    const float all = swap_max4(top[n]), l = sum4(total[n] * exp2_from(top[n], all));
     if (row >= W.rows) continue;
-    const float inv = l == 0.0f ? 0.0f : ref / l;
-    const float lse2 = l == 0.0f ? minus_inf() : top[n] - kLift + __builtin_amdgcn_logf(l);
+    // o 2^(peak - 12) / (l 2^all), in two steps since small pages' powers may lie outside FP32
+    const float half = 0.5f * (peak[n] - kLift - all), inv = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(half) / l;
+    const float rest = l == 0.0f ? 0.0f : __builtin_amdgcn_exp2f(half);
+    const float lse2 = l == 0.0f ? minus_inf() : all + __builtin_amdgcn_logf(l);
     const int64_t token = W.q0 + row / (uint32_t)A.group, head = W.h * A.group + row % (uint32_t)A.group;
     if (A.splits > 1) {
       const int64_t at = ((int64_t)split * A.total_q + token) * q_heads + head;
 #pragma unroll
       for (int t = 0; t < kTiles; t++)
-        *reinterpret_cast<v4f*>(A.part_out + at * D + 16 * t + 4 * quarter) = o[t][n] * inv;
+        *reinterpret_cast<v4f*>(A.part_out + at * D + 16 * t + 4 * quarter) = o[t][n] * inv * rest;
       if (quarter == 0) A.part_lse[at] = lse2;
     } else {
       uint16_t* const dst = A.out + token * A.out_row + head * D + 4 * quarter;
@@ -820,7 +821,7 @@ __global__ __launch_bounds__(64 * kPromptWaves, 2) void attention_prompt_kernel(
         typedef uint16_t v4s __attribute__((ext_vector_type(4)));
         v4s x;
 #pragma unroll
-        for (int r = 0; r < 4; r++) x[r] = narrow<FP16>(o[t][n][r] * inv);
+        for (int r = 0; r < 4; r++) x[r] = narrow<FP16>(o[t][n][r] * inv * rest);
         *reinterpret_cast<v4s*>(dst + 16 * t) = x;
       }
       if (quarter == 0 && A.lse) A.lse[token * q_heads + head] = lse2 * kLn2;

@@ -448,6 +448,91 @@ def test_attention_wide_spread_of_scales(E):
         c.check(c.call(E))
 
 
+def place_weight(c, value_scales, heavy, gap):
+    """Request 0's page i gets the value scale value_scales[i] and keys that score the same for every
+    query of it: 0 in the pages of `heavy`, 2^-gap of the weight elsewhere."""
+    one, minus = (1, 0xFF) if c.int8 else (0x38, 0xB8)
+    for i, s in enumerate(value_scales):
+        p = int(c.table[0, i])
+        c.kc[p] = 0
+        c.kc[p, :, :, 0] = one if i in heavy else minus
+        c.ks[p], c.vs[p] = 1.0, s
+    c.q[: c.requests[0][1], :, 0] = gap * math.log(2) * math.sqrt(c.dim) / 2
+
+
+def check_weights(c, out):
+    """Either kernel against the bound above with what a weight is rounded to in the one for many rows,
+    p vs to 11 bits or 2^-37 of the row's largest p vs: n 2^-37 max(p vs) times the largest code more."""
+    group, at = c.q_heads // c.heads, 0
+    scale, n_heads = 1 / math.sqrt(c.dim), c.heads
+    for b, (n, m) in enumerate(c.requests):
+        idx = c.table[b, : -(-n // c.page)].long()
+        pos, mine = torch.arange(n, device="cuda"), torch.arange(n - m, n, device="cuda")[:, None]
+        seen = (pos <= mine) if c.causal else torch.ones((m, n), dtype=torch.bool, device="cuda")
+        if c.window:
+            seen &= pos > mine - c.window
+        for h in range(n_heads):
+            page_vs = c.vs[idx, h].double().repeat_interleave(c.page)[:n]
+            key = (c.value(c.kc[idx, h]) * c.ks[idx, h].double()[:, None, None]).reshape(-1, c.dim)[:n]
+            val = c.value(c.vc[idx, h]).transpose(1, 2).reshape(-1, c.dim)[:n] * page_vs[:, None]
+            for j in range(h * group, (h + 1) * group):
+                q = c.q[at: at + m, j].double()
+                s = (q @ key.t() * scale).masked_fill(~seen, -math.inf)
+                d = (c.dim + 8) * 2.0 ** -23 * scale * ((q.abs() @ key.abs().t()) * seen).amax(1, keepdim=True)
+                p = torch.softmax(s, 1)
+                want, size = p @ val, p @ val.abs()
+                floor = n * 2.0 ** -37 * (p * page_vs).amax(1, keepdim=True) * (127 if c.int8 else 448)
+                tol = size * (2 * (2 * d + 2.0 ** -21) + 2.0 ** -11 + (n + 64) * 2.0 ** -22) + floor
+                tol = tol + 2.0 ** -8 * (want.abs() + tol)
+                off = (out[at: at + m, j].double() - want).abs()
+                assert bool((off <= tol).all()), (b, j, float((off / tol.clamp(min=1e-300)).max()))
+                lse = torch.logsumexp(s, 1)
+                assert bool(((c.lse[at: at + m, j].double() - lse).abs() <= 2 * d[:, 0] + (n + 64) * 2.0 ** -22 + 2.0 ** -21 * lse.abs()).all())
+        at += m
+
+
+@pytest.mark.parametrize("int8", [False, True])
+@pytest.mark.parametrize("r", [10, 22, 28, 32, 36, 45, 60])
+def test_attention_weight_on_pages_of_small_scales(E, r, int8):
+    """All of a row's weight on pages whose value scale is 2^-r of one that has next to none of it,
+    before or after them, behind the causal diagonal of the same chunk, or outside the window: either
+    kernel gives what the pages with the weight hold."""
+    small = 1.3 * 2.0 ** -r
+    for name, request, page, window, scales, heavy in (
+            ("large first", (192, 64), 64, 0, [1.0, small, small], (1,)),
+            ("large second", (192, 64), 64, 0, [small, 1.0, small], (0,)),
+            ("behind the diagonal", (64, 64), 16, 0, [small, small, small, 1.0], (0, 1, 2)),
+            ("outside the window", (192, 64), 16, 40, [small] * 4 + [1.0] + [small] * 7, tuple(range(5, 12)))):
+        for dim in (64, 128, 256):
+            c = Case([request, (40, 40)], 2, 2, dim, page, int8, "bf16", window=window, seed=20 + r)
+            place_weight(c, scales, heavy, 64)
+            for max_q in (1, 64):
+                say(f"  scales 2^-{r} {name} dim {dim} max_q {max_q}")
+                check_weights(c, c.call(E, max_q=max_q))
+
+
+@pytest.mark.parametrize("gap", [10, 30, 60])
+def test_attention_weight_on_pages_of_zeros(E, gap):
+    """All of a row's weight on pages of zeros (value scale 0): the others count for their share of it."""
+    for scales, heavy in (([0.0, 1.0, 1.0], (0,)), ([1.0, 0.0, 0.03], (1,)), ([0.0, 0.0, 0.0], (1,))):
+        c = Case([(192, 64), (40, 40)], 2, 2, 128, 64, False, "bf16", seed=31)
+        place_weight(c, scales, heavy, gap)
+        for max_q in (1, 64):
+            check_weights(c, c.call(E, max_q=max_q))
+
+
+@pytest.mark.parametrize("spread", [2.0 ** 60, 2.0 ** 100])
+def test_attention_scales_across_the_range_of_fp32(E, spread):
+    """Neighbouring pages whose value scales lie up to 2^200 apart: rows that see only the small ones
+    give their values, rows with weight on both give the large ones', and no sum overflows."""
+    for scales, heavy in (([1 / spread, spread, 1 / spread], (0, 2)), ([spread, 1 / spread, spread], (1,)),
+                          ([1 / spread, 1 / spread, spread], (0, 1, 2))):
+        c = Case([(192, 192)], 2, 2, 128, 64, False, "bf16", seed=33)
+        place_weight(c, scales, heavy, 64)
+        for max_q in (1, 192):
+            check_weights(c, c.call(E, max_q=max_q))
+
+
 def test_attention_zero_scales_and_large_scores(E):
     c = Case([(500, 1), (200, 60)], 8, 2, 128, 16, True, "bf16", seed=5)
     c.vs[:, 0] = 0.0
