@@ -81,6 +81,13 @@ __device__ __forceinline__ v2u codes8(const float (&v)[8], const Divider& by) {
 constexpr int kQuantThreads = 256;
 constexpr int kLanes = 16;                 // lanes on one 128-column block, eight columns each
 
+// Workgroups in one or more rows of a grid, whose x dimension holds fewer than 2^32 threads.
+dim3 quant_grid(int64_t groups) {
+  const int64_t x = std::min<int64_t>(groups, 1 << 22);
+  return dim3((uint32_t)x, (uint32_t)((groups + x - 1) / x));
+}
+__device__ __forceinline__ uint32_t quant_group() { return blockIdx.y * gridDim.x + blockIdx.x; }
+
 // One row's block of 128 for each 16 lanes: a wave reads four blocks of a row in one load of up to
 // 32 bytes a lane and keeps them in registers until the codes are made, so that X crosses the memory
 // once.  Bound by memory: 8192 x 17408 of BF16 in 80 us, 5.3 TB/s of reads and writes; a row of
@@ -91,7 +98,7 @@ __global__ __launch_bounds__(kQuantThreads) void quant_rows_kernel(const T* __re
                                                                    float* __restrict__ scale,
                                                                    uint32_t units, uint32_t kb,
                                                                    int64_t k, int64_t x_row) {
-  const uint32_t unit = blockIdx.x * (kQuantThreads / kLanes) + threadIdx.x / kLanes;
+  const uint32_t unit = quant_group() * (kQuantThreads / kLanes) + threadIdx.x / kLanes;   // below 2^32
   if (unit >= units) return;
   const uint32_t row = unit / kb, col = (unit - row * kb) * 128 + 8 * (threadIdx.x % kLanes);
   float v[8] = {};
@@ -110,11 +117,13 @@ template <typename T>
 __global__ __launch_bounds__(kQuantThreads) void quant_blocks_kernel(const T* __restrict__ x,
                                                                      uint8_t* __restrict__ q,
                                                                      float* __restrict__ scale,
-                                                                     uint32_t kb, int64_t m, int64_t k,
-                                                                     int64_t x_row) {
+                                                                     uint32_t blocks, uint32_t kb, int64_t m,
+                                                                     int64_t k, int64_t x_row) {
   constexpr int kRows = kQuantThreads / kLanes, kPasses = 128 / kRows;
   __shared__ uint32_t wave_top[kQuantThreads / 64];
-  const uint32_t bi = blockIdx.x / kb, col = (blockIdx.x - bi * kb) * 128 + 8 * (threadIdx.x % kLanes);
+  const uint32_t block = quant_group();
+  if (block >= blocks) return;
+  const uint32_t bi = block / kb, col = (block - bi * kb) * 128 + 8 * (threadIdx.x % kLanes);
   const int64_t r0 = (int64_t)bi * 128 + threadIdx.x / kLanes;
   float v[kPasses][8] = {};
   uint32_t top = 0;
@@ -135,7 +144,7 @@ __global__ __launch_bounds__(kQuantThreads) void quant_blocks_kernel(const T* __
   for (int p = 0; p < kPasses; p++)
     if (col < k && r0 + kRows * p < m)
       *reinterpret_cast<v2u*>(q + (r0 + kRows * p) * k + col) = codes8(v[p], by);
-  if (threadIdx.x == 0) scale[blockIdx.x] = s;
+  if (threadIdx.x == 0) scale[block] = s;
 }
 
 template <typename T>
@@ -143,11 +152,12 @@ void quant_launch(const void* x, uint8_t* q, float* scale, int64_t m, int64_t k,
                   int block_rows, uint32_t kb, hipStream_t stream) {
   if (block_rows == 1) {
     const uint32_t units = (uint32_t)(m * kb), per = kQuantThreads / kLanes;
-    hipLaunchKernelGGL(quant_rows_kernel<T>, dim3((units + per - 1) / per), dim3(kQuantThreads), 0, stream,
+    hipLaunchKernelGGL(quant_rows_kernel<T>, quant_grid(((int64_t)units + per - 1) / per), dim3(kQuantThreads), 0, stream,
                        static_cast<const T*>(x), q, scale, units, kb, k, x_row);
   } else {
-    hipLaunchKernelGGL(quant_blocks_kernel<T>, dim3((uint32_t)((m + 127) / 128 * kb)), dim3(kQuantThreads), 0,
-                       stream, static_cast<const T*>(x), q, scale, kb, m, k, x_row);
+    const int64_t blocks = (m + 127) / 128 * kb;
+    hipLaunchKernelGGL(quant_blocks_kernel<T>, quant_grid(blocks), dim3(kQuantThreads), 0, stream,
+                       static_cast<const T*>(x), q, scale, (uint32_t)blocks, kb, m, k, x_row);
   }
 }
 

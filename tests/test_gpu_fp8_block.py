@@ -141,6 +141,33 @@ def test_quant_non_finite_blocks_show(E):
     assert np.isnan(v[0, :128]).all() and np.isnan(v[1, 128:256]).all()
 
 
+@pytest.mark.parametrize("block_rows,m", [(1, (1 << 28) + 3), (128, (1 << 31) - 1)])
+def test_quant_of_more_blocks_than_a_grid_row_holds(E, block_rows, m):
+    """From 2^28 blocks of one row on (2^24 of 128), the workgroups fill more than one row of a grid."""
+    k, step = 16, 1 << 22
+    if torch.cuda.mem_get_info()[0] < 4 * m * k:
+        pytest.skip("needs more device memory")
+    base = torch.randn((step, k), generator=torch.Generator("cuda").manual_seed(6), device="cuda").to(torch.bfloat16)
+    q0, s0 = torch.empty((step, k), dtype=torch.uint8, device="cuda"), torch.empty(step // block_rows, device="cuda")
+    E.quant_fp8_block(base.data_ptr(), E.BF16, step, k, q0.data_ptr(), s0.data_ptr(), block_rows=block_rows, stream=stream())
+    x = torch.empty((m, k), dtype=torch.bfloat16, device="cuda")
+    for i in range(0, m, step):
+        x[i: i + step] = base[: min(step, m - i)]
+    q, s = torch.empty((m, k), dtype=torch.uint8, device="cuda"), torch.empty(-(-m // block_rows), device="cuda")
+    E.quant_fp8_block(x.data_ptr(), E.BF16, m, k, q.data_ptr(), s.data_ptr(), block_rows=block_rows, stream=stream())
+    del x
+    last = m // 128 * 128 if block_rows == 128 else m       # a block that is cut has another scale
+    for i in range(0, m, step):
+        n = min(step, last - i)
+        assert torch.equal(q[i: i + n], q0[:n]) and torch.equal(s[i // block_rows: (i + n) // block_rows], s0[: n // block_rows])
+    if last < m:
+        tail = base[last % step: last % step + m - last]
+        rq, rs = quant_ref(tail.float().cpu().numpy(), block_rows)
+        assert np.array_equal(q[last:].cpu().numpy(), rq) and np.array_equal(s[last // block_rows:].cpu().numpy(), rs[:, 0])
+    del q
+    torch.cuda.empty_cache()
+
+
 # ---- product ----------------------------------------------------------------------------
 LAYOUTS = ("block", "row_block", "row")
 
