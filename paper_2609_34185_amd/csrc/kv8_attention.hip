@@ -903,17 +903,20 @@ struct Plan {
   bool prompt, counted;
 };
 
+constexpr int64_t kMostGroups = (1 << 24) - 1;   // of 256 threads in one row of a grid
+
 Plan plan_of(const ep_kv8_cache& c, const ep_kv8_attn& a) {
   Plan P;
-  const int64_t rows = a.max_q * (int64_t)(a.q_heads / c.kv_heads);
+  const int64_t group = a.q_heads / c.kv_heads, rows = a.max_q * group;
   P.max_q = a.max_q;
   // At 8 kv heads, few-row kernel and prompt kernel: 16 rows 29 and 59 us (16 requests of up to 8000
   // tokens), 36 and 37 (64 of up to 1000); 32 rows 45 and 63, 56 and 37; 48 rows 52 and 66, 76 and 42.
-  P.prompt = rows > 32;
+  // (Also with far more queries than max_q says, whose tiles of 16 rows would not fit a grid.)
+  P.prompt = rows > 32 || (a.n_req <= 64 * kWaves && (a.total_q * group / kRows + a.n_req) * c.kv_heads > kMostGroups);
   // the tiles of all requests are at most those that total_q would fill, and one more for each
   const int64_t tile_rows = P.prompt ? prompt_rows(c.head_dim) : kRows;
   P.counted = P.prompt || a.n_req <= 64 * kWaves;
-  P.tiles = P.counted ? a.total_q * (a.q_heads / c.kv_heads) / tile_rows + a.n_req : std::min<int64_t>((rows + kRows - 1) / kRows, 64);
+  P.tiles = P.counted ? a.total_q * group / tile_rows + a.n_req : std::min<int64_t>((rows + kRows - 1) / kRows, 64);
   const int64_t max_len = std::min(std::max(a.max_len, 1), 1 << 30);   // the last split takes what is past it
   // Up to ten workgroups for a CU of at least 1024 tokens (64 requests of up to 16384 tokens in 5
   // splits: 150 us, in 2 168, in 10 158), but of 256 where that leaves less than four (3 requests
@@ -921,6 +924,7 @@ Plan plan_of(const ep_kv8_cache& c, const ep_kv8_attn& a) {
   // what they read and count once.
   const int64_t groups = (P.prompt ? P.tiles : a.n_req) * c.kv_heads;
   P.splits = std::min(2560 / groups, std::max(max_len / 1024, std::min(1024 / groups, (max_len + 255) / 256)));
+  if (P.counted && !P.prompt) P.splits = std::min(P.splits, kMostGroups / (P.tiles * c.kv_heads));
   P.splits = std::min<int64_t>(std::max<int64_t>(P.splits, 1), 256);
   P.split_tokens = (max_len + P.splits - 1) / P.splits;
   P.split_tokens = (P.split_tokens + kChunk - 1) / kChunk * kChunk;

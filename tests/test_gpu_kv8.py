@@ -604,6 +604,32 @@ def test_attention_past_32_bit_offsets(E):
         c.check(c.call(E))
 
 
+def test_attention_of_far_more_queries_than_max_q(E):
+    """2^28 query rows of one request in a call that says one: they fit a grid, and get what the same
+    queries get in a small call."""
+    some, times = 64, (1 << 18) + 1
+    c = Case([(100, some)], 16, 1, 64, 64, False, "bf16", causal=False, seed=14)
+    if torch.cuda.mem_get_info()[0] < 6 * c.q.numel() * times:
+        pytest.skip("needs more device memory")
+    want = c.call(E, lse=False)
+    c.check(want, lse=False)
+    q = c.q.repeat(times, 1, 1)
+    out = torch.empty_like(q)
+    cu = ints([0, len(q)])
+    cache = E.kv8_cache(c.kc.data_ptr(), c.vc.data_ptr(), c.ks.data_ptr(), c.vs.data_ptr(), c.pages, 1, 64, 64)
+    call = E.kv8_attention_args(q.data_ptr(), out.data_ptr(), cu.data_ptr(), c.lens.data_ptr(), c.table.data_ptr(), c.table.shape[1],
+                                1, len(q), 16, E.BF16, scale=1 / 8, causal=False, max_q=1, max_len=100)
+    assert E.kv8_attention_workspace(cache, call) == 0
+    E.kv8_attention(cache, call, 0, 0, stream())
+    torch.cuda.synchronize()
+    del q
+    for part in out.split(some * 1024):
+        got = part.view(-1, some, 16, 64)
+        assert torch.equal(got, want[None].expand_as(got))
+    del out, part, got
+    torch.cuda.empty_cache()
+
+
 def test_append_past_32_bit_offsets(E):
     page, heads, dim = 64, 8, 128
     pages = (1 << 32) // (page * heads * dim) + 2

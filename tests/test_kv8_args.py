@@ -113,3 +113,14 @@ def test_attention_refusals(E):
     refused(E, E.kv8_attention, good_cache(E), long, 0, need)
     refused(E, E.kv8_attention, good_cache(E), long, H + 4, need)
     E.kv8_attention(good_cache(E), call(total_q=0, d_q=0, d_out=0), 0, 0)
+
+
+def test_attention_workgroups_fit_a_grid_beyond_max_q(E):
+    """A call whose queries are far more than max_q says: tiles of 16 rows times splits stay below the
+    2^24 workgroups of a grid's row.  The splits show in the workspace."""
+    cache = E.kv8_cache(A, B, D, F, 1 << 20, 1, 256, 64, E.FP8_E4M3)
+    for total_q, q_heads, max_len in ((100, 8, 1 << 20), (1 << 18, 16, 1 << 20), (1 << 20, 8, 1 << 20), (1 << 22, 1, 1 << 18),
+                                      (1 << 24, 15, 1 << 20)):
+        call = E.kv8_attention_args(A, B, D, F, G, 1 << 13, 1, total_q, q_heads, E.BF16, scale=0.1, max_q=1, max_len=max_len)
+        splits = max(1, E.kv8_attention_workspace(cache, call) // (total_q * q_heads * 65 * 4))
+        assert splits * (total_q * q_heads // 16 + 1) < 1 << 24
