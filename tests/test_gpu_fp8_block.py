@@ -278,6 +278,54 @@ def test_product_of_extremes(E, m, n, k):
     assert (product_gpu(E, x, xs, w, ws * 2.0 ** -24, "row", "fp16") == 448.0 * 57344.0 * k * 2.0 ** -24).all()
 
 
+# What each kernel is reached by on 256 CUs: streaming with 8 and 4 waves (up to 16 rows of X), with 32
+# and 64 rows; small tiles whole, all halved, and the last of several rounds halved; middle ones, whole
+# and (FP32 outputs) halved; large ones all halved, whole, some halved; and middle ones with some halved
+# (FP32).  Odd m and n, k in part of its last block.
+KERNELS = [(5, 775, 1200), (11, 8279, 400), (37, 633, 656), (57, 7993, 208), (139, 8225, 336), (583, 661, 464), (259, 7083, 400),
+           (387, 4743, 272), (595, 1537, 144), (1171, 3357, 272), (2523, 3205, 208), (2011, 8193, 144), (1029, 7261, 400)]
+
+
+def check_sums(y, x, xs, w, ws, layout, y_dtype):
+    """The bound above, and for 16-bit outputs 7 2^-13 of the products' magnitudes more: of every eight
+    products the FP8 instructions cut each but the largest by less than 2^-13 of that one, whose exponent
+    is at least what the smallest normal codes have."""
+    m, n, k = x.shape[0], w.shape[0], x.shape[1]
+    a = x.double() * xs.double()[:, torch.arange(k, device="cuda") // 128]
+    b = w.double() * wide_scales(ws, layout, n, k)
+    exact, size = a @ b.t().contiguous(), a.abs() @ b.abs().t().contiguous()
+    e5m2 = w.dtype == torch.float8_e5m2
+    cut_of = (x.double().abs().clamp(min=2.0 ** -6) * xs.double()[:, torch.arange(k, device="cuda") // 128]) @ \
+        (w.double().abs().clamp(min=2.0 ** -14 if e5m2 else 2.0 ** -6) * wide_scales(ws, layout, n, k)).t().contiguous()
+    half, least, cut = {"bf16": (2.0 ** -8, 0.0, 7 * 2.0 ** -13), "fp16": (2.0 ** -11, 2.0 ** -25, 7 * 2.0 ** -13), "fp32": (0.0, 0.0, 0.0)}[y_dtype]
+    tol = (256 + -(-k // 128) + 4) * 2.0 ** -24 * size + cut * cut_of
+    tol = tol + half * (exact.abs() + tol) + least
+    off = (y.double() - exact).abs()
+    assert bool((off <= tol).all()), f"off by {float((off / tol).max()):.3g} of the bound"
+    return exact, size, off
+
+
+@pytest.mark.parametrize("y_dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("i", range(len(KERNELS)))
+def test_product_of_cancelling_blocks(E, i, y_dtype):
+    """In every eight products two of up to 448 * 448 that cancel, beside six of around 1: FP32 outputs
+    hold the sum, 16-bit ones stay within what their instructions' cut is stated to cost."""
+    m, n, k = KERNELS[i]
+    say(f"  cancelling {m}x{n}x{k} {y_dtype}")
+    g = torch.Generator().manual_seed(300 + i)
+    x, w = torch.randn((m, k), generator=g), torch.randn((n, k), generator=g)
+    big = torch.randint(20, 28, (m, k // 8), generator=g).float() * 16
+    x[:, 0::8] = x[:, 1::8] = big
+    big = torch.randint(20, 28, (n, k // 8), generator=g).float() * 16
+    w[:, 0::8], w[:, 1::8] = big, -big
+    x, w = x.to(torch.float8_e4m3fn).cuda(), w.to(torch.float8_e4m3fn).cuda()
+    xs, ws = torch.ones((m, -(-k // 128)), device="cuda"), torch.ones(n, device="cuda")
+    exact, size, off = check_sums(product_gpu(E, x, xs, w, ws, "row", y_dtype), x, xs, w, ws, "row", y_dtype)
+    assert float(exact.abs().max()) < 2.0 ** -9 * float(size.min())      # the large products do cancel
+    if y_dtype == "fp32":
+        assert float(off.max()) < 2.0 ** -2 * float(exact.abs().max())
+
+
 def test_product_on_another_stream_and_in_a_graph(E):
     """The call orders itself on the stream it is given, and replays from a graph."""
     m, n, k = 24, 640, 1024
