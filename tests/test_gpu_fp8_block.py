@@ -326,6 +326,45 @@ def test_product_of_cancelling_blocks(E, i, y_dtype):
         assert float(off.max()) < 2.0 ** -2 * float(exact.abs().max())
 
 
+@pytest.mark.parametrize("layout", LAYOUTS)
+@pytest.mark.parametrize("i", range(len(KERNELS)))
+def test_product_of_every_kernel(E, i, layout):
+    """Every kernel with both weight types, the three outputs and layouts of scales."""
+    m, n, k = KERNELS[i]
+    for w_kind in ("e4m3", "e5m2"):
+        t = product_inputs(m, n, k, w_kind, layout, 400 + i)
+        for y_dtype in ("bf16", "fp16", "fp32"):
+            say(f"  product {m}x{n}x{k} {w_kind} {layout} {y_dtype}")
+            check_sums(product_gpu(E, *t, layout, y_dtype), *t, layout, y_dtype)
+
+
+@pytest.mark.parametrize("y_dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("i", range(len(KERNELS)))
+def test_product_isolates_and_repeats_in_every_kernel(E, i, y_dtype):
+    """Equal calls give equal bits; a NaN scale or code, or a sum beyond the type, shows in its own row
+    or column of Y alone, at the first and the last of them."""
+    m, n, k = KERNELS[i]
+    say(f"  isolation {m}x{n}x{k} {y_dtype}")
+    x, xs, w, ws = product_inputs(m, n, k, "e4m3", "row_block", 500 + i)
+    clean = product_gpu(E, x, xs, w, ws, "row_block", y_dtype)
+    for _ in range(2):
+        assert torch.equal(clean, product_gpu(E, x, xs, w, ws, "row_block", y_dtype))
+    for row, col in ((0, 0), (m - 1, n - 1), (m // 2, n // 2)):
+        xs2, w2 = xs.clone(), w.clone()
+        xs2[row, -1] = float("nan")
+        w2.view(torch.uint8)[col, k - 1] = 0x7F
+        y = product_gpu(E, x, xs2, w2, ws, "row_block", y_dtype)
+        keep = torch.ones((m, n), dtype=torch.bool, device="cuda")
+        keep[row], keep[:, col] = False, False
+        assert torch.equal(y[keep], clean[keep])
+        assert torch.isnan(y[row]).all() and torch.isnan(y[:, col]).all()
+    # one row of X at the largest codes and a scale that passes the type
+    x2, xs2, w2 = x.clone(), xs.clone(), w.clone()
+    x2[m - 1], xs2[m - 1], w2[:] = 448.0, 3e38 / 448 / 448 / 128, 448.0
+    y = product_gpu(E, x2, xs2, w2, torch.full_like(ws, 1e3), "row_block", y_dtype)
+    assert torch.isinf(y[m - 1]).all() and torch.isfinite(y[: m - 1].float()).all()
+
+
 def test_product_on_another_stream_and_in_a_graph(E):
     """The call orders itself on the stream it is given, and replays from a graph."""
     m, n, k = 24, 640, 1024
