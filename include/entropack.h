@@ -465,7 +465,7 @@ enum ep_scale_layout {
  * w_dtype EP_FP8_E4M3 or EP_FP8_E5M2 (for example the output of ep_decode_tiles),
  * with d_w_scale in layout w_scales; Y: m x n of y_dtype EP_BF16, EP_FP16 or
  * EP_FP32 (round to nearest even; a sum beyond the type's range becomes an
- * infinity).  All row-major; X and W 16-byte aligned.  Every block's sum is scaled
+ * infinity).  All row-major; X and W 16-byte aligned, Y at any element.  Every block's sum is scaled
  * in FP32 and the blocks are added in FP32 in an order fixed by the shape, so equal
  * calls give equal bits.  The output's type chooses how a block is summed:
  *   EP_FP32: FP16 matrix instructions, into which both FP8 types widen exactly, with

@@ -170,6 +170,7 @@ struct Product {
   void* y;
   int64_t m, n, k;
   uint32_t kb;         // blocks of 128 along k
+  uint32_t wide;       // four values of a row of Y from a multiple of four on lie aligned as one store's
 };
 
 // Y's element types: ep_dtype codes as template arguments.
@@ -180,11 +181,11 @@ __device__ __forceinline__ void store_y(void* y, int64_t at, float f) {
   else static_cast<__bf16*>(y)[at] = (__bf16)f;
 }
 
-// Four values of row i from column j on; in one store where n keeps its address aligned.
+// Four values of row i from column j, a multiple of four, on; in one store where it is aligned.
 template <int OUT>
 __device__ __forceinline__ void store_y4(const Product& P, int64_t i, int64_t j, const v4f& v) {
   const int64_t at = i * P.n + j;
-  if (P.n % 4 == 0 && j + 4 <= P.n) {
+  if (P.wide && j + 4 <= P.n) {
     if (OUT == EP_FP32) {
       *reinterpret_cast<v4f*>(static_cast<float*>(P.y) + at) = v;
     } else if (OUT == EP_FP16) {
@@ -717,8 +718,9 @@ extern "C" int ep_gemm_fp8_block(const void* d_x, const float* d_x_scale, const 
   if (hipGetDevice(&dev) != hipSuccess ||
       hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0)
     return ep::fail(EP_ERR_HIP, "ep_gemm_fp8_block: no device");
+  const uintptr_t quad = y_dtype == EP_FP32 ? 16 : 8;
   const ep::Product P = {static_cast<const uint8_t*>(d_x), d_x_scale, static_cast<const uint8_t*>(d_w), d_w_scale,
-                         d_y, m, n, k, (uint32_t)((k + 127) / 128)};
+                         d_y, m, n, k, (uint32_t)((k + 127) / 128), n % 4 == 0 && reinterpret_cast<uintptr_t>(d_y) % quad == 0};
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   if (w_dtype == EP_FP8_E4M3) ep::product_launch<0>(P, w_scales, y_dtype, cus, stream);
   else ep::product_launch<1>(P, w_scales, y_dtype, cus, stream);

@@ -326,6 +326,21 @@ def test_product_of_cancelling_blocks(E, i, y_dtype):
         assert float(off.max()) < 2.0 ** -2 * float(exact.abs().max())
 
 
+@pytest.mark.parametrize("y_dtype", ["bf16", "fp16", "fp32"])
+def test_product_into_an_unaligned_output(E, y_dtype):
+    """Y may begin at any element, also where n is a multiple of four."""
+    dt = {"bf16": torch.bfloat16, "fp16": torch.float16, "fp32": torch.float32}[y_dtype]
+    for m, n, k in ((3, 200, 272), (40, 640, 272), (139, 8224, 336), (387, 4744, 272), (1171, 3356, 272)):
+        x, xs, w, ws = product_inputs(m, n, k, "e4m3", "block", 600)
+        want = product_gpu(E, x, xs, w, ws, "block", y_dtype)
+        for first in (1, 2, 3):
+            y = torch.full((first + m * n + 1,), 5.0, dtype=dt, device="cuda")
+            E.gemm_fp8_block(x.data_ptr(), xs.data_ptr(), w.data_ptr(), ws.data_ptr(), y.data_ptr() + first * y.element_size(), m, n, k,
+                             y_dtype={"bf16": E.BF16, "fp16": E.FP16, "fp32": E.FP32}[y_dtype], stream=stream())
+            torch.cuda.synchronize()
+            assert (y[:first] == 5.0).all() and y[-1] == 5.0 and torch.equal(y[first:-1].view(m, n), want)
+
+
 @pytest.mark.parametrize("layout", LAYOUTS)
 @pytest.mark.parametrize("i", range(len(KERNELS)))
 def test_product_of_every_kernel(E, i, layout):
