@@ -465,9 +465,11 @@ enum ep_scale_layout {
  * w_dtype EP_FP8_E4M3 or EP_FP8_E5M2 (for example the output of ep_decode_tiles),
  * with d_w_scale in layout w_scales; Y: m x n of y_dtype EP_BF16, EP_FP16 or
  * EP_FP32 (round to nearest even; a sum beyond the type's range becomes an
- * infinity).  All row-major; X and W 16-byte aligned, Y at any element.  Every block's sum is scaled
- * in FP32 and the blocks are added in FP32 in an order fixed by the shape, so equal
- * calls give equal bits.  The output's type chooses how a block is summed:
+ * infinity).  All row-major; X and W 16-byte aligned, Y at any element.  Every
+ * block's sum is scaled in FP32 (EP_SCALE_BLOCK: by the FP32 product of the two
+ * scales, which has to stay in that type's range) and the blocks are added in FP32
+ * in an order fixed by the shape, so equal calls give equal bits.  The output's type
+ * chooses how a block is summed:
  *   EP_FP32: FP16 matrix instructions, into which both FP8 types widen exactly, with
  *   FP32 sums; Y is within (256 + ceil(k/128) + 4) 2^-24 of S = sum |xs ws X W|.
  *   EP_BF16, EP_FP16: FP8 matrix instructions, twice as fast, which cut every product
@@ -496,7 +498,7 @@ typedef struct {
   void* d_k;               /* [n_pages][kv_heads][page_tokens][head_dim] codes */
   void* d_v;               /* [n_pages][kv_heads][head_dim][page_tokens] codes */
   float* d_k_scale;        /* [n_pages][kv_heads], not negative */
-  float* d_v_scale;        /* [n_pages][kv_heads] */
+  float* d_v_scale;        /* [n_pages][kv_heads], not negative */
   int64_t n_pages;         /* n_pages * kv_heads at most 2^30 */
   int32_t kv_heads;
   int32_t page_tokens;
@@ -591,7 +593,8 @@ uint64_t ep_kv8_attention_workspace(const ep_kv8_cache* cache, const ep_kv8_attn
  * value scale is rounded to 16 bits where max_q is small (the kernel for few query
  * rows), and else to 11 bits or to within 2^-37 of the largest such product that
  * the row sees, whichever is coarser: a key that counts for less than that in its
- * row may count as 0.  Outputs round to nearest even.
+ * row may count as 0, and so may what is below FP32's normal range.  Outputs round to
+ * nearest even.
  * A value code that is E4M3's not-a-number under a finite scale, which
  * ep_kv8_append never writes, may count as 0.
  * d_workspace: >= ep_kv8_attention_workspace bytes of device memory (nullable if
