@@ -11,8 +11,8 @@ row.  A step of a batch of requests, prompts and single tokens alike, is then
   attention of their queries over the cache            ep_kv8_attention
   the result to E4M3, output projection                ep_quant_fp8_block, ep_gemm_fp8_block
 
-Nothing in a step waits for the GPU or allocates: a step of single tokens is captured into a graph
-and replayed.  The hidden states are random; what comes out is compared with the same layer in
+Nothing in a step waits for the GPU, and its buffers come from torch's pool: a step of single tokens is
+captured into a graph and replayed.  The hidden states are random; what comes out is compared with the same layer in
 32-bit torch operations without any quantisation of activations, keys or values.
 
     python examples/serve_attention_layer.py [--steps N] [--cache e4m3|int8]

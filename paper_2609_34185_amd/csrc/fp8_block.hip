@@ -273,8 +273,9 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, int64_t
 // Few rows of X.  A workgroup owns `height` <= 16 NW rows of W and 16 NX rows of X; its KW waves
 // take blocks of 128 along k in turn, each through NS stages of LDS of its own, and add their sums
 // in the order of the waves at the end.  No wave waits for another before that, and what bounds the
-// kernel is how many bytes a CU has in flight: about 50 GB/s for each CU whatever the shape of the
-// workgroup, so that W is read once by as many CUs as there are.  (Fragments loaded from memory into
+// kernel is what a CU reads, at about 50 GB/s for each whatever the shape of the workgroup: W once by
+// as many CUs as there are, and X again for every strip of W, which of 61 rows is 0.56 of a CU's 1.25
+// MB.  Taller strips over a share of k would read less of X; they are not built.  (Fragments loaded into
 // registers, 16 rows of 64 bytes a load instead of 8 of 128, took 94 us where this takes 28:
 // 61 x 5120 x 17408.)  Measured: 1 x 17408 x 5120 in 15.4 us, 5.8 TB/s of W; 61 x 5120 x 17408 with
 // FP32 outputs in 30 us, 3.0 TB/s.

@@ -497,13 +497,15 @@ __global__ __launch_bounds__(64 * kWaves) void attention_rows_kernel(Attn A, uin
 // where a row's peak follows the largest s + log2 vs among the keys that it sees, whatever the scales
 // of others are: 11 bits down to 2^-26 of the row's largest product of weight and scale, 0 below
 // 2^-37 of it.  (Two BF16 numbers, as in the kernel for few rows, would keep those too, for half as
-// many matrix instructions again.)  The peak moves only when it is passed by more than 3, so that the
-// sums are rarely rescaled and FP16 holds 2^15.  The sum of the weights themselves, which pages of
-// small values and of zeros count in all the same, is kept apart by each lane, at a maximum of its own.
+// many matrix instructions again: 1427 us for 1177, 929 for 744 with 64 channels.)  The peak moves only
+// when it is passed by more than 3, so that the sums are rarely rescaled and FP16 holds 2^15.  The sum
+// of the weights themselves, which pages of small values and of zeros count in all the same, is kept
+// apart by each lane, at a maximum of its own.
 //
-// Bound by the vector unit, which widens codes and makes weights while the matrix unit works for
-// another wave: busy 67 % of the cycles, the matrix unit 35 %.  Two causal prompts of up to 8192
-// tokens, 40 query and 8 kv heads of 128, E4M3: 1040 us, 0.87 PFLOP/s.  Codes widened once for
+// Bound by how little the two units work at once: the vector unit, which widens codes and makes
+// weights, is busy 68 % of the cycles and the matrix unit 35 %, together about all of them.  What is
+// left is to issue a chunk's K Q^T under the exponentials of the one before.  Two causal prompts of up
+// to 8192 tokens, 40 query and 8 kv heads of 128, E4M3: 1055 us, 0.86 PFLOP/s.  Codes widened once for
 // the workgroup and kept in LDS as FP16 take 16 % off the vector unit and are no faster (1104 us for
 // 1109 in one run; 64 channels 793 for 726): LDS then moves twice the bytes.
 constexpr int kPromptWaves = kWaves;
@@ -920,8 +922,10 @@ Plan plan_of(const ep_kv8_cache& c, const ep_kv8_attn& a) {
   const int64_t max_len = std::min(std::max(a.max_len, 1), 1 << 30);   // the last split takes what is past it
   // Up to ten workgroups for a CU of at least 1024 tokens (64 requests of up to 16384 tokens in 5
   // splits: 150 us, in 2 168, in 10 158), but of 256 where that leaves less than four (3 requests
-  // of up to 1999 tokens, 8 kv heads: 11.3 us in 8 splits).  Of few rows, a request's tiles share
-  // what they read and count once.
+  // of up to 1999 tokens, 8 kv heads: 11.3 us in 8 splits, 26.5 in one).  Of few rows, a request's tiles
+  // share what they read and count once.  Of many, partial results cost more the more rows there are:
+  // 512 queries after 15872 tokens, 40 query heads, 306 us in 15 splits, 288 in 8, 319 in 4, 478 in
+  // one; 128 after 16256 100, 108, 137 and 467.
   const int64_t groups = (P.prompt ? P.tiles : a.n_req) * c.kv_heads;
   P.splits = std::min(2560 / groups, std::max(max_len / 1024, std::min(1024 / groups, (max_len + 255) / 256)));
   if (P.counted && !P.prompt) P.splits = std::min(P.splits, kMostGroups / (P.tiles * c.kv_heads));
