@@ -23,7 +23,12 @@
  *     (ep_quant_fp8_block), the FP8 product with such scales
  *     (ep_gemm_fp8_block), and a paged 8-bit key/value cache: its block tables
  *     and slot maps (ep_kv8_slots), its writer (ep_kv8_append) and the
- *     attention that reads it (ep_kv8_attention).
+ *     attention that reads it (ep_kv8_attention),
+ *   - what lies between a layer's products: rotary positions (ep_rope_freqs,
+ *     ep_rope), norms with the residual sum and its gate (ep_norm), the gated
+ *     activation of an MLP (ep_glu), and for decoded INT8 weights the quantiser
+ *     of activations (ep_quant_i8_row) and the product with both scales
+ *     (ep_gemm_i8_scaled).
  *
  * Conventions shared by every entry point:
  *   - Return value: EP_OK (0) or a negative ep_status.  ep_last_error() gives a
@@ -606,6 +611,184 @@ uint64_t ep_kv8_attention_workspace(const ep_kv8_cache* cache, const ep_kv8_attn
  * total_q * q_heads above 2^29, a short workspace), EP_ERR_HIP. */
 int ep_kv8_attention(const ep_kv8_cache* cache, const ep_kv8_attn* call, void* d_workspace,
                      uint64_t ws_bytes, void* hip_stream);
+
+/* ---- INT8 product with scales ---------------------------------------------- */
+/* Activations to INT8 with one FP32 scale for each row.  With amax the row's largest
+ * magnitude:
+ *   scale = fp32(amax * fp32(1 / 127)), or 1 where that is zero;
+ *   q     = round(fp32(x / scale)), halves to even, within +-127.
+ * A row that holds a NaN or an infinity gets a scale that is one (and codes that say
+ * nothing), so that what is made of it does not pass as finite.  d_x: m rows of k
+ * elements (x_dtype EP_BF16, EP_FP16 or EP_FP32), x_row elements from one row to the
+ * next (x_row >= k; 16-byte aligned rows); d_q: m x k codes, row-major, 16-byte
+ * aligned; d_scale: m floats.  m may be 0 (nothing is done).
+ * Asynchronous on hip_stream, no allocation, one launch.
+ * Errors: EP_ERR_ARG (null or misaligned pointers, m outside 0 .. 2^31 - 1, k outside
+ * 1 .. 65536, k % 16, x_row < k, another dtype), EP_ERR_HIP. */
+int ep_quant_i8_row(const void* d_x, int x_dtype, int64_t m, int64_t k, int64_t x_row, int8_t* d_q,
+                    float* d_scale, void* hip_stream);
+
+/* Y[i][j] = xs[i] * ws[j] * sum_p X[i][p] * W[j][p] + bias[j].  X: m x k INT8 with a
+ * scale for each row as ep_quant_i8_row writes them; W: n x k INT8 with a scale for each
+ * row (for example what ep_decode_tiles makes of an INT8 row container, delta_r among
+ * it); d_bias: n floats, or null; Y: m x n of y_dtype EP_BF16, EP_FP16 or EP_FP32.  All
+ * row-major; X and W 16-byte aligned, Y at any element.  The sums are exact in 32-bit
+ * integers; a sum is rounded to FP32, multiplied by xs and then by ws and the bias is
+ * added, each with one FP32 rounding, and the result is rounded once to y_dtype (nearest
+ * even; beyond the type's range an infinity).  Equal calls give equal bits.
+ * d_workspace: >= ep_gemm_i8_scaled_workspace(m, n, k) bytes of device memory owned by
+ * the caller (nullable if that is 0), 16-byte aligned, not shared by calls that overlap:
+ * partial sums of launches that share k out over workgroups.  m may be 0 (nothing is
+ * done).  Asynchronous on hip_stream, no allocation, at most two launches.
+ * Errors: EP_ERR_ARG (null or misaligned pointers, m < 0, n <= 0, k outside 1 .. 131071,
+ * k % 16, m or n above 2^24, another dtype, a short workspace), EP_ERR_HIP. */
+int ep_gemm_i8_scaled(const int8_t* d_x, const float* d_x_scale, const int8_t* d_w,
+                      const float* d_w_scale, const float* d_bias, void* d_y, int y_dtype, int64_t m,
+                      int64_t n, int64_t k, void* d_workspace, uint64_t ws_bytes, void* hip_stream);
+
+/* Device bytes ep_gemm_i8_scaled needs for these sizes on the current device (0 for bad
+ * ones or where no device is present). */
+uint64_t ep_gemm_i8_scaled_workspace(int64_t m, int64_t n, int64_t k);
+
+/* ---- norms, residual sums, gated activations ---------------------------------- */
+enum ep_norm_kind {
+  EP_NORM_NONE = 0,
+  EP_NORM_RMS = 1,         /* v / sqrt(mean(v^2) + eps) */
+  EP_NORM_LAYER = 2        /* (v - mean(v)) / sqrt(mean((v - mean(v))^2) + eps) */
+};
+
+/* One call of ep_norm over m rows of n elements. */
+typedef struct {
+  const void* d_x;         /* rows of x_dtype: a block's output, or its input */
+  const void* d_res;       /* nullable: rows of the residual stream, res_dtype */
+  void* d_res_out;         /* nullable: rows of the new stream h, res_dtype; may be d_res itself */
+  void* d_y;               /* rows of y_dtype (pre other than EP_NORM_NONE, else null) */
+  float* d_y_scale;        /* scales of an 8-bit y, else ignored */
+  const void* d_post_w;    /* n of w_dtype each: weight and bias of the norm of x, nullable */
+  const void* d_post_b;
+  const void* d_gate;      /* vectors of n of w_dtype, nullable; one for each group of rows */
+  const void* d_w;         /* weight and bias of the norm of h, likewise */
+  const void* d_b;
+  int64_t m, n;
+  int64_t x_row, res_row, res_out_row, y_row; /* elements from one row to the next; 0: n */
+  int64_t group_rows;      /* row i takes the gate, w and b of group i / group_rows; 0: group 0 */
+  int64_t gate_ld, w_ld, b_ld; /* elements from one group's vector to the next's; 0: all take one */
+  int32_t x_dtype, res_dtype, w_dtype; /* EP_BF16, EP_FP16 or EP_FP32 */
+  int32_t y_dtype;         /* the same, or EP_FP8_E4M3 or EP_INT8 */
+  int32_t post, pre;       /* ep_norm_kind: of x before the sum, of h after it */
+  int32_t w_plus_one;      /* nonzero: the norm of h is multiplied by 1 + w */
+  float alpha;             /* of what is added to the residual */
+  float eps;               /* above 0 */
+  int32_t reserved;
+} ep_norm_call;
+
+/* The norm after one block, the residual sum and the norm before the next, for each row:
+ *   u = N_post(x) * post_w + post_b   (x itself if post is EP_NORM_NONE)
+ *   h = res + alpha * gate * u        (absent terms and factors left out)
+ *   y = N_pre(h) * w + b              (weights that are null are 1, biases 0)
+ * h is rounded to res_dtype where it is stored, and the norm is of the unrounded one.
+ * y is rounded to y_dtype (16- and 32-bit types; nearest even, beyond the range an
+ * infinity), or quantised, unrounded: EP_FP8_E4M3 with a scale for each 128 of a row
+ * (d_y_scale: m x ceil(n / 128)) as ep_quant_fp8_block with block_rows 1, EP_INT8 with a
+ * scale for each row (d_y_scale: m) as ep_quant_i8_row.  Everything in between is FP32,
+ * sums included; equal calls give equal bits.  A NaN or infinity changes its own row only.
+ * d_y may be d_x itself where their types have one size and their rows one distance.
+ * Rows of x, res, h and y and the vectors are 16-byte aligned.  m may be 0.
+ * Asynchronous on hip_stream, no allocation, one launch.
+ * Errors: EP_ERR_ARG (null or misaligned pointers, m outside 0 .. 2^31 - 1, n outside
+ * 8 .. 65536, n % 8, or n % 16 with an 8-bit y, short or misaligned rows, a negative
+ * group size or distance, another dtype or kind, eps or alpha out of range, nothing to
+ * write), EP_ERR_HIP. */
+int ep_norm(const ep_norm_call* call, void* hip_stream);
+
+enum ep_act {
+  EP_ACT_SILU = 1,         /* a / (1 + exp(-a)) */
+  EP_ACT_GELU = 2,         /* a Phi(a), Phi the normal distribution */
+  EP_ACT_GELU_TANH = 3     /* a (1 + tanh(sqrt(2 / pi) (a + 0.044715 a^3))) / 2 */
+};
+
+/* y = act(a) * b of an MLP's two halves (d_b null: y = act(a)).  d_a, d_b: m rows of n
+ * elements of x_dtype (EP_BF16, EP_FP16 or EP_FP32), a_row and b_row elements from one row
+ * to the next, 16-byte aligned, so that both may lie in one fused projection's output; d_y:
+ * m x n of y_dtype, row-major, 16-byte aligned, as ep_norm's y, with d_y_scale for 8-bit
+ * ones.  Computed in FP32, rounded or quantised once.  m may be 0 (nothing is done).
+ * Asynchronous on hip_stream, no allocation, one launch.
+ * Errors: EP_ERR_ARG (null or misaligned pointers, m outside 0 .. 2^31 - 1, n outside
+ * 8 .. 65536, n % 8, or n % 16 with an 8-bit y, short or misaligned rows, another dtype
+ * or activation), EP_ERR_HIP. */
+int ep_glu(const void* d_a, const void* d_b, int x_dtype, int64_t m, int64_t n, int64_t a_row,
+           int64_t b_row, int act, void* d_y, int y_dtype, float* d_y_scale, void* hip_stream);
+
+/* ---- rotary positions --------------------------------------------------------- */
+/* How frequencies theta_i = base^(-2 i / rot_dim), i < rot_dim / 2, are stretched by
+ * `factor` (>= 1) for positions beyond those a model was trained on. */
+enum ep_rope_stretch {
+  EP_ROPE_PLAIN = 0,       /* theta_i */
+  EP_ROPE_LINEAR = 1,      /* theta_i / factor */
+  EP_ROPE_BASE = 2,        /* base * factor^(rot_dim / (rot_dim - 2)) in place of base */
+  /* the others keep a share s_i: theta_i (s_i + (1 - s_i) / factor) */
+  EP_ROPE_TURNS = 3,       /* t_i = trained_len theta_i / (2 pi) turns over the trained length:
+                              s_i = (t_i - low) / (high - low) within 0 .. 1 */
+  EP_ROPE_INDEX = 4        /* s_i falls with i from 1 to 0 between the pairs that make `high` and
+                              `low` turns: with d(t) = rot_dim ln(trained_len / (2 pi t)) /
+                              (2 ln base), a = max(floor(d(high)), 0), z = min(ceil(d(low)),
+                              rot_dim - 1): s_i = 1 - (i - a) / max(z - a, 0.001) within 0 .. 1 */
+};
+
+/* Frequencies for ep_rope, on the host: freqs[i] = round(2^64 theta_i / (2 pi)), the
+ * fraction of a turn for each position, so that a position times it is the angle modulo
+ * whole turns, without rounding, at any position.  freqs: rot_dim / 2 values, to be copied
+ * to the device.  A caller may make others by the same formula.  trained_len, low and high
+ * are read by the last two kinds only.
+ * Errors: EP_ERR_ARG (null, rot_dim outside 2 .. 1024 or odd, base outside 1 .. 1e18,
+ * factor below 1 or above 1e9, another kind; EP_ROPE_BASE: rot_dim 2; EP_ROPE_TURNS and
+ * EP_ROPE_INDEX: trained_len outside 1 .. 2^31, low <= 0, high <= low or above 1e9, and
+ * for the latter base 1). */
+int ep_rope_freqs(int rot_dim, double base, int stretch, double factor, double trained_len,
+                  double low, double high, uint64_t* freqs);
+
+enum ep_rope_layout {
+  EP_ROPE_HALF = 1,        /* channel i of the rotated part pairs with i + rot_dim / 2 */
+  EP_ROPE_PAIRS = 2        /* channel 2 i with 2 i + 1 */
+};
+
+/* One call of ep_rope. */
+typedef struct {
+  const void* d_q;         /* n_tokens rows of q_heads x head_dim, q_row elements apart */
+  void* d_q_out;           /* the same, q_out_row apart; may be d_q itself (and q_out_row q_row) */
+  const void* d_k;         /* likewise with k_heads, nullable if k_heads is 0 */
+  void* d_k_out;
+  const uint64_t* d_freqs; /* [rot_dim / 2], as ep_rope_freqs gives them */
+  const int32_t* d_pos;    /* [n_tokens] positions (negative ones too), or null: */
+  const int32_t* d_cu;     /* [n_req + 1] and [n_req] as ep_kv8_slots writes them: token t of request */
+  const int32_t* d_len;    /*  b (d_cu[b] <= t < d_cu[b + 1]) is at d_len[b] - d_cu[b + 1] + t */
+  int64_t n_req;
+  int64_t n_tokens;
+  int64_t q_row, q_out_row, k_row, k_out_row; /* 0: packed, heads * head_dim */
+  int32_t q_heads, k_heads, head_dim;
+  int32_t rot_first, rot_dim; /* channels rot_first .. rot_first + rot_dim - 1 of a head are rotated */
+  int32_t layout;          /* ep_rope_layout */
+  int32_t dtype;           /* EP_BF16, EP_FP16 or EP_FP32 */
+  int32_t inverse;         /* nonzero: by the negative angles, which takes gradients back */
+  float amplitude;         /* factor of cosine and sine, usually 1 */
+  int32_t reserved;
+} ep_rope_call;
+
+/* Rotate queries and keys by their positions: with phi_i = position * theta_i, pair i's
+ * values become
+ *   a' = amplitude (a cos phi_i - b sin phi_i),   b' = amplitude (a sin phi_i + b cos phi_i)
+ * (inverse: with -phi_i).  Channels outside the rotated part are copied.  With d_cu, rows
+ * of tokens from d_cu[n_req] on are left as they were.  The angle is exact to 2^-32 of a turn at
+ * every position, cosine and sine are within 2^-22, the rest is FP32 and rounded once
+ * (nearest even).  Inputs and outputs lie at any element; outputs overlap no input but
+ * their own, at the same place.  n_tokens may be 0.
+ * Asynchronous on hip_stream, no allocation, one launch.
+ * Errors: EP_ERR_ARG (null pointers or ones off their elements, n_tokens outside 0 .. 2^31
+ * - 1, n_req outside 1 .. 2^31 - 2 without d_pos, heads outside 1 .. 65536 (0 for keys),
+ * head_dim outside 2 .. 1024, a rotated part that is odd, empty or beyond it, short rows,
+ * another layout or dtype, an output at its input with another distance of rows, amplitude
+ * that is not finite), EP_ERR_HIP. */
+int ep_rope(const ep_rope_call* call, void* hip_stream);
 
 /* ---- errors -------------------------------------------------------------- */
 const char* ep_last_error(void);

@@ -8,6 +8,7 @@
 
 #include "../../include/entropack.h"
 #include "common.h"
+#include "product_tiles.h"
 #include "scaled.h"
 #include "tile_order.h"
 
@@ -24,60 +25,7 @@ typedef __bf16 v4b __attribute__((ext_vector_type(4)));
 typedef uint32_t v2u __attribute__((ext_vector_type(2)));
 typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
-constexpr float kE4m3Max = 448.0f;
-
-// ---- element types -------------------------------------------------------------
-// Eight consecutive elements as floats.
-__device__ __forceinline__ void load8(const Bf16* p, float (&v)[8]) {
-  const v4u w = *reinterpret_cast<const v4u*>(p);
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    v[2 * i] = __uint_as_float(w[i] << 16);
-    v[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
-  }
-}
-__device__ __forceinline__ void load8(const Fp16* p, float (&v)[8]) {
-  typedef _Float16 v8h __attribute__((ext_vector_type(8)));
-  const v8h w = *reinterpret_cast<const v8h*>(p);
-#pragma unroll
-  for (int i = 0; i < 8; i++) v[i] = (float)w[i];
-}
-__device__ __forceinline__ void load8(const float* p, float (&v)[8]) {
-  const v4f a = reinterpret_cast<const v4f*>(p)[0], b = reinterpret_cast<const v4f*>(p)[1];
-#pragma unroll
-  for (int i = 0; i < 4; i++) {
-    v[i] = a[i];
-    v[4 + i] = b[i];
-  }
-}
-
 // ---- quantiser -------------------------------------------------------------------
-// Largest magnitude as bits: the order of the bits of |x| is the order of |x|, an infinity
-// above every finite value and a NaN above that, so neither is lost in a maximum.
-__device__ __forceinline__ uint32_t top_bits(const float (&v)[8]) {
-  uint32_t t = 0;
-#pragma unroll
-  for (int i = 0; i < 8; i++) t = max(t, __float_as_uint(v[i]) & 0x7FFFFFFFu);
-  return t;
-}
-
-__device__ __forceinline__ float scale_of(uint32_t top) {
-  const float s = __uint_as_float(top) * (1.0f / kE4m3Max);
-  return s == 0.0f ? 1.0f : s;
-}
-
-// E4M3(x / s) of eight values.
-__device__ __forceinline__ v2u codes8(const float (&v)[8], const Divider& by) {
-  v2u out;
-#pragma unroll
-  for (int i = 0; i < 2; i++) {
-    int w = __builtin_amdgcn_cvt_pk_fp8_f32(by(v[4 * i]), by(v[4 * i + 1]), 0, false);
-    w = __builtin_amdgcn_cvt_pk_fp8_f32(by(v[4 * i + 2]), by(v[4 * i + 3]), w, true);
-    out[i] = (uint32_t)w;
-  }
-  return out;
-}
-
 constexpr int kQuantThreads = 256;
 constexpr int kLanes = 16;                 // lanes on one 128-column block, eight columns each
 
@@ -106,7 +54,7 @@ __global__ __launch_bounds__(kQuantThreads) void quant_rows_kernel(const T* __re
   uint32_t top = top_bits(v);
 #pragma unroll
   for (int d = 1; d < kLanes; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-  const float s = scale_of(top);
+  const float s = scale_of(top, kE4m3Max);
   if (col < k) *reinterpret_cast<v2u*>(q + row * k + col) = codes8(v, Divider(s, kE4m3Max));
   if (threadIdx.x % kLanes == 0) scale[unit] = s;
 }
@@ -138,7 +86,7 @@ __global__ __launch_bounds__(kQuantThreads) void quant_blocks_kernel(const T* __
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kQuantThreads / 64; w++) top = max(top, wave_top[w]);
-  const float s = scale_of(top);
+  const float s = scale_of(top, kE4m3Max);
   const Divider by(s, kE4m3Max);
 #pragma unroll
   for (int p = 0; p < kPasses; p++)
@@ -172,45 +120,6 @@ struct Product {
   uint32_t kb;         // blocks of 128 along k
   uint32_t wide;       // four values of a row of Y from a multiple of four on lie aligned as one store's
 };
-
-// Y's element types: ep_dtype codes as template arguments.
-template <int OUT>
-__device__ __forceinline__ void store_y(void* y, int64_t at, float f) {
-  if (OUT == EP_FP32) static_cast<float*>(y)[at] = f;
-  else if (OUT == EP_FP16) static_cast<_Float16*>(y)[at] = (_Float16)f;
-  else static_cast<__bf16*>(y)[at] = (__bf16)f;
-}
-
-// Four values of row i from column j, a multiple of four, on; in one store where it is aligned.
-template <int OUT>
-__device__ __forceinline__ void store_y4(const Product& P, int64_t i, int64_t j, const v4f& v) {
-  const int64_t at = i * P.n + j;
-  if (P.wide && j + 4 <= P.n) {
-    if (OUT == EP_FP32) {
-      *reinterpret_cast<v4f*>(static_cast<float*>(P.y) + at) = v;
-    } else if (OUT == EP_FP16) {
-      *reinterpret_cast<v4h*>(static_cast<_Float16*>(P.y) + at) = __builtin_convertvector(v, v4h);
-    } else {
-      *reinterpret_cast<v4b*>(static_cast<__bf16*>(P.y) + at) = __builtin_convertvector(v, v4b);
-    }
-  } else {
-#pragma unroll
-    for (int r = 0; r < 4; r++)
-      if (j + r < P.n) store_y<OUT>(P.y, at + r, v[r]);
-  }
-}
-
-// Workgroup barrier for direct loads: this wave's LDS reads have returned and at most N of its
-// direct loads are still in flight, then s_barrier.  The scheduling barriers keep the compiler
-// from moving LDS accesses across it.
-template <int N>
-__device__ __forceinline__ void stage_barrier() {
-  static_assert(N >= 0 && N < 64, "vmcnt");
-  __builtin_amdgcn_sched_barrier(0);
-  __builtin_amdgcn_s_waitcnt((N & 15) | ((N >> 4) << 14) | (7 << 4));   // vmcnt(N) lgkmcnt(0)
-  __builtin_amdgcn_s_barrier();
-  __builtin_amdgcn_sched_barrier(0);
-}
 
 // One block of 128 of a 16 x 16 tile.  v_mfma_f32_16x16x128_f8f6f4 multiplies 16 rows of W by 16
 // rows of X: lane l supplies 32 bytes of row l mod 16 of both, and gets the products of W rows
@@ -254,22 +163,6 @@ __device__ __forceinline__ v4f block_product(const v8i& w, const v8i& x) {
 }
 
 // ---- product in tiles, operands through LDS --------------------------------------------
-typedef __attribute__((address_space(3))) uint8_t lds_u8;
-
-// LDS rows of 128 bytes: chunk j (16 bytes) of row r lies at place j ^ swz(r).  A 16-byte read is
-// served to 16 lanes at a time, of the first 32 lanes 0-3, 12-15 and 20-27 together and then the
-// others (measured), and is free of conflicts if they meet 16 different columns of a 256-byte bank
-// row.  Where lane l reads chunk q + l / 16 of row l mod 16, rows 0-3 and 12-15 are read at one
-// chunk together with rows 4-11 at the next: with r / 2 as the key, their eight places in either
-// half of the bank row are different.
-__device__ __forceinline__ uint32_t swz(uint32_t r) { return (r >> 1) & 7; }
-
-constexpr uint32_t kOutside = 0x80000000u;   // past the end of every buffer below (2^30 bytes at most), also with a row's offset added
-
-__device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, int64_t bytes) {
-  return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, (int)bytes, 0x00020000);
-}
-
 // Few rows of X.  A workgroup owns `height` <= 16 NW rows of W and 16 NX rows of X; its KW waves
 // take blocks of 128 along k in turn, each through NS stages of LDS of its own, and add their sums
 // in the order of the waves at the end.  No wave waits for another before that, and what bounds the
@@ -403,7 +296,7 @@ __global__ __launch_bounds__(64 * KW) void product_ring_kernel(Product P, uint32
     if (LAYOUT == EP_SCALE_ROW)
 #pragma unroll
       for (int r = 0; r < 4; r++) v[r] *= P.w_scale[min(j + r, P.n - 1)];
-    store_y4<OUT>(P, row, j, v);
+    store_y4<OUT>(P.y, P.n, P.wide, row, j, v);
   }
 }
 
@@ -532,7 +425,7 @@ __device__ __forceinline__ void tile_product(const Product& P, int64_t i0, int64
 #pragma unroll
     for (int t = 0; t < NX; t++) {
       const int64_t row = i0 + 16 * (NX * wx + t) + col;
-      if (row < P.m) store_y4<OUT>(P, row, j, LAYOUT == EP_SCALE_ROW ? acc[i][t] * ws : acc[i][t]);
+      if (row < P.m) store_y4<OUT>(P.y, P.n, P.wide, row, j, LAYOUT == EP_SCALE_ROW ? acc[i][t] * ws : acc[i][t]);
     }
   }
 }
@@ -568,9 +461,6 @@ void tiles_launch(const Product& P, int cus, hipStream_t stream) {
 }
 
 // ---- which kernel -----------------------------------------------------------------------
-// Workgroups of a launch, and how many of them a CU takes in all.
-int64_t rounds(int64_t groups, int cus) { return (groups + cus - 1) / cus; }
-
 // Rows of W for a workgroup of the streaming kernel: the multiple of 8 up to 16 NW that makes the
 // CU with the most work read the fewest rows.
 template <int NW, int NX>

@@ -24,6 +24,10 @@ CONT_DIRECT, CONT_FP8_ROW, CONT_INT8_ROW, CONT_FP8E5M2_ROW, CONT_UINT8_TENSOR = 
 STATUS_PAYLOAD_OVERRUN, STATUS_BAD_FINAL_STATE, STATUS_BAD_END_OFFSET = 1, 2, 4
 STATUS_NO_PAGES, STATUS_TABLE_FULL, STATUS_SLOTS_FULL = 8, 16, 32
 SCALE_BLOCK, SCALE_ROW_BLOCK, SCALE_ROW = 1, 2, 3
+NORM_NONE, NORM_RMS, NORM_LAYER = 0, 1, 2
+ACT_SILU, ACT_GELU, ACT_GELU_TANH = 1, 2, 3
+ROPE_PLAIN, ROPE_LINEAR, ROPE_BASE, ROPE_TURNS, ROPE_INDEX = 0, 1, 2, 3, 4
+ROPE_HALF, ROPE_PAIRS = 1, 2
 
 ITEMSIZE = {BF16: 2, FP16: 2, FP32: 4, FP8_E4M3: 1, INT8: 1, FP8_E5M2: 1, UINT8: 1, COORD2_I32: 4}
 
@@ -96,6 +100,30 @@ class Kv8Attn(C.Structure):
                 ("reserved", C.c_int32)]
 
 
+class NormCall(C.Structure):
+    _fields_ = [("d_x", C.c_void_p), ("d_res", C.c_void_p), ("d_res_out", C.c_void_p),
+                ("d_y", C.c_void_p), ("d_y_scale", C.c_void_p), ("d_post_w", C.c_void_p),
+                ("d_post_b", C.c_void_p), ("d_gate", C.c_void_p), ("d_w", C.c_void_p),
+                ("d_b", C.c_void_p), ("m", C.c_int64), ("n", C.c_int64), ("x_row", C.c_int64),
+                ("res_row", C.c_int64), ("res_out_row", C.c_int64), ("y_row", C.c_int64),
+                ("group_rows", C.c_int64), ("gate_ld", C.c_int64), ("w_ld", C.c_int64),
+                ("b_ld", C.c_int64), ("x_dtype", C.c_int32), ("res_dtype", C.c_int32),
+                ("w_dtype", C.c_int32), ("y_dtype", C.c_int32), ("post", C.c_int32),
+                ("pre", C.c_int32), ("w_plus_one", C.c_int32), ("alpha", C.c_float),
+                ("eps", C.c_float), ("reserved", C.c_int32)]
+
+
+class RopeCall(C.Structure):
+    _fields_ = [("d_q", C.c_void_p), ("d_q_out", C.c_void_p), ("d_k", C.c_void_p),
+                ("d_k_out", C.c_void_p), ("d_freqs", C.c_void_p), ("d_pos", C.c_void_p),
+                ("d_cu", C.c_void_p), ("d_len", C.c_void_p), ("n_req", C.c_int64),
+                ("n_tokens", C.c_int64), ("q_row", C.c_int64), ("q_out_row", C.c_int64),
+                ("k_row", C.c_int64), ("k_out_row", C.c_int64), ("q_heads", C.c_int32),
+                ("k_heads", C.c_int32), ("head_dim", C.c_int32), ("rot_first", C.c_int32),
+                ("rot_dim", C.c_int32), ("layout", C.c_int32), ("dtype", C.c_int32),
+                ("inverse", C.c_int32), ("amplitude", C.c_float), ("reserved", C.c_int32)]
+
+
 class EntroPackError(RuntimeError):
     def __init__(self, code: int, what: str, msg: str):
         super().__init__(f"{what}: status {code}: {msg}")
@@ -152,6 +180,15 @@ def lib():
         L.ep_kv8_attention_workspace.argtypes = [C.POINTER(Kv8Cache), C.POINTER(Kv8Attn)]
         L.ep_kv8_attention_workspace.restype = u64
         L.ep_kv8_attention.argtypes = [C.POINTER(Kv8Cache), C.POINTER(Kv8Attn), vp, u64, vp]
+        L.ep_quant_i8_row.argtypes = [vp, C.c_int, i64, i64, i64, vp, vp, vp]
+        L.ep_gemm_i8_scaled.argtypes = [vp, vp, vp, vp, vp, vp, C.c_int, i64, i64, i64, vp, u64, vp]
+        L.ep_gemm_i8_scaled_workspace.argtypes = [i64, i64, i64]
+        L.ep_gemm_i8_scaled_workspace.restype = u64
+        L.ep_norm.argtypes = [C.POINTER(NormCall), vp]
+        L.ep_glu.argtypes = [vp, vp, C.c_int, i64, i64, i64, i64, C.c_int, vp, C.c_int, vp, vp]
+        L.ep_rope_freqs.argtypes = [C.c_int, C.c_double, C.c_int, C.c_double, C.c_double, C.c_double,
+                                    C.c_double, vp]
+        L.ep_rope.argtypes = [C.POINTER(RopeCall), vp]
         L.ep_last_error.restype = C.c_char_p
         _lib = L
     return _lib
@@ -167,6 +204,8 @@ EXPORTS = ["ep_encode_params_default", "ep_encode_cpu", "ep_encode_gpu", "ep_blo
            "ep_decode_gemm_bf16_prepared",
            "ep_quant_fp8_block", "ep_gemm_fp8_block", "ep_kv8_slots", "ep_kv8_append",
            "ep_kv8_attention_workspace", "ep_kv8_attention",
+           "ep_quant_i8_row", "ep_gemm_i8_scaled", "ep_gemm_i8_scaled_workspace", "ep_norm", "ep_glu",
+           "ep_rope_freqs", "ep_rope",
            "ep_last_error"]
 
 
@@ -412,6 +451,80 @@ def kv8_attention(cache: Kv8Cache, call: Kv8Attn, d_ws: int, ws_bytes: int, stre
     """Attention of call's queries over the cache."""
     _check(lib().ep_kv8_attention(C.byref(cache), C.byref(call), d_ws or None, ws_bytes,
                                   stream or None), "ep_kv8_attention")
+
+
+def quant_i8_row(d_x: int, x_dtype: int, m: int, k: int, d_q: int, d_scale: int,
+                 x_row: int | None = None, stream: int = 0):
+    """X (m x k, rows x_row elements apart) to INT8 codes and an FP32 scale for each row."""
+    _check(lib().ep_quant_i8_row(d_x or None, x_dtype, m, k, k if x_row is None else x_row, d_q or None,
+                                 d_scale or None, stream or None), "ep_quant_i8_row")
+
+
+def gemm_i8_scaled_workspace(m: int, n: int, k: int) -> int:
+    return int(lib().ep_gemm_i8_scaled_workspace(m, n, k))
+
+
+def gemm_i8_scaled(d_x: int, d_x_scale: int, d_w: int, d_w_scale: int, d_y: int, m: int, n: int, k: int,
+                   y_dtype: int = BF16, d_bias: int = 0, d_ws: int = 0, ws_bytes: int = 0, stream: int = 0):
+    """Y (m x n) = X (m x k INT8) times W (n x k INT8) transposed, with a scale for each row of both
+    and an FP32 bias."""
+    _check(lib().ep_gemm_i8_scaled(d_x or None, d_x_scale or None, d_w or None, d_w_scale or None,
+                                   d_bias or None, d_y or None, y_dtype, m, n, k, d_ws or None, ws_bytes,
+                                   stream or None), "ep_gemm_i8_scaled")
+
+
+def norm_call(d_x: int, m: int, n: int, x_dtype: int = BF16, d_res: int = 0, d_res_out: int = 0,
+              res_dtype: int = BF16, d_y: int = 0, y_dtype: int = BF16, d_y_scale: int = 0,
+              post: int = NORM_NONE, d_post_w: int = 0, d_post_b: int = 0, d_gate: int = 0, gate_ld: int = 0,
+              alpha: float = 1.0, pre: int = NORM_RMS, d_w: int = 0, d_b: int = 0, w_ld: int = 0, b_ld: int = 0,
+              w_dtype: int = BF16, group_rows: int = 0, w_plus_one: bool = False, eps: float = 1e-6,
+              x_row: int = 0, res_row: int = 0, res_out_row: int = 0, y_row: int = 0) -> NormCall:
+    """Describe one call of norm: h = res + alpha gate N_post(x), y = N_pre(h).  Rows are n elements
+    apart where their distance is 0."""
+    return NormCall(d_x or None, d_res or None, d_res_out or None, d_y or None, d_y_scale or None,
+                    d_post_w or None, d_post_b or None, d_gate or None, d_w or None, d_b or None, m, n,
+                    x_row, res_row, res_out_row, y_row, group_rows, gate_ld, w_ld, b_ld, x_dtype, res_dtype,
+                    w_dtype, y_dtype, post, pre, int(w_plus_one), alpha, eps, 0)
+
+
+def norm(call: NormCall, stream: int = 0):
+    """The norm after one block, the residual sum and the norm before the next."""
+    _check(lib().ep_norm(C.byref(call), stream or None), "ep_norm")
+
+
+def glu(d_a: int, d_b: int, x_dtype: int, m: int, n: int, act: int, d_y: int, y_dtype: int = BF16,
+        d_y_scale: int = 0, a_row: int | None = None, b_row: int | None = None, stream: int = 0):
+    """Y (m x n) = act(A) * B, or act(A) without B, rounded or quantised."""
+    _check(lib().ep_glu(d_a or None, d_b or None, x_dtype, m, n, n if a_row is None else a_row,
+                        n if b_row is None else b_row, act, d_y or None, y_dtype, d_y_scale or None,
+                        stream or None), "ep_glu")
+
+
+def rope_freqs(rot_dim: int, base: float = 10000.0, stretch: int = ROPE_PLAIN, factor: float = 1.0,
+               trained_len: float = 0.0, low: float = 0.0, high: float = 0.0) -> np.ndarray:
+    """Frequencies of rot_dim / 2 pairs as fractions of a turn in 64 bits (host array, uint64)."""
+    out = np.zeros(max(0, rot_dim // 2), dtype=np.uint64)
+    _check(lib().ep_rope_freqs(rot_dim, base, stretch, factor, trained_len, low, high,
+                               out.ctypes.data_as(C.c_void_p)), "ep_rope_freqs")
+    return out
+
+
+def rope_call(d_q: int, d_q_out: int, d_freqs: int, n_tokens: int, q_heads: int, head_dim: int, dtype: int,
+              d_k: int = 0, d_k_out: int = 0, k_heads: int = 0, rot_dim: int = 0, rot_first: int = 0,
+              layout: int = ROPE_HALF, d_pos: int = 0, d_cu: int = 0, d_len: int = 0, n_req: int = 0,
+              q_row: int = 0, q_out_row: int = 0, k_row: int = 0, k_out_row: int = 0, inverse: bool = False,
+              amplitude: float = 1.0) -> RopeCall:
+    """Describe one rotation of queries and keys (rot_dim 0: whole heads; rows packed where their
+    distance is 0), positions in d_pos or from ep_kv8_slots' d_cu and d_len."""
+    return RopeCall(d_q or None, d_q_out or None, d_k or None, d_k_out or None, d_freqs or None,
+                    d_pos or None, d_cu or None, d_len or None, n_req, n_tokens, q_row, q_out_row, k_row,
+                    k_out_row, q_heads, k_heads, head_dim, rot_first, rot_dim or head_dim, layout, dtype,
+                    int(inverse), amplitude, 0)
+
+
+def rope(call: RopeCall, stream: int = 0):
+    """Rotate call's queries and keys by their positions."""
+    _check(lib().ep_rope(C.byref(call), stream or None), "ep_rope")
 
 
 # ---- torch conveniences (device memory and streams only) ------------------------

@@ -1,0 +1,174 @@
+"""The operators between a layer's products without a GPU: every bad argument is refused on the host,
+before any device call, with EP_ERR_ARG and a message; calls over nothing do nothing (no device
+pointer below is ever dereferenced); the rotary frequencies, which are made on the host, against
+their formulas in 60 decimal digits."""
+import ctypes
+import math
+from decimal import Decimal, getcontext
+
+import numpy as np
+import pytest
+
+A, B, D, F, G, H = (i << 20 for i in range(1, 7))   # aligned addresses
+NAN, INF = float("nan"), float("inf")
+
+
+@pytest.fixture(scope="module")
+def E():
+    import os
+    from paper_2609_34185_amd import entropack
+    if not os.path.exists(entropack.LIB_PATH):
+        from paper_2609_34185_amd import build
+        build.build()
+    return entropack
+
+
+def refused(E, call, *a, **kw):
+    with pytest.raises(E.EntroPackError) as e:
+        call(*a, **kw)
+    assert e.value.code == E.ERR_ARG and str(e.value)
+
+
+def test_struct_sizes_match_the_header(E):
+    """The binding's structs, field by field, as the C declarations lay them out."""
+    assert ctypes.sizeof(E.NormCall) == 10 * 8 + 10 * 8 + 10 * 4
+    assert ctypes.sizeof(E.RopeCall) == 8 * 8 + 6 * 8 + 10 * 4
+
+
+def test_quant_refusals(E):
+    ok = dict(x_dtype=E.BF16, m=4, k=256, d_q=B, d_scale=D)
+    for bad in (dict(m=-1), dict(m=1 << 31), dict(k=0), dict(k=-16), dict(k=24), dict(k=65552), dict(x_row=128), dict(x_row=260),
+                dict(x_row=1 << 60), dict(x_dtype=E.INT8), dict(x_dtype=0), dict(d_q=0), dict(d_scale=0), dict(d_q=B + 8),
+                dict(d_scale=D + 2)):
+        refused(E, E.quant_i8_row, A, **{**ok, **bad})
+    refused(E, E.quant_i8_row, 0, **ok)
+    refused(E, E.quant_i8_row, A + 2, **ok)
+    refused(E, E.quant_i8_row, A, **{**ok, "x_dtype": E.FP32, "x_row": 258})
+    E.quant_i8_row(0, E.BF16, 0, 256, 0, 0)               # no rows: nothing to do
+
+
+def test_product_refusals(E):
+    ok = dict(m=4, n=8, k=256, d_ws=H, ws_bytes=1 << 40)
+    for bad in (dict(m=-1), dict(n=0), dict(k=0), dict(k=24), dict(k=131072), dict(n=1 << 25), dict(m=1 << 25),
+                dict(y_dtype=E.INT8), dict(y_dtype=E.FP8_E4M3), dict(d_bias=F + 2)):
+        refused(E, E.gemm_i8_scaled, A, B, D, F, G, **{**ok, **bad})
+    for i in range(5):
+        p = [A, B, D, F, G]
+        p[i] = 0
+        refused(E, E.gemm_i8_scaled, *p, **ok)
+        p[i] = (A, B, D, F, G)[i] + (8 if i in (0, 2) else 1)
+        refused(E, E.gemm_i8_scaled, *p, **ok)
+    E.gemm_i8_scaled(0, 0, D, F, 0, 0, 8, 256)
+    for bad in ((-1, 8, 256), (4, 0, 256), (4, 8, 24), (4, 8, 131072), (1 << 25, 8, 256), (0, 8, 256)):
+        assert E.gemm_i8_scaled_workspace(*bad) == 0
+
+
+def test_glu_refusals(E):
+    ok = dict(x_dtype=E.BF16, m=4, n=256, act=E.ACT_SILU, d_y=D, y_dtype=E.FP8_E4M3, d_y_scale=F)
+    for bad in (dict(x_dtype=E.INT8), dict(y_dtype=E.FP8_E5M2), dict(y_dtype=0), dict(act=0), dict(act=4), dict(m=-1), dict(m=1 << 31),
+                dict(n=0), dict(n=264), dict(n=65552), dict(n=260, y_dtype=E.BF16), dict(a_row=248), dict(a_row=260), dict(b_row=248),
+                dict(b_row=1 << 60), dict(d_y=0), dict(d_y=D + 8), dict(d_y_scale=0), dict(d_y_scale=F + 2)):
+        refused(E, E.glu, A, B, **{**ok, **bad})
+    refused(E, E.glu, 0, B, **ok)
+    refused(E, E.glu, A + 2, B, **ok)
+    refused(E, E.glu, A, B + 8, **ok)
+    E.glu(0, 0, E.BF16, 0, 256, E.ACT_SILU, 0)
+
+
+def test_norm_refusals(E):
+    ok = dict(d_x=A, m=4, n=256, d_res=B, d_res_out=D, d_y=F, y_dtype=E.FP8_E4M3, d_y_scale=G, d_gate=H, d_w=H, d_b=H, d_post_w=H,
+              d_post_b=H, post=E.NORM_LAYER)
+
+    def call(**kw):
+        E.norm(E.norm_call(**{**ok, **kw}))
+
+    for bad in (dict(post=-1), dict(post=3), dict(pre=-1), dict(pre=3), dict(x_dtype=E.INT8), dict(res_dtype=E.FP8_E4M3), dict(w_dtype=0),
+                dict(y_dtype=E.FP8_E5M2), dict(m=-1), dict(m=1 << 31), dict(n=0), dict(n=-8), dict(n=264), dict(n=252, y_dtype=E.BF16),
+                dict(n=65552), dict(eps=0.0), dict(eps=-1e-6), dict(eps=NAN), dict(eps=INF), dict(alpha=NAN), dict(alpha=INF),
+                dict(x_row=248), dict(x_row=260), dict(res_row=248), dict(res_out_row=252), dict(y_row=264), dict(x_row=1 << 60),
+                dict(group_rows=-1), dict(gate_ld=-8), dict(w_ld=-8), dict(b_ld=4), dict(w_ld=1 << 60), dict(d_x=0), dict(d_y=0),
+                dict(d_y_scale=0), dict(d_y_scale=G + 1), dict(d_x=A + 8), dict(d_res=B + 2), dict(d_res_out=D + 8), dict(d_y=F + 8),
+                dict(d_post_w=H + 2), dict(d_post_b=H + 2), dict(d_gate=H + 2), dict(d_w=H + 2), dict(d_b=H + 4),
+                dict(pre=E.NORM_NONE, d_res_out=0), dict(d_res=D, res_row=512)):
+        refused(E, call, **bad)
+    with pytest.raises(E.EntroPackError):
+        E._check(E.lib().ep_norm(None, None), "ep_norm")
+    E.norm(E.norm_call(0, 0, 256))                        # no rows: nothing to do
+
+
+def test_rope_refusals(E):
+    ok = dict(d_q=A, d_q_out=B, d_freqs=D, n_tokens=5, q_heads=8, head_dim=128, dtype=E.BF16, d_k=F, d_k_out=G, k_heads=2, d_pos=H)
+
+    def call(**kw):
+        E.rope(E.rope_call(**{**ok, **kw}))
+
+    for bad in (dict(dtype=E.INT8), dict(layout=0), dict(layout=3), dict(n_tokens=-1), dict(n_tokens=1 << 31), dict(q_heads=0),
+                dict(q_heads=65537), dict(k_heads=-1), dict(head_dim=1), dict(head_dim=1026), dict(rot_dim=3), dict(rot_dim=130),
+                dict(rot_first=-2), dict(rot_first=2), dict(rot_first=64, rot_dim=66), dict(rot_dim=-2), dict(q_row=1016), dict(q_out_row=1016),
+                dict(k_row=248), dict(k_out_row=255), dict(q_row=1 << 32), dict(amplitude=NAN), dict(amplitude=INF), dict(d_q=0),
+                dict(d_q_out=0), dict(d_freqs=0), dict(d_k=0), dict(d_k_out=0), dict(d_pos=0), dict(d_pos=0, n_req=2),
+                dict(d_pos=0, n_req=2, d_cu=H), dict(d_pos=0, n_req=0, d_cu=H, d_len=H), dict(d_pos=0, n_req=1 << 31, d_cu=H, d_len=H),
+                dict(d_q=A + 1), dict(d_q_out=B + 1), dict(d_k=F + 1), dict(d_k_out=G + 1), dict(d_freqs=D + 4), dict(d_pos=H + 2),
+                dict(dtype=E.FP32, d_q=A + 2), dict(d_q_out=A, q_row=2048), dict(d_k_out=F, k_out_row=512)):
+        refused(E, call, **bad)
+    with pytest.raises(E.EntroPackError):
+        E._check(E.lib().ep_rope(None, None), "ep_rope")
+    call(n_tokens=0)
+    call(n_tokens=0, d_q=0, d_q_out=0, d_k=0, d_k_out=0, d_freqs=0)
+
+
+def test_rope_freqs_refusals(E):
+    ok = dict(rot_dim=64, base=1e4, stretch=E.ROPE_TURNS, factor=4.0, trained_len=4096.0, low=1.0, high=4.0)
+    for bad in (dict(rot_dim=0), dict(rot_dim=3), dict(rot_dim=1026), dict(base=0.5), dict(base=1e19), dict(base=NAN), dict(stretch=-1),
+                dict(stretch=5), dict(factor=0.5), dict(factor=1e10), dict(factor=NAN), dict(trained_len=0.0), dict(trained_len=3e9),
+                dict(trained_len=NAN), dict(low=0.0), dict(low=NAN), dict(high=1.0), dict(high=NAN), dict(high=1e10),
+                dict(stretch=E.ROPE_BASE, rot_dim=2), dict(stretch=E.ROPE_INDEX, base=1.0)):
+        refused(E, E.rope_freqs, **{**ok, **bad})
+    assert E.lib().ep_rope_freqs(64, 1e4, 0, 1.0, 0.0, 0.0, 0.0, None) == E.ERR_ARG
+
+
+PI = Decimal("3.14159265358979323846264338327950288419716939937510582097494")
+
+
+def freqs_by_formula(rot, base, stretch, factor, trained, low, high, kinds):
+    """Turns a position of every pair, by the header's formulas in 60 digits."""
+    plain, linear, by_base, turns, index = kinds
+    getcontext().prec = 60
+    base, factor, trained, low, high = (Decimal(v) for v in (base, factor, trained, low, high))
+    if stretch == by_base:
+        base *= factor ** (Decimal(rot) / (rot - 2))
+    out = []
+    if stretch == index:
+        def place(t):
+            return rot * (trained / (2 * PI * t)).ln() / (2 * base.ln())
+        a, z = max(math.floor(place(high)), 0), min(math.ceil(place(low)), rot - 1)
+    for i in range(rot // 2):
+        theta, keep = base ** (Decimal(-2 * i) / rot), Decimal(1)
+        if stretch == linear:
+            keep = Decimal(0)
+        elif stretch == turns:
+            keep = (trained * theta / (2 * PI) - low) / (high - low)
+        elif stretch == index:
+            keep = 1 - (i - a) / max(Decimal(z - a), Decimal("0.001"))
+        keep = min(max(keep, Decimal(0)), Decimal(1))
+        out.append(theta * (keep + (1 - keep) / factor) / (2 * PI))
+    return out
+
+
+@pytest.mark.parametrize("rot,base,factor,trained,low,high", [
+    (128, 10000.0, 8.0, 8192.0, 1.0, 4.0), (64, 500000.0, 32.0, 2048.0, 0.5, 31.5), (20, 1e6, 1.0, 4096.0, 1.0, 2.0),
+    (4, 10000.0, 40.0, 100.0, 1.0, 32.0), (2, 10.0, 3.0, 9.0, 1.0, 2.0), (256, 1e18, 1e9, 2147483648.0, 1e-3, 1e9)])
+@pytest.mark.parametrize("name", ["PLAIN", "LINEAR", "BASE", "TURNS", "INDEX"])
+def test_rope_freqs(E, name, rot, base, factor, trained, low, high):
+    """Every frequency within 2^-57 of itself and half a unit: computed in 64 bits of mantissa, a power's
+    error is its exponent's rounding times the logarithm (at most ln 1e27 = 63), twice where the base
+    is one too.  A position of 31 bits times that is below 2^-28 of a turn even at a whole radian."""
+    stretch = getattr(E, "ROPE_" + name)
+    if name == "BASE" and rot == 2:
+        pytest.skip("refused")
+    got = E.rope_freqs(rot, base, stretch, factor, trained, low, high)
+    want = freqs_by_formula(rot, base, stretch, factor, trained, low, high, (E.ROPE_PLAIN, E.ROPE_LINEAR, E.ROPE_BASE, E.ROPE_TURNS, E.ROPE_INDEX))
+    assert got.dtype == np.uint64 and len(got) == rot // 2
+    for g, w in zip(got.tolist(), want):
+        w *= 1 << 64
+        assert abs(g - w) <= w * Decimal(2) ** -57 + Decimal("0.5")
