@@ -6,6 +6,7 @@
 #include <algorithm>
 #include <cmath>
 #include <cstdint>
+#include <type_traits>
 
 #include "../../include/entropack.h"
 #include "common.h"
@@ -23,54 +24,86 @@ typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
 constexpr int64_t kMostRow = 65536;   // elements: 1024 threads of eight vectors of eight
 
-// ---- eight elements of a type that is known at run time ----------------------------------
-// Loads do not depend on the type but by its size, so that several rows' loads are in flight
-// before the first one's values are needed.
-struct Raw8 {
-  v4u lo, hi;
+// ---- rows of a type that is known at run time ----------------------------------------------
+// V vectors of eight elements from places `at`, `at` + step, ... of a row of `vecs` of them, as they lie
+// in memory.  All loads go out before the first value is needed: those past the row's end read its
+// last vector, and are not waited for one by one.  A 16-bit vector takes four registers until it is
+// widened.
+template <int V>
+struct RawRow {
+  v4u lo[V], hi[V];   // hi: FP32 only
+  __device__ __forceinline__ void load(const void* row, int dtype, uint32_t at, uint32_t step, uint32_t vecs) {
+    if (dtype == EP_FP32) {
+#pragma unroll
+      for (int j = 0; j < V; j++) {
+        const v4u* const p = static_cast<const v4u*>(row) + 2 * (size_t)min(at + j * step, vecs - 1);
+        lo[j] = p[0];
+        hi[j] = p[1];
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; j++) {
+        lo[j] = static_cast<const v4u*>(row)[min(at + j * step, vecs - 1)];
+        hi[j] = v4u{};
+      }
+    }
+  }
+  // Vector j as floats, 0 past the row's end.
+  __device__ __forceinline__ void get(int j, int dtype, uint32_t at, uint32_t step, uint32_t vecs, float (&v)[8]) const {
+    if (dtype == EP_BF16) {
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        v[2 * i] = __uint_as_float(lo[j][i] << 16);
+        v[2 * i + 1] = __uint_as_float(lo[j][i] & 0xFFFF0000u);
+      }
+    } else if (dtype == EP_FP16) {
+      const v8h h = __builtin_bit_cast(v8h, lo[j]);
+#pragma unroll
+      for (int i = 0; i < 8; i++) v[i] = (float)h[i];
+    } else {
+#pragma unroll
+      for (int i = 0; i < 4; i++) {
+        v[i] = __uint_as_float(lo[j][i]);
+        v[4 + i] = __uint_as_float(hi[j][i]);
+      }
+    }
+    if (at + j * step >= vecs) {
+#pragma unroll
+      for (int i = 0; i < 8; i++) v[i] = 0.0f;
+    }
+  }
 };
-__device__ __forceinline__ Raw8 raw8(const void* row, int dtype, uint32_t vec) {
-  Raw8 r = {};
-  if (dtype == EP_FP32) {
-    const v4u* const p = static_cast<const v4u*>(row) + 2 * (size_t)vec;
-    r.lo = p[0];
-    r.hi = p[1];
-  } else {
-    r.lo = static_cast<const v4u*>(row)[vec];
-  }
-  return r;
-}
-__device__ __forceinline__ void widen8(const Raw8& r, int dtype, float (&v)[8]) {
-  if (dtype == EP_BF16) {
+template <int V>
+__device__ __forceinline__ void load_row(const void* row, int dtype, uint32_t at, uint32_t step, uint32_t vecs, float (&v)[V][8]) {
+  const auto of = [&](auto type) {   // the type's branch once for all vectors
+    constexpr int G = V > 4 ? 4 : V;
 #pragma unroll
-    for (int i = 0; i < 4; i++) {
-      v[2 * i] = __uint_as_float(r.lo[i] << 16);
-      v[2 * i + 1] = __uint_as_float(r.lo[i] & 0xFFFF0000u);
+    for (int g = 0; g < V; g += G) {
+      RawRow<G> raw;
+      raw.load(row, type(), at + g * step, step, vecs);
+#pragma unroll
+      for (int j = 0; j < G; j++) raw.get(j, type(), at + g * step, step, vecs, v[g + j]);
     }
-  } else if (dtype == EP_FP16) {
-    const v8h h = __builtin_bit_cast(v8h, r.lo);
+  };
+  if (dtype == EP_BF16) of(std::integral_constant<int, EP_BF16>{});
+  else if (dtype == EP_FP16) of(std::integral_constant<int, EP_FP16>{});
+  else of(std::integral_constant<int, EP_FP32>{});
+}
+template <int V>
+__device__ __forceinline__ void store_row(void* row, int dtype, uint32_t at, uint32_t step, uint32_t vecs, const float (&v)[V][8]) {
 #pragma unroll
-    for (int i = 0; i < 8; i++) v[i] = (float)h[i];
-  } else {
-#pragma unroll
-    for (int i = 0; i < 4; i++) {
-      v[i] = __uint_as_float(r.lo[i]);
-      v[4 + i] = __uint_as_float(r.hi[i]);
+  for (int j = 0; j < V; j++) {
+    const uint32_t vec = at + j * step;
+    if (vec >= vecs) continue;
+    const v8f f = {v[j][0], v[j][1], v[j][2], v[j][3], v[j][4], v[j][5], v[j][6], v[j][7]};
+    if (dtype == EP_BF16) {
+      static_cast<v8b*>(row)[vec] = __builtin_convertvector(f, v8b);
+    } else if (dtype == EP_FP16) {
+      static_cast<v8h*>(row)[vec] = __builtin_convertvector(f, v8h);
+    } else {
+      static_cast<v4f*>(row)[2 * (size_t)vec] = v4f{f[0], f[1], f[2], f[3]};
+      static_cast<v4f*>(row)[2 * (size_t)vec + 1] = v4f{f[4], f[5], f[6], f[7]};
     }
-  }
-}
-__device__ __forceinline__ void load8(const void* row, int dtype, uint32_t vec, float (&v)[8]) {
-  widen8(raw8(row, dtype, vec), dtype, v);
-}
-__device__ __forceinline__ void store8(void* row, int dtype, uint32_t vec, const float (&v)[8]) {
-  const v8f f = {v[0], v[1], v[2], v[3], v[4], v[5], v[6], v[7]};
-  if (dtype == EP_BF16) {
-    static_cast<v8b*>(row)[vec] = __builtin_convertvector(f, v8b);
-  } else if (dtype == EP_FP16) {
-    static_cast<v8h*>(row)[vec] = __builtin_convertvector(f, v8h);
-  } else {
-    static_cast<v4f*>(row)[2 * (size_t)vec] = v4f{v[0], v[1], v[2], v[3]};
-    static_cast<v4f*>(row)[2 * (size_t)vec + 1] = v4f{v[4], v[5], v[6], v[7]};
   }
 }
 // The row that lies `row` rows of `ld` elements of a type after p.
@@ -81,18 +114,17 @@ __device__ __forceinline__ void* row_at(void* p, int dtype, int64_t row, int64_t
   return static_cast<uint8_t*>(p) + row * ld * (dtype == EP_FP32 ? 4 : 2);
 }
 
-// INT8 round(x / s) of eight values, halves to even.
+// INT8 round(x / s) of eight values, halves to even: added to 1.5 2^23 a quotient of at most 127 (and a
+// rounding) is rounded to a whole number, whose low eight bits are the code.
 __device__ __forceinline__ v2u codes8_i8(const float (&v)[8], const Divider& by) {
   v2u out;
 #pragma unroll
   for (int i = 0; i < 2; i++) {
-    uint32_t w = 0;
+    uint32_t q[4];
 #pragma unroll
-    for (int j = 0; j < 4; j++) {
-      const float q = fminf(fmaxf(rintf(by(v[4 * i + j])), -kI8Max), kI8Max);
-      w |= ((uint32_t)(int)q & 0xFFu) << (8 * j);
-    }
-    out[i] = w;
+    for (int j = 0; j < 4; j++) q[j] = __float_as_uint(by(v[4 * i + j]) + 12582912.0f);
+    const uint32_t lo = __builtin_amdgcn_perm(q[1], q[0], 0x0C0C0400u), hi = __builtin_amdgcn_perm(q[3], q[2], 0x04000C0Cu);
+    out[i] = lo | hi;
   }
   return out;
 }
@@ -106,6 +138,24 @@ struct Sum {
 struct Top {
   __device__ __forceinline__ uint32_t operator()(uint32_t a, uint32_t b) const { return max(a, b); }
 };
+// The reduction over 16 lanes in every one of them: each adds what the lanes 8, 4, 2 and 1 after it
+// hold, by moves inside the vector unit.
+template <int N, typename T>
+__device__ __forceinline__ T rotated(T x) {
+  const int v = __builtin_bit_cast(int, x);
+  return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(v, v, 0x120 + N, 0xF, 0xF, false));
+}
+template <typename T, typename F>
+__device__ __forceinline__ T all16(T x, F f) {
+  x = f(x, rotated<8>(x));
+  x = f(x, rotated<4>(x));
+  x = f(x, rotated<2>(x));
+  return f(x, rotated<1>(x));
+}
+template <typename T>
+__device__ __forceinline__ T lane_of(T x, int lane) {
+  return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, x), lane));
+}
 
 template <int L>
 struct RowThreads {
@@ -118,16 +168,18 @@ struct RowThreads {
   template <typename T, typename F>
   __device__ __forceinline__ T all(T x, F f) {
     static_assert(sizeof(T) == 4, "one word");
-#pragma unroll
-    for (int d = 1; d < (L ? L : 64); d *= 2) x = f(x, __builtin_bit_cast(T, __shfl_xor(__builtin_bit_cast(int, x), d)));
+    x = all16(x, f);
+    if (L == 16) return x;
+    if (L == 32) return f(x, __builtin_bit_cast(T, __shfl_xor(__builtin_bit_cast(int, x), 16)));
+    x = f(f(lane_of(x, 0), lane_of(x, 16)), f(lane_of(x, 32), lane_of(x, 48)));
     if (L) return x;
     uint32_t* const slot = lds + 16 * turn;
     turn ^= 1;
     if (threadIdx.x % 64 == 0) slot[threadIdx.x / 64] = __builtin_bit_cast(uint32_t, x);
     __syncthreads();
-    x = __builtin_bit_cast(T, slot[0]);
-    for (uint32_t w = 1; w < blockDim.x / 64; w++) x = f(x, __builtin_bit_cast(T, slot[w]));
-    return x;
+    // a lane for each wave's; 0 is neutral to both reductions
+    const uint32_t w = threadIdx.x % 16;
+    return all16(__builtin_bit_cast(T, w < blockDim.x / 64 ? slot[w] : 0u), f);
   }
   __device__ __forceinline__ float sum(float x) { return all(x, Sum{}); }
   __device__ __forceinline__ uint32_t top(uint32_t x) { return all(x, Top{}); }
@@ -163,7 +215,7 @@ __device__ __forceinline__ float normed(RowThreads<L>& row, float (&v)[V][8], in
 #pragma unroll
         for (int j = 0; j < V; j++)
 #pragma unroll
-          for (int i = 0; i < 8; i++) v[j][i] -= mean;
+          for (int i = 0; i < 8; i++) v[j][i] = row.at() + j * row.lanes() < vecs ? v[j][i] - mean : 0.0f;
       }
       return 1.0f / __builtin_sqrtf(total / (float)n + eps);
     }
@@ -187,6 +239,10 @@ __device__ __forceinline__ float normed(RowThreads<L>& row, float (&v)[V][8], in
 // Rounds or quantises the row and writes it; vectors at or past `vecs` hold zeros.
 template <int L, int V>
 __device__ __forceinline__ void write_row(RowThreads<L>& row, const float (&v)[V][8], uint32_t vecs, void* y, int dtype, float* scale) {
+  if (dtype != EP_INT8 && dtype != EP_FP8_E4M3) {
+    store_row<V>(y, dtype, row.at(), row.lanes(), vecs, v);
+    return;
+  }
   if (dtype == EP_INT8) {
     uint32_t top = 0;
 #pragma unroll
@@ -202,19 +258,12 @@ __device__ __forceinline__ void write_row(RowThreads<L>& row, const float (&v)[V
     return;
   }
 #pragma unroll
-  for (int j = 0; j < V; j++) {
+  for (int j = 0; j < V; j++) {   // sixteen lanes hold a block of 128
     const uint32_t vec = row.at() + j * row.lanes();
-    if (dtype == EP_FP8_E4M3) {   // sixteen lanes hold a block of 128
-      uint32_t top = top_bits(v[j]);
-#pragma unroll
-      for (int d = 1; d < 16; d *= 2) top = max(top, (uint32_t)__shfl_xor((int)top, d));
-      const float s = scale_of(top, kE4m3Max);
-      if (vec < vecs) {
-        static_cast<v2u*>(y)[vec] = codes8(v[j], Divider(s, kE4m3Max));
-        if (vec % 16 == 0) scale[vec / 16] = s;
-      }
-    } else if (vec < vecs) {
-      store8(y, dtype, vec, v[j]);
+    const float s = scale_of(all16(top_bits(v[j]), Top{}), kE4m3Max);
+    if (vec < vecs) {
+      static_cast<v2u*>(y)[vec] = codes8(v[j], Divider(s, kE4m3Max));
+      if (vec % 16 == 0) scale[vec / 16] = s;
     }
   }
 }
@@ -238,6 +287,30 @@ __device__ __forceinline__ int64_t row_of(uint32_t lanes) {
   return ((int64_t)blockIdx.y * gridDim.x + blockIdx.x) * (blockDim.x / lanes) + threadIdx.x / lanes;
 }
 
+// v = f(v), and v = f(v, row), a few vectors of the row at a time; past its end the row is 0.
+template <int V, typename F>
+__device__ __forceinline__ void each(F f, float (&v)[V][8]) {
+#pragma unroll
+  for (int j = 0; j < V; j++)
+#pragma unroll
+    for (int i = 0; i < 8; i++) v[j][i] = f(v[j][i]);
+}
+template <int V, typename F>
+__device__ __forceinline__ void with_row(F f, const void* row, int dtype, uint32_t at, uint32_t step, uint32_t vecs, float (&v)[V][8]) {
+  constexpr int G = V > 4 ? 2 : V;
+#pragma unroll
+  for (int g = 0; g < V; g += G) {
+    float t[G][8];
+    load_row<G>(row, dtype, at + g * step, step, vecs, t);
+#pragma unroll
+    for (int j = 0; j < G; j++)
+      if (g + j < V) {
+#pragma unroll
+        for (int i = 0; i < 8; i++) v[g + j][i] = f(v[g + j][i], t[j][i]);
+      }
+  }
+}
+
 // ---- norm ----------------------------------------------------------------------------------
 template <int L, int V>
 __global__ __launch_bounds__(L ? 256 : 1024) void norm_kernel(ep_norm_call C) {
@@ -253,141 +326,141 @@ __global__ __launch_bounds__(L ? 256 : 1024) void norm_kernel(ep_norm_call C) {
   const void* const w = C.d_w ? row_at(C.d_w, C.w_dtype, group, C.w_ld) : nullptr;
   const void* const b = C.d_b ? row_at(C.d_b, C.w_dtype, group, C.b_ld) : nullptr;
 
+  const uint32_t at = row.at(), step = row.lanes();
   float v[V][8];
-#pragma unroll
-  for (int j = 0; j < V; j++) {
-    const uint32_t vec = row.at() + j * row.lanes();
-#pragma unroll
-    for (int e = 0; e < 8; e++) v[j][e] = 0.0f;
-    if (vec < vecs) load8(x, C.x_dtype, vec, v[j]);
-  }
+  load_row<V>(x, C.x_dtype, at, step, vecs, v);
   if (C.post != EP_NORM_NONE) {
     const float r = normed<L, V>(row, v, C.post, vecs, n, C.eps);
-#pragma unroll
-    for (int j = 0; j < V; j++) {
-      const uint32_t vec = row.at() + j * row.lanes();
-      if (vec >= vecs) continue;
-      float f[8];
-#pragma unroll
-      for (int e = 0; e < 8; e++) v[j][e] *= r;
-      if (C.d_post_w) {
-        load8(C.d_post_w, C.w_dtype, vec, f);
-#pragma unroll
-        for (int e = 0; e < 8; e++) v[j][e] *= f[e];
-      }
-      if (C.d_post_b) {
-        load8(C.d_post_b, C.w_dtype, vec, f);
-#pragma unroll
-        for (int e = 0; e < 8; e++) v[j][e] += f[e];
-      }
-    }
+    each<V>([&](float a) { return a * r; }, v);
+    if (C.d_post_w) with_row<V>([](float a, float f) { return a * f; }, C.d_post_w, C.w_dtype, at, step, vecs, v);
+    if (C.d_post_b) with_row<V>([](float a, float f) { return a + f; }, C.d_post_b, C.w_dtype, at, step, vecs, v);
   }
-#pragma unroll
-  for (int j = 0; j < V; j++) {
-    const uint32_t vec = row.at() + j * row.lanes();
-    if (vec >= vecs) {
-#pragma unroll
-      for (int e = 0; e < 8; e++) v[j][e] = 0.0f;
-      continue;
-    }
-    float f[8];
-    if (gate) {
-      load8(gate, C.w_dtype, vec, f);
-#pragma unroll
-      for (int e = 0; e < 8; e++) v[j][e] *= f[e];
-    }
-    if (res) {
-      load8(res, C.res_dtype, vec, f);
-#pragma unroll
-      for (int e = 0; e < 8; e++) v[j][e] = __builtin_fmaf(C.alpha, v[j][e], f[e]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; e++) v[j][e] *= C.alpha;
-    }
-    if (C.d_res_out) store8(row_at(C.d_res_out, C.res_dtype, i, C.res_out_row), C.res_dtype, vec, v[j]);
-  }
+  if (gate) with_row<V>([](float a, float f) { return a * f; }, gate, C.w_dtype, at, step, vecs, v);
+  const float alpha = C.alpha;
+  if (res) with_row<V>([=](float a, float f) { return __builtin_fmaf(alpha, a, f); }, res, C.res_dtype, at, step, vecs, v);
+  else each<V>([=](float a) { return alpha * a; }, v);
+  if (C.d_res_out) store_row<V>(row_at(C.d_res_out, C.res_dtype, i, C.res_out_row), C.res_dtype, at, step, vecs, v);
   if (C.pre == EP_NORM_NONE) return;
   const float r = normed<L, V>(row, v, C.pre, vecs, n, C.eps);
-#pragma unroll
-  for (int j = 0; j < V; j++) {
-    const uint32_t vec = row.at() + j * row.lanes();
-    if (vec >= vecs) {
-#pragma unroll
-      for (int e = 0; e < 8; e++) v[j][e] = 0.0f;
-      continue;
-    }
-    float f[8], a[8] = {};
-    if (b) load8(b, C.w_dtype, vec, a);
-    if (w) {
-      load8(w, C.w_dtype, vec, f);
-      if (C.w_plus_one) {
-#pragma unroll
-        for (int e = 0; e < 8; e++) f[e] += 1.0f;
-      }
-#pragma unroll
-      for (int e = 0; e < 8; e++) v[j][e] = __builtin_fmaf(v[j][e] * r, f[e], a[e]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; e++) v[j][e] = __builtin_fmaf(v[j][e], r, a[e]);
-    }
-  }
+  each<V>([=](float a) { return a * r; }, v);
+  const float one = C.w_plus_one ? 1.0f : 0.0f;
+  if (w) with_row<V>([=](float a, float f) { return a * (f + one); }, w, C.w_dtype, at, step, vecs, v);
+  if (b) with_row<V>([](float a, float f) { return a + f; }, b, C.w_dtype, at, step, vecs, v);
   const RowOut out = {C.d_y, C.d_y_scale, C.y_row, C.y_dtype, n};
   write_row<L, V>(row, v, vecs, out.row(i), C.y_dtype, out.scale_row(i));
 }
 
 // ---- activation and quantiser -----------------------------------------------------------------
+// exp(x) for x <= 0: 2^n 2^f with n the whole number nearest to x log2(e) and f what is left of it, in
+// two parts of log2(e) so that no bit of the product is lost; results fall to 0 through the
+// subnormal values, and are 0 long before -150.
+__device__ __forceinline__ float exp_negative(float x) {
+  x = fmaxf(x, -150.0f);
+  const float n = rintf(x * 1.44269504f);
+  const float f = __builtin_fmaf(x, 1.925963033e-8f, __builtin_fmaf(x, 1.44269502f, -n));
+  return __builtin_ldexpf(__builtin_amdgcn_exp2f(f), (int)n);
+}
+// a / (1 + exp(-z)), by the exponential that does not overflow.  The quotient by one step of Newton's
+// on the instruction's reciprocal, which is within a unit.
+__device__ __forceinline__ float gated(float a, float z) {
+  const float e = exp_negative(-fabsf(z)), d = 1.0f + e;
+  float r = __builtin_amdgcn_rcpf(d);
+  r = __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r);
+  return (z < 0.0f ? a * e : a) * r;
+}
+__device__ __forceinline__ float gelu(float a) { return 0.5f * a * erfcf(-0.70710678118654752f * a); }
+// (1 + tanh z) / 2 is 1 / (1 + exp(-2 z))
+__device__ __forceinline__ float gelu_tanh(float a) { return gated(a, 1.5957691216057308f * __builtin_fmaf(0.044715f * a * a, a, a)); }
+
+
 struct ActCall {
   const void* a;
-  const void* b;   // nullable
+  const void* b;
   int64_t m, a_row, b_row;
-  int x_dtype, act;
+  int act;         // 0: none
   RowOut out;
 };
 
-constexpr int kActNone = 0;
-
-// a / (1 + exp(-z)), by the exponential that does not overflow: far out on the negative side it falls
-// to 0 through FP32's subnormal values.
-__device__ __forceinline__ float gated(float a, float z) {
-  const float e = expf(-fabsf(z));
-  return (z < 0.0f ? a * e : a) / (1.0f + e);
-}
-__device__ __forceinline__ float activated(float a, int act) {
-  if (act == EP_ACT_SILU) return gated(a, a);
-  if (act == EP_ACT_GELU) return 0.5f * a * erfcf(-0.70710678118654752f * a);
-  // (1 + tanh z) / 2 is 1 / (1 + exp(-2 z))
-  return gated(a, 1.5957691216057308f * __builtin_fmaf(0.044715f * a * a, a, a));
+__device__ __forceinline__ void activate(int act, float (&v)[8]) {
+#pragma unroll
+  for (int i = 0; i < 8; i++) {
+    if (act == EP_ACT_SILU) v[i] = gated(v[i], v[i]);
+    else if (act == EP_ACT_GELU) v[i] = gelu(v[i]);
+    else if (act == EP_ACT_GELU_TANH) v[i] = gelu_tanh(v[i]);
+  }
 }
 
-template <int L, int V>
-__global__ __launch_bounds__(L ? 256 : 1024) void act_kernel(ActCall C) {
+// INT8 rows: the whole row is in registers until its largest value is known.
+template <int L, int V, int TYPE, bool GATED>
+__global__ __launch_bounds__(L ? 256 : 1024) void act_rows_kernel(ActCall C) {
   __shared__ uint32_t lds[32];
   RowThreads<L> row(lds);
   const int64_t i = row_of(row.lanes());
   if (i >= C.m) return;
-  const uint32_t vecs = C.out.n / 8;
-  const void* const a = row_at(C.a, C.x_dtype, i, C.a_row);
-  const void* const b = C.b ? row_at(C.b, C.x_dtype, i, C.b_row) : nullptr;
+  const uint32_t vecs = C.out.n / 8, at = row.at(), step = row.lanes();
+  RawRow<V> a, b;
+  a.load(row_at(C.a, TYPE, i, C.a_row), TYPE, at, step, vecs);
+  if (GATED) b.load(row_at(C.b, TYPE, i, C.b_row), TYPE, at, step, vecs);
   float v[V][8];
 #pragma unroll
   for (int j = 0; j < V; j++) {
-    const uint32_t vec = row.at() + j * row.lanes();
-#pragma unroll
-    for (int e = 0; e < 8; e++) v[j][e] = 0.0f;
-    if (vec >= vecs) continue;
-    load8(a, C.x_dtype, vec, v[j]);
-    if (C.act != kActNone) {
-#pragma unroll
-      for (int e = 0; e < 8; e++) v[j][e] = activated(v[j][e], C.act);
-    }
-    if (b) {
+    a.get(j, TYPE, at, step, vecs, v[j]);
+    activate(C.act, v[j]);
+    if (GATED) {
       float f[8];
-      load8(b, C.x_dtype, vec, f);
+      b.get(j, TYPE, at, step, vecs, f);
 #pragma unroll
       for (int e = 0; e < 8; e++) v[j][e] *= f[e];
     }
   }
-  write_row<L, V>(row, v, vecs, C.out.row(i), C.out.dtype, C.out.scale_row(i));
+  write_row<L, V>(row, v, vecs, C.out.row(i), EP_INT8, C.out.scale_row(i));
+}
+
+// Other outputs, where no more than 128 of a row's values belong together: the rows' vectors one after
+// the other, each row padded to whole blocks, V of them for a thread.
+constexpr int kFlatThreads = 256;
+template <int V, int TYPE, bool GATED>
+__global__ __launch_bounds__(kFlatThreads) void act_flat_kernel(ActCall C) {
+  const uint32_t vecs = C.out.n / 8, padded = (vecs + 15) / 16 * 16;
+  const uint64_t first = ((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * (V * kFlatThreads);
+  const int64_t row0 = (int64_t)(first / padded);
+  const uint32_t in0 = (uint32_t)(first - (uint64_t)row0 * padded);
+  const float inverse = 1.0f / (float)padded;
+  RawRow<1> a[V], b[V];
+  int64_t row[V];
+  uint32_t vec[V];
+#pragma unroll
+  for (int j = 0; j < V; j++) {
+    const uint32_t x = in0 + threadIdx.x + j * kFlatThreads;
+    const uint32_t r = (uint32_t)(((float)x + 0.5f) * inverse);   // x / padded: x is below 2^14, half a unit decides
+    row[j] = row0 + r;
+    vec[j] = x - r * padded;
+    const int64_t i = min(row[j], C.m - 1);   // past the end the last row is read for nothing
+    a[j].load(row_at(C.a, TYPE, i, C.a_row), TYPE, vec[j], 16, vecs);
+    if (GATED) b[j].load(row_at(C.b, TYPE, i, C.b_row), TYPE, vec[j], 16, vecs);
+  }
+#pragma unroll
+  for (int j = 0; j < V; j++) {
+    float v[1][8];
+    a[j].get(0, TYPE, vec[j], 16, vecs, v[0]);
+    activate(C.act, v[0]);
+    if (GATED) {
+      float f[8];
+      b[j].get(0, TYPE, vec[j], 16, vecs, f);
+#pragma unroll
+      for (int e = 0; e < 8; e++) v[0][e] *= f[e];
+    }
+    const bool mine = row[j] < C.m && vec[j] < vecs;
+    if (C.out.dtype == EP_FP8_E4M3) {
+      const float s = scale_of(all16(top_bits(v[0]), Top{}), kE4m3Max);
+      if (mine) {
+        static_cast<v2u*>(C.out.row(row[j]))[vec[j]] = codes8(v[0], Divider(s, kE4m3Max));
+        if (vec[j] % 16 == 0) C.out.scale_row(row[j])[vec[j] / 16] = s;
+      }
+    } else if (mine) {
+      store_row<1>(C.out.row(row[j]), C.out.dtype, vec[j], 16, vecs, v);
+    }
+  }
 }
 
 // ---- launches --------------------------------------------------------------------------------
@@ -395,12 +468,16 @@ struct Shape {
   int lanes, vectors;   // of a row; lanes 0: a workgroup of `threads`
   int threads;
 };
+// Two vectors a thread where a row has enough of them: one leaves each thread too little in flight
+// (8192 x 5120 with both norms in 94 us, 64 with two, 64 and 65 with four and three), and eight leave
+// too few threads on a CU; longer rows take three (8192 x 17408 to INT8 in 75 us, 86 with four) and
+// more only where 1024 threads do not hold them else.
 Shape shape_of(int64_t n) {
   const int64_t vecs = n / 8;
   if (vecs <= 16) return {16, 1, 256};
   if (vecs <= 32) return {32, 1, 256};
   if (vecs <= 64) return {64, 1, 256};
-  const int v = vecs <= 1024 ? 1 : vecs <= 2048 ? 2 : vecs <= 4096 ? 4 : 8;
+  const int v = vecs <= 2048 ? 2 : vecs <= 3072 ? 3 : vecs <= 4096 ? 4 : 8;
   return {0, v, (int)(((vecs + v - 1) / v + 63) / 64 * 64)};
 }
 // Workgroups in one or more rows of a grid, whose x dimension holds fewer than 2^32 threads.
@@ -410,22 +487,42 @@ dim3 row_grid(int64_t m, const Shape& s) {
   return dim3((uint32_t)x, (uint32_t)((groups + x - 1) / x));
 }
 
-#define EP_ROW_LAUNCH(kernel, L, V, call) hipLaunchKernelGGL((kernel<L, V>), grid, dim3(s.threads), 0, stream, call)
-#define EP_ROW_LAUNCHES(kernel, call)                           \
-  do {                                                          \
-    if (s.lanes == 16) EP_ROW_LAUNCH(kernel, 16, 1, call);      \
-    else if (s.lanes == 32) EP_ROW_LAUNCH(kernel, 32, 1, call); \
-    else if (s.lanes == 64) EP_ROW_LAUNCH(kernel, 64, 1, call); \
-    else if (s.vectors == 1) EP_ROW_LAUNCH(kernel, 0, 1, call); \
-    else if (s.vectors == 2) EP_ROW_LAUNCH(kernel, 0, 2, call); \
-    else if (s.vectors == 4) EP_ROW_LAUNCH(kernel, 0, 4, call); \
-    else EP_ROW_LAUNCH(kernel, 0, 8, call);                     \
-  } while (0)
+// f<L, V>() for the row's shape.
+template <typename F>
+void by_shape(const Shape& s, F f) {
+  using std::integral_constant;
+#define EP_SHAPE_CASE(L, V) \
+  if (s.lanes == L && s.vectors == V) return f(integral_constant<int, L>{}, integral_constant<int, V>{})
+  EP_SHAPE_CASE(16, 1);
+  EP_SHAPE_CASE(32, 1);
+  EP_SHAPE_CASE(64, 1);
+  EP_SHAPE_CASE(0, 2);
+  EP_SHAPE_CASE(0, 3);
+  EP_SHAPE_CASE(0, 4);
+  EP_SHAPE_CASE(0, 8);
+#undef EP_SHAPE_CASE
+}
 
+template <int TYPE, bool GATED>
 void act_launch(const ActCall& C, hipStream_t stream) {
-  const Shape s = shape_of(C.out.n);
-  const dim3 grid = row_grid(C.m, s);
-  EP_ROW_LAUNCHES(act_kernel, C);
+  if (C.out.dtype == EP_INT8) {
+    const Shape s = shape_of(C.out.n);
+    by_shape(s, [&](auto l, auto v) {
+      hipLaunchKernelGGL((act_rows_kernel<l(), v(), TYPE, GATED>), row_grid(C.m, s), dim3(s.threads), 0, stream, C);
+    });
+    return;
+  }
+  constexpr int kVectors = 2;
+  const int64_t vectors = C.m * ((C.out.n + 127) / 128 * 16), groups = (vectors + kVectors * kFlatThreads - 1) / (kVectors * kFlatThreads);
+  const int64_t x = std::min<int64_t>(groups, 1 << 23);
+  hipLaunchKernelGGL((act_flat_kernel<kVectors, TYPE, GATED>), dim3((uint32_t)x, (uint32_t)((groups + x - 1) / x)), dim3(kFlatThreads), 0,
+                     stream, C);
+}
+template <bool GATED>
+void act_launch(const ActCall& C, int x_dtype, hipStream_t stream) {
+  if (x_dtype == EP_BF16) act_launch<EP_BF16, GATED>(C, stream);
+  else if (x_dtype == EP_FP16) act_launch<EP_FP16, GATED>(C, stream);
+  else act_launch<EP_FP32, GATED>(C, stream);
 }
 
 bool misaligned(const void* p) { return reinterpret_cast<uintptr_t>(p) & 15; }
@@ -450,8 +547,8 @@ extern "C" int ep_quant_i8_row(const void* d_x, int x_dtype, int64_t m, int64_t 
   if (!d_x || !d_q || !d_scale) return fail(EP_ERR_ARG, "ep_quant_i8_row: null pointer");
   if (misaligned(d_x) || misaligned(d_q) || reinterpret_cast<uintptr_t>(d_scale) & 3)
     return fail(EP_ERR_ARG, "ep_quant_i8_row: x and q must be 16-byte aligned, scale by its elements");
-  const ActCall C = {d_x, nullptr, m, x_row, 0, x_dtype, kActNone, {d_q, d_scale, k, EP_INT8, (uint32_t)k}};
-  act_launch(C, static_cast<hipStream_t>(hip_stream));
+  const ActCall C = {d_x, nullptr, m, x_row, 0, 0, {d_q, d_scale, k, EP_INT8, (uint32_t)k}};
+  act_launch<false>(C, x_dtype, static_cast<hipStream_t>(hip_stream));
   if (hipGetLastError() != hipSuccess) return fail(EP_ERR_HIP, "ep_quant_i8_row: launch failed");
   return EP_OK;
 }
@@ -471,8 +568,9 @@ extern "C" int ep_glu(const void* d_a, const void* d_b, int x_dtype, int64_t m, 
   if (!d_a || !d_y || (codes && !d_y_scale)) return fail(EP_ERR_ARG, "ep_glu: null pointer");
   if (misaligned(d_a) || misaligned(d_b) || misaligned(d_y) || (codes && reinterpret_cast<uintptr_t>(d_y_scale) & 3))
     return fail(EP_ERR_ARG, "ep_glu: a, b and y must be 16-byte aligned, scales by their elements");
-  const ActCall C = {d_a, d_b, m, a_row, b_row, x_dtype, act, {d_y, d_y_scale, n, y_dtype, (uint32_t)n}};
-  act_launch(C, static_cast<hipStream_t>(hip_stream));
+  const ActCall C = {d_a, d_b, m, a_row, b_row, act, {d_y, d_y_scale, n, y_dtype, (uint32_t)n}};
+  if (d_b) act_launch<true>(C, x_dtype, static_cast<hipStream_t>(hip_stream));
+  else act_launch<false>(C, x_dtype, static_cast<hipStream_t>(hip_stream));
   if (hipGetLastError() != hipSuccess) return fail(EP_ERR_HIP, "ep_glu: launch failed");
   return EP_OK;
 }
@@ -516,9 +614,8 @@ extern "C" int ep_norm(const ep_norm_call* call, void* hip_stream) {
   if (normed && codes && reinterpret_cast<uintptr_t>(C.d_y_scale) & 3)
     return fail(EP_ERR_ARG, "ep_norm: scales must be aligned by their elements");
   const Shape s = shape_of(C.n);
-  const dim3 grid = row_grid(C.m, s);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  EP_ROW_LAUNCHES(norm_kernel, C);
+  by_shape(s, [&](auto l, auto v) { hipLaunchKernelGGL((norm_kernel<l(), v()>), row_grid(C.m, s), dim3(s.threads), 0, stream, C); });
   if (hipGetLastError() != hipSuccess) return fail(EP_ERR_HIP, "ep_norm: launch failed");
   return EP_OK;
 }
