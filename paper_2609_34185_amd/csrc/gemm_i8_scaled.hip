@@ -7,6 +7,7 @@
 
 #include "../../include/entropack.h"
 #include "common.h"
+#include "i8_tile.h"
 #include "product_tiles.h"
 #include "tile_order.h"
 
@@ -14,7 +15,10 @@ namespace ep {
 namespace {
 
 typedef int v4i __attribute__((ext_vector_type(4)));
+typedef uint32_t v2u __attribute__((ext_vector_type(2)));
+typedef uint32_t v4u __attribute__((ext_vector_type(4)));
 
+// A launch's operands and, where it shares k out over workgroups, the sums that it leaves for another.
 struct Product {
   const uint8_t* x;
   const float* x_scale;
@@ -25,21 +29,104 @@ struct Product {
   int64_t m, n, k;
   uint32_t kb;         // steps of 128 along k
   uint32_t wide;       // four values of a row of Y from a multiple of four on lie aligned as one store's
+  uint32_t lines;      // every 16 bytes of a row of Y from a multiple of 16 on lie aligned inside it
+  int32_t* sums;       // [parts][m][sums_ld], or null: one part, which writes Y
+  int64_t sums_ld;     // n, rounded up to a multiple of 4
+  uint32_t parts, part_steps;   // of k, and the steps of 128 of each
 };
 
-// Scales, bias and the rounding to Y's type of four sums of row i (below m) from column j on.
+// What a tile's sums become: Y's element types by their ep_dtype codes, or the sums themselves.
+constexpr int kSums = 0;
+template <int OUT>
+constexpr int kSize = OUT == EP_BF16 || OUT == EP_FP16 ? 2 : 4;
+
+// Four values of row i (below m) from column j, a multiple of four below n, on.
+template <int OUT>
+__device__ __forceinline__ v4f scaled(const v4i& sum, float xs, const v4f& ws, const v4f& bias) {
+  v4f v;
+#pragma unroll
+  for (int r = 0; r < 4; r++) v[r] = (float)sum[r] * xs * ws[r] + bias[r];
+  return v;
+}
 template <int OUT>
 __device__ __forceinline__ void finish(const Product& P, int64_t i, int64_t j, const v4i& sum) {
-  const float xs = P.x_scale[i];
-  v4f v;
+  v4f ws, bias = {};
 #pragma unroll
   for (int r = 0; r < 4; r++) {
     const int64_t c = min(j + r, P.n - 1);
-    v[r] = (float)sum[r] * xs * P.w_scale[c];
-    if (P.bias) v[r] += P.bias[c];
+    ws[r] = P.w_scale[c];
+    if (P.bias) bias[r] = P.bias[c];
   }
-  store_y4<OUT>(P.y, P.n, P.wide, i, j, v);
+  store_y4<OUT>(P.y, P.n, P.wide, i, j, scaled<OUT>(sum, P.x_scale[i], ws, bias));
 }
+
+// The scales and biases of a tile's `count` columns of Y from j0 on, in LDS that nothing else uses any more
+// or yet; all threads of the workgroup take part.
+template <int OUT>
+__device__ __forceinline__ void stage_scales(const Product& P, int64_t j0, int count, lds_u8* lds) {
+  __attribute__((address_space(3))) float* const to = (__attribute__((address_space(3))) float*)lds;
+  __syncthreads();
+  if (OUT != kSums)
+    for (int c = threadIdx.x; c < count; c += blockDim.x) {
+      const int64_t j = min(j0 + c, P.n - 1);
+      to[c] = P.w_scale[j];
+      to[count + c] = P.bias ? P.bias[j] : 0.0f;
+    }
+  __syncthreads();
+}
+
+// A wave's ROWS x COLS block of Y goes through LDS of its own, so that its stores are whole lines of rows
+// instead of the pieces of 8 or 16 bytes that a lane holds.  Rows there are padded by 16 bytes.
+template <int OUT, int ROWS, int COLS>
+struct Block {
+  static constexpr int kPitch = COLS * kSize<OUT> + 16, kBytes = ROWS * kPitch;
+  lds_u8* lds;
+  // four values of a row from column c, a multiple of four, on
+  __device__ __forceinline__ void put(int row, int c, const v4i& sum, float xs, const v4f& ws, const v4f& bias) const {
+    typedef __attribute__((address_space(3))) v2u* two;
+    typedef __attribute__((address_space(3))) v4u* four;
+    lds_u8* const at = lds + row * kPitch + c * kSize<OUT>;
+    if (OUT == kSums) {
+      *(four)at = __builtin_bit_cast(v4u, sum);
+      return;
+    }
+    const v4f v = scaled<OUT>(sum, xs, ws, bias);
+    if (OUT == EP_FP32) *(four)at = __builtin_bit_cast(v4u, v);
+    else if (OUT == EP_FP16) *(two)at = __builtin_bit_cast(v2u, __builtin_convertvector(v, v4h));
+    else *(two)at = __builtin_bit_cast(v2u, __builtin_convertvector(v, v4b));
+  }
+  // the block's rows below m and columns below n to row i and column j of Y, or of the part's sums
+  __device__ __forceinline__ void store(const Product& P, uint32_t part, int64_t i, int64_t j, int lane) const {
+    constexpr int kPerRow = COLS * kSize<OUT> / 16, kRows = 64 / kPerRow, kEach = 16 / kSize<OUT>;
+    static_assert(64 % kPerRow == 0 && ROWS % kRows == 0, "block");
+    asm volatile("" ::: "memory");
+    const int64_t ld = OUT == kSums ? P.sums_ld : P.n, col = j + kEach * (lane % kPerRow);
+    uint8_t* const to = OUT == kSums ? reinterpret_cast<uint8_t*>(P.sums + (int64_t)part * P.m * ld) : static_cast<uint8_t*>(P.y);
+    const lds_u8* const from = lds + lane / kPerRow * kPitch + 16 * (lane % kPerRow);
+    if (col < ld) {
+#pragma unroll
+      for (int r = 0; r < ROWS; r += kRows) {
+        const v4u v = *(const __attribute__((address_space(3))) v4u*)(from + r * kPitch);
+        const int64_t row = i + r + lane / kPerRow;
+        if (row >= P.m) continue;
+        uint8_t* const at = to + (row * ld + col) * kSize<OUT>;
+        if (P.lines || OUT == kSums) {
+          *reinterpret_cast<v4u*>(at) = v;
+        } else if (OUT == EP_FP32) {
+#pragma unroll
+          for (int e = 0; e < 4; e++)
+            if (col + e < P.n) reinterpret_cast<uint32_t*>(at)[e] = v[e];
+        } else {
+#pragma unroll
+          for (int e = 0; e < 8; e++)
+            if (col + e < P.n) reinterpret_cast<uint16_t*>(at)[e] = (uint16_t)(v[e / 2] >> (16 * (e % 2)));
+        }
+      }
+    }
+    asm volatile("" ::: "memory");
+  }
+};
+__device__ __forceinline__ v4f staged4(const lds_u8* lds, int c) { return *(const __attribute__((address_space(3))) v4f*)(lds + 4 * c); }
 
 // A 16 x 16 tile over 128 of k: v_mfma_i32_16x16x64_i8 multiplies 16 rows of W by 16 rows of X, lane l
 // supplying 16 bytes of row l mod 16 of both and getting the sums of W rows 4 (l / 16) + 0 .. 3 with
@@ -150,7 +237,7 @@ __global__ __launch_bounds__(64 * KW) void ring_kernel(Product P, uint32_t heigh
 // 16 x 16; NS stages of operands are in LDS, written by direct loads while the stage before is
 // multiplied.
 template <int OUT, int NW, int NX, int WW, int WX, int NS>
-__device__ __forceinline__ void tile_product(const Product& P, int64_t i0, int64_t j0, lds_u8* lds) {
+__device__ __forceinline__ void tile_product(const Product& P, uint32_t part, int64_t i0, int64_t j0, lds_u8* lds) {
   constexpr int kWaves = WW * WX, TW = 16 * NW * WW, TX = 16 * NX * WX;
   constexpr int kSegsW = TW / 8 / kWaves, kSegsX = TX / 8 / kWaves;   // 1 KiB loads of a wave and step
   constexpr int kPerStep = kSegsW + kSegsX;
@@ -161,7 +248,7 @@ __device__ __forceinline__ void tile_product(const Product& P, int64_t i0, int64
   const int col = lane & 15, quarter = lane >> 4;
   const int ww = wave % WW, wx = wave / WW;
   const int64_t rows_x = min(P.m - i0, (int64_t)TX), rows_w = min(P.n - j0, (int64_t)TW);
-  const uint32_t k = (uint32_t)P.k, kb = P.kb;
+  const uint32_t k = (uint32_t)P.k, b0 = part * P.part_steps, b1 = min(b0 + P.part_steps, P.kb);
   const __amdgpu_buffer_rsrc_t rx = rsrc_of(P.x + i0 * P.k, rows_x * P.k), rw = rsrc_of(P.w + j0 * P.k, rows_w * P.k);
 
   // direct loads: a wave instruction fills one segment of 8 rows; lane l writes the 16 bytes at
@@ -172,7 +259,7 @@ __device__ __forceinline__ void tile_product(const Product& P, int64_t i0, int64
   auto fetch = [&](uint32_t b, uint32_t stage) {
     lds_u8* const dst = lds + kStage * stage + 1024 * wave;
     const uint32_t at = 128 * b + chunk;
-    const uint32_t off = at < k ? seg_row * k + at : kOutside;
+    const uint32_t off = b < b1 && at < k ? seg_row * k + at : kOutside;
 #pragma unroll
     for (int q = 0; q < kSegsX; q++)
       __builtin_amdgcn_raw_ptr_buffer_load_lds(rx, dst + 1024 * kWaves * q, 16, off + 8 * kWaves * q * k, 0, 0, 0);
@@ -197,10 +284,10 @@ __device__ __forceinline__ void tile_product(const Product& P, int64_t i0, int64
   };
 
 #pragma unroll
-  for (int s = 0; s < NS - 1; s++) fetch(s, s);
+  for (int s = 0; s < NS - 1; s++) fetch(b0 + s, s);
   stage_barrier<(NS - 2) * kPerStep>();
   uint32_t stage = 0;
-  for (uint32_t b = 0; b < kb; b++) {
+  for (uint32_t b = b0; b < b1; b++) {
     const lds_u8* const p = lds + kStage * stage;
     fetch(b + NS - 1, stage == 0 ? NS - 1 : stage - 1);
     Fragment xf[NX];
@@ -215,56 +302,144 @@ __device__ __forceinline__ void tile_product(const Product& P, int64_t i0, int64
     stage_barrier<(NS - 2) * kPerStep>();
     stage = stage + 1 == NS ? 0 : stage + 1;
   }
-  __builtin_amdgcn_s_waitcnt(0);   // direct loads still in flight land before the wave ends
-
+  __builtin_amdgcn_s_waitcnt(0);   // direct loads still in flight land before LDS is used again
+  stage_scales<OUT>(P, j0, TW, lds);
+  typedef Block<OUT, 16, 16 * NW> Strip;
+  static_assert(8 * TW + kWaves * Strip::kBytes <= NS * kStage, "LDS");
+  const Strip strip = {lds + 8 * TW + wave * Strip::kBytes};
 #pragma unroll
-  for (int i = 0; i < NW; i++) {
-    const int64_t j = j0 + 16 * (NW * ww + i) + 4 * quarter;
-    if (j >= P.n) continue;
+  for (int t = 0; t < NX; t++) {
+    const int64_t row = i0 + 16 * (NX * wx + t);
+    const float xs = OUT == kSums ? 0.0f : P.x_scale[min(row + col, P.m - 1)];
 #pragma unroll
-    for (int t = 0; t < NX; t++) {
-      const int64_t row = i0 + 16 * (NX * wx + t) + col;
-      if (row < P.m) finish<OUT>(P, row, j, acc[i][t]);
+    for (int i = 0; i < NW; i++) {
+      const int c = 16 * (NW * ww + i) + 4 * quarter;
+      strip.put(col, 16 * i + 4 * quarter, acc[i][t], xs, staged4(lds, c), staged4(lds, TW + c));
     }
+    strip.store(P, part, row, j0 + 16 * NW * ww, lane);
   }
 }
 
-// Workgroups [0, full) take whole tiles; the `split` last tiles are taken as two halves of W's
-// rows each by the others, so that a last round of few tiles takes half as long.
+// Units [0, full) are whole tiles; the `split` last tiles are taken as two halves of W's rows each, so that
+// a last round of few tiles takes half as long.  Every unit is taken by `parts` workgroups, one for each
+// share of k, which follow each other on one XCD: they read the same rows of W or X.
+struct Units {
+  uint32_t tw, tx, full, split;
+  // The unit and the share of k of this workgroup; whole tiles and halves are spread over the XCDs apart.
+  __device__ __forceinline__ void mine(uint32_t parts, uint32_t& unit, uint32_t& part) const {
+    const uint32_t whole = full * parts;
+    const uint32_t id = blockIdx.x < whole ? xcd_spread(blockIdx.x, whole) : whole + xcd_spread(blockIdx.x - whole, 2 * split * parts);
+    unit = id / parts;
+    part = id - unit * parts;
+  }
+};
 template <int OUT, int NW, int NX, int WW, int WX, int NS>
-__global__ __launch_bounds__(64 * WW * WX) void tiles_kernel(Product P, uint32_t tw, uint32_t tx, uint32_t full, uint32_t split) {
+__global__ __launch_bounds__(64 * WW * WX) void tiles_kernel(Product P, Units U) {
   constexpr int TW = 16 * NW * WW, TX = 16 * NX * WX;
   __shared__ __attribute__((aligned(1024))) uint8_t lds_mem[NS * (TW + TX) * 128];
   lds_u8* const lds = (lds_u8*)lds_mem;
-  uint32_t ti, tj;
-  if (blockIdx.x < full) {
-    tile_of(xcd_spread(blockIdx.x, full), tx, tw, ti, tj);
-    tile_product<OUT, NW, NX, WW, WX, NS>(P, (int64_t)ti * TX, (int64_t)tj * TW, lds);
+  uint32_t unit, part, ti, tj;
+  U.mine(P.parts, unit, part);
+  if (unit < U.full) {
+    tile_of(unit, U.tx, U.tw, ti, tj);
+    tile_product<OUT, NW, NX, WW, WX, NS>(P, part, (int64_t)ti * TX, (int64_t)tj * TW, lds);
   } else {
-    const uint32_t u = xcd_spread(blockIdx.x - full, 2 * split);
-    tile_of(full + u / 2, tx, tw, ti, tj);
+    const uint32_t u = unit - U.full;
+    tile_of(U.full + u / 2, U.tx, U.tw, ti, tj);
     const int64_t j0 = (int64_t)tj * TW + TW / 2 * (u & 1);
-    if (j0 < P.n) tile_product<OUT, NW / 2, NX, WW, WX, NS>(P, (int64_t)ti * TX, j0, lds);
+    if (j0 < P.n) tile_product<OUT, NW / 2, NX, WW, WX, NS>(P, part, (int64_t)ti * TX, j0, lds);
   }
 }
 
+// Many rows: tiles of 256 x 256 by four waves (i8_tile.h), W's rows as A so that a lane has four columns
+// of a row of Y side by side; halves are of X's rows.
+template <int OUT, int TN>
+__device__ __forceinline__ void large_tile(const Product& P, uint32_t part, int64_t i0, int64_t j0, lds_u8* lds) {
+  const int64_t k_lo = (int64_t)part * P.part_steps * 128, k_hi = min(k_lo + (int64_t)P.part_steps * 128, P.k);
+  i8::tile_product<TN>(reinterpret_cast<const int8_t*>(P.w), reinterpret_cast<const int8_t*>(P.x), P.n, P.m, P.k, j0, i0, k_lo, k_hi,
+                       (i8::lds_u8*)lds, [&](const auto& acc, int ww, int wx, int lane) {
+    constexpr int kWaveX = TN / 2;
+    const int half = lane >> 5, col = lane & 31;
+    stage_scales<OUT>(P, j0, 256, lds);
+    typedef Block<OUT, 32, i8::kWaveM> Strip;
+    static_assert(8 * 256 + 4 * Strip::kBytes <= i8::kSlots * i8::kSlotBytes, "LDS");
+    const Strip strip = {lds + 8 * 256 + (2 * ww + wx) * Strip::kBytes};
+#pragma unroll
+    for (int t = 0; t < kWaveX / 32; t++) {
+      const int64_t row = i0 + kWaveX * wx + 32 * t;
+      const float xs = OUT == kSums ? 0.0f : P.x_scale[min(row + col, P.m - 1)];
+#pragma unroll
+      for (int i = 0; i < i8::kBlocksM; i++)
+#pragma unroll
+        for (int g = 0; g < 4; g++) {
+          const int c = 32 * i + 8 * g + 4 * half, at = i8::kWaveM * ww + c;
+          const v4i v = {acc[i][t][4 * g], acc[i][t][4 * g + 1], acc[i][t][4 * g + 2], acc[i][t][4 * g + 3]};
+          strip.put(col, c, v, xs, staged4(lds, at), staged4(lds, 256 + at));
+        }
+      strip.store(P, part, row, j0 + i8::kWaveM * ww, lane);
+    }
+  });
+}
+template <int OUT>
+__global__ __launch_bounds__(i8::kGemmThreads) void large_kernel(Product P, Units U) {
+  __shared__ __attribute__((aligned(1024))) uint8_t lds_mem[i8::kSlots * i8::kSlotBytes];
+  lds_u8* const lds = (lds_u8*)lds_mem;
+  uint32_t unit, part, ti, tj;
+  U.mine(P.parts, unit, part);
+  if (unit < U.full) {
+    tile_of(unit, U.tw, U.tx, tj, ti);
+    large_tile<OUT, 256>(P, part, (int64_t)ti * 256, (int64_t)tj * 256, lds);
+  } else {
+    const uint32_t u = unit - U.full;
+    tile_of(U.full + u / 2, U.tw, U.tx, tj, ti);
+    large_tile<OUT, 128>(P, part, (int64_t)ti * 256 + 128 * (u & 1), (int64_t)tj * 256, lds);
+  }
+}
+
+// The parts' sums, scales, bias and rounding: a thread for four columns of a row.
+template <int OUT>
+__global__ __launch_bounds__(256) void join_kernel(Product P) {
+  const uint32_t per_row = (uint32_t)(P.sums_ld / 4), id = blockIdx.x * 256 + threadIdx.x;   // below 2^31
+  const int64_t i = id / per_row, j = 4 * (int64_t)(id - (uint32_t)i * per_row);
+  if (i >= P.m) return;
+  const v4i* p = reinterpret_cast<const v4i*>(P.sums + i * P.sums_ld + j);
+  const int64_t next = P.m * P.sums_ld / 4;
+  v4i v = {};
+  for (uint32_t s = 0; s < P.parts; s += 4) {
+    v4i part[4];
+#pragma unroll
+    for (uint32_t e = 0; e < 4; e++) part[e] = p[min(s + e, P.parts - 1) * next];
+#pragma unroll
+    for (uint32_t e = 0; e < 4; e++)
+      if (s + e < P.parts) v += part[e];
+  }
+  finish<OUT>(P, i, j, v);
+}
+
+Units units_of(const Product& P, int tw, int tx, int cus) {
+  const uint32_t x = (uint32_t)((P.m + tx - 1) / tx), w = (uint32_t)((P.n + tw - 1) / tw), tiles = x * w;
+  const uint32_t last = tiles % cus, split = P.parts == 1 && 2 * last <= (uint32_t)cus ? last : 0;
+  return {w, x, tiles - split, split};
+}
 template <int OUT, int NW, int NX, int WW, int WX, int NS>
 void tiles_launch(const Product& P, int cus, hipStream_t stream) {
-  constexpr int TW = 16 * NW * WW, TX = 16 * NX * WX;
-  const uint32_t tx = (uint32_t)((P.m + TX - 1) / TX), tw = (uint32_t)((P.n + TW - 1) / TW);
-  const uint32_t tiles = tx * tw, last = tiles % cus, split = 2 * last <= (uint32_t)cus ? last : 0;
-  hipLaunchKernelGGL((tiles_kernel<OUT, NW, NX, WW, WX, NS>), dim3(tiles + split), dim3(64 * WW * WX), 0, stream, P, tw, tx,
-                     tiles - split, split);
+  const Units U = units_of(P, 16 * NW * WW, 16 * NX * WX, cus);
+  hipLaunchKernelGGL((tiles_kernel<OUT, NW, NX, WW, WX, NS>), dim3((U.full + 2 * U.split) * P.parts), dim3(64 * WW * WX), 0, stream, P, U);
+}
+template <int OUT>
+void large_launch(const Product& P, int cus, hipStream_t stream) {
+  const Units U = units_of(P, 256, 256, cus);
+  hipLaunchKernelGGL(large_kernel<OUT>, dim3((U.full + 2 * U.split) * P.parts), dim3(i8::kGemmThreads), 0, stream, P, U);
 }
 
 // Rows of W for a workgroup of the streaming kernel: the multiple of 8 up to 16 NW that makes the
 // CU with the most work read the fewest rows.
 template <int NW, int NX>
-uint32_t ring_height(const Product& P, int cus) {
-  const int64_t tx = (P.m + 16 * NX - 1) / (16 * NX), rows_x = std::min<int64_t>(P.m, 16 * NX);
+uint32_t ring_height(int64_t m, int64_t n, int cus) {
+  const int64_t tx = (m + 16 * NX - 1) / (16 * NX), rows_x = std::min<int64_t>(m, 16 * NX);
   int64_t best = 16 * NW, least = INT64_MAX;
   for (int64_t h = 16 * NW; h >= 8; h -= 8) {
-    const int64_t read = rounds((P.n + h - 1) / h * tx, cus) * (h + rows_x);
+    const int64_t read = rounds((n + h - 1) / h * tx, cus) * (h + rows_x);
     if (read < least) {
       least = read;
       best = h;
@@ -280,20 +455,105 @@ void ring_launch(const Product& P, uint32_t height, hipStream_t stream) {
   hipLaunchKernelGGL((ring_kernel<OUT, NW, NX, KW, NS>), dim3(per_xcd * kXcds * tx), dim3(64 * KW), 0, stream, P, height, per_xcd);
 }
 
-template <int OUT>
-void product_launch(const Product& P, int cus, hipStream_t stream) {
-  if (P.m <= 16) {
-    const uint32_t h = ring_height<2, 1>(P, cus);
-    if (rounds((P.n + h - 1) / h, cus) > 1) ring_launch<OUT, 2, 1, 4, 2>(P, h, stream);
-    else ring_launch<OUT, 2, 1, 8, 2>(P, h, stream);
-    return;
+// ---- which kernel -----------------------------------------------------------------------
+// Estimates of a launch's time in ns: what a step of 128 along k takes on the busiest CU, what a
+// workgroup takes besides (first loads, stores), what the launch takes besides, and never less than the
+// operands' way from memory.  Fitted to 5339 launches of 17 to 3000 rows, 1000 to 17408 columns and k from
+// 512 to 17408, each with every kernel and up to 16 shares of k; over the 136 sizes the choice is 2 % slower
+// than the best of them (geometric mean), and 7 to 55 % where 1000 columns leave most CUs idle.
+enum Kernel { kRing16, kRing32, kRing64, kTile64, kTile128, kWideX, kWideW, kWideW64, kLarge };
+struct TileCost {
+  Kernel kernel;
+  int rows_w, rows_x;
+  int half, one, each;   // a CU with half a tile (of W's rows, the largest one's of X's), with one, and with more, for each
+};
+constexpr TileCost kTiles[] = {{kTile64, 128, 64, 290, 540, 365},    {kTile128, 128, 128, 420, 580, 705},
+                               {kWideX, 128, 256, 595, 700, 965},    {kWideW, 256, 128, 520, 985, 935},
+                               {kWideW64, 256, 64, 385, 635, 715},   {kLarge, 256, 256, 1025, 1580, 1330}};
+constexpr int kMostParts = 16;
+constexpr int kGroup = 1125, kRingGroup = 1570, kLaunch = 4030, kRingLaunch = 3660, kRing32Step = 133, kRing64Step = 181;
+constexpr int kMemory = 6440, kJoin = 2480, kJoinValues = 740;   // bytes in a ns; a join, and the sums that it adds in a ns
+
+struct Plan {
+  Kernel kernel;
+  uint32_t parts, part_steps, height;
+};
+
+// A launch of few tiles shares k out over workgroups, whose sums another launch joins.
+// 203 x 5120 x 17408 in tiles of 128 x 256, 40 of them: 39 us in 6 parts, 100 in one, 48 in tiles of half the size.
+Plan plan_of(int64_t m, int64_t n, int64_t k, int cus) {
+  const uint32_t kb = (uint32_t)((k + 127) / 128);
+  if (m <= 16) return {kRing16, 1, kb, ring_height<2, 1>(m, n, cus)};
+  const int64_t memory = (m + n) * k / kMemory;
+  // the streaming kernels read X again for every strip of W: not where X is what there is most of
+  Plan best = {kRing32, 1, kb, 0};
+  int64_t least = INT64_MAX;
+  if (m <= 512) {
+    const uint32_t h2 = ring_height<3, 2>(m, n, cus), h4 = ring_height<3, 4>(m, n, cus);
+    const int64_t t2 = (kRing32Step * kb + kRingGroup) * rounds((n + h2 - 1) / h2 * ((m + 31) / 32), cus);
+    const int64_t t4 = (kRing64Step * kb + kRingGroup) * rounds((n + h4 - 1) / h4 * ((m + 63) / 64), cus);
+    best = t2 <= t4 ? Plan{kRing32, 1, kb, h2} : Plan{kRing64, 1, kb, h4};
+    least = std::max(std::min(t2, t4), memory) + kRingLaunch;
   }
-  const int64_t large = rounds(((P.m + 255) / 256) * ((P.n + 255) / 256), cus);
-  if (P.m > 512 && large >= 1) tiles_launch<OUT, 8, 4, 2, 4, 2>(P, cus, stream);
-  else tiles_launch<OUT, 4, 2, 2, 2, 3>(P, cus, stream);
+  for (const TileCost& c : kTiles) {
+    const int64_t tiles = (m + c.rows_x - 1) / c.rows_x * ((n + c.rows_w - 1) / c.rows_w);
+    const uint32_t most = tiles >= cus ? 1 : (uint32_t)std::min<int64_t>(kMostParts, 4 * cus / tiles);
+    for (uint32_t p = 1; p <= most && p <= kb; p++) {
+      const uint32_t steps = (kb + p - 1) / p;
+      if ((kb + steps - 1) / steps != p) continue;   // the last parts would be empty
+      const int64_t halves = p == 1 ? rounds(2 * tiles, cus) : 2 * rounds(tiles * p, cus);
+      const int64_t step = halves == 1 ? c.half : std::max<int64_t>(c.one, c.each * halves / 2);
+      int64_t time = std::max(step * steps + kGroup * ((halves + 1) / 2), memory) + kLaunch;
+      if (p > 1) time += kJoin + p * m * n / kJoinValues;
+      if (time < least) {
+        least = time;
+        best = {c.kernel, p, steps, 0};
+      }
+    }
+  }
+  return best;
+}
+uint64_t workspace_of(const Plan& plan, int64_t m, int64_t n) {
+  return plan.parts > 1 ? (uint64_t)plan.parts * m * ((n + 3) / 4 * 4) * 4 : 0;
+}
+
+template <int OUT>
+void tile_launch(Kernel kernel, const Product& P, int cus, hipStream_t stream) {
+  if (kernel == kTile64) tiles_launch<OUT, 4, 2, 2, 2, 3>(P, cus, stream);
+  else if (kernel == kTile128) tiles_launch<OUT, 4, 4, 2, 2, 4>(P, cus, stream);
+  else if (kernel == kWideX) tiles_launch<OUT, 4, 4, 2, 4, 3>(P, cus, stream);
+  else if (kernel == kWideW) tiles_launch<OUT, 4, 4, 4, 2, 3>(P, cus, stream);
+  else if (kernel == kWideW64) tiles_launch<OUT, 4, 2, 4, 2, 4>(P, cus, stream);
+  else large_launch<OUT>(P, cus, stream);
+}
+
+// Up to 16 rows the launch is W's stream from memory: by four waves a workgroup, or eight where W has too
+// few strips for several workgroups on a CU.
+template <int OUT>
+void product_launch(const Plan& plan, const Product& P, int cus, hipStream_t stream) {
+  if (plan.kernel == kRing16) {
+    if (rounds((P.n + plan.height - 1) / plan.height, cus) > 1) ring_launch<OUT, 2, 1, 4, 2>(P, plan.height, stream);
+    else ring_launch<OUT, 2, 1, 8, 2>(P, plan.height, stream);
+  } else if (plan.kernel == kRing32) {
+    ring_launch<OUT, 3, 2, 6, 2>(P, plan.height, stream);
+  } else if (plan.kernel == kRing64) {
+    ring_launch<OUT, 3, 4, 5, 2>(P, plan.height, stream);
+  } else if (P.parts == 1) {
+    tile_launch<OUT>(plan.kernel, P, cus, stream);
+  } else {
+    tile_launch<kSums>(plan.kernel, P, cus, stream);
+    const int64_t threads = P.m * (P.sums_ld / 4);   // of fewer tiles than CUs: below 2^31
+    hipLaunchKernelGGL(join_kernel<OUT>, dim3((uint32_t)((threads + 255) / 256)), dim3(256), 0, stream, P);
+  }
 }
 
 bool misaligned(const void* p) { return reinterpret_cast<uintptr_t>(p) & 15; }
+
+int compute_units() {
+  int dev = 0, cus = 0;
+  if (hipGetDevice(&dev) != hipSuccess || hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess) return 0;
+  return cus;
+}
 
 constexpr int64_t kMost = 1 << 24, kMostK = 131071;   // sums of k products of two codes stay below 2^31
 bool bad_sizes(int64_t m, int64_t n, int64_t k) { return m < 0 || n <= 0 || k <= 0 || k % 16 || m > kMost || n > kMost || k > kMostK; }
@@ -302,8 +562,8 @@ bool bad_sizes(int64_t m, int64_t n, int64_t k) { return m < 0 || n <= 0 || k <=
 }  // namespace ep
 
 extern "C" uint64_t ep_gemm_i8_scaled_workspace(int64_t m, int64_t n, int64_t k) {
-  if (ep::bad_sizes(m, n, k)) return 0;
-  return 0;
+  const int cus = ep::compute_units();
+  return ep::bad_sizes(m, n, k) || m == 0 || cus <= 0 ? 0 : ep::workspace_of(ep::plan_of(m, n, k, cus), m, n);
 }
 
 extern "C" int ep_gemm_i8_scaled(const int8_t* d_x, const float* d_x_scale, const int8_t* d_w, const float* d_w_scale,
@@ -320,19 +580,19 @@ extern "C" int ep_gemm_i8_scaled(const int8_t* d_x, const float* d_x_scale, cons
   if (misaligned(d_x) || misaligned(d_w) || reinterpret_cast<uintptr_t>(d_y) % size ||
       (reinterpret_cast<uintptr_t>(d_x_scale) | reinterpret_cast<uintptr_t>(d_w_scale) | reinterpret_cast<uintptr_t>(d_bias)) % 4)
     return fail(EP_ERR_ARG, "ep_gemm_i8_scaled: operands must be 16-byte aligned, scales, bias and y by their elements");
-  const uint64_t need = ep_gemm_i8_scaled_workspace(m, n, k);
-  if (need && (!d_workspace || misaligned(d_workspace) || ws_bytes < need))
+  const int cus = compute_units();
+  if (cus <= 0) return fail(EP_ERR_HIP, "ep_gemm_i8_scaled: no device");
+  const Plan plan = plan_of(m, n, k, cus);
+  if (workspace_of(plan, m, n) && (!d_workspace || misaligned(d_workspace) || ws_bytes < workspace_of(plan, m, n)))
     return fail(EP_ERR_ARG, "ep_gemm_i8_scaled: a workspace that is missing, misaligned or short");
-  int dev = 0, cus = 0;
-  if (hipGetDevice(&dev) != hipSuccess ||
-      hipDeviceGetAttribute(&cus, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || cus <= 0)
-    return fail(EP_ERR_HIP, "ep_gemm_i8_scaled: no device");
   const Product P = {reinterpret_cast<const uint8_t*>(d_x), d_x_scale, reinterpret_cast<const uint8_t*>(d_w), d_w_scale, d_bias, d_y, m, n, k,
-                     (uint32_t)((k + 127) / 128), n % 4 == 0 && reinterpret_cast<uintptr_t>(d_y) % (4 * size) == 0};
+                     (uint32_t)((k + 127) / 128), n % 4 == 0 && reinterpret_cast<uintptr_t>(d_y) % (4 * size) == 0,
+                     n * size % 16 == 0 && reinterpret_cast<uintptr_t>(d_y) % 16 == 0,
+                     plan.parts > 1 ? static_cast<int32_t*>(d_workspace) : nullptr, (n + 3) / 4 * 4, plan.parts, plan.part_steps};
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
-  if (y_dtype == EP_FP32) product_launch<EP_FP32>(P, cus, stream);
-  else if (y_dtype == EP_FP16) product_launch<EP_FP16>(P, cus, stream);
-  else product_launch<EP_BF16>(P, cus, stream);
+  if (y_dtype == EP_FP32) product_launch<EP_FP32>(plan, P, cus, stream);
+  else if (y_dtype == EP_FP16) product_launch<EP_FP16>(plan, P, cus, stream);
+  else product_launch<EP_BF16>(plan, P, cus, stream);
   if (hipGetLastError() != hipSuccess) return fail(EP_ERR_HIP, "ep_gemm_i8_scaled: launch failed");
   return EP_OK;
 }
