@@ -4,6 +4,7 @@
 
 #include <algorithm>
 #include <cstdint>
+#include <type_traits>
 
 #include "../../include/entropack.h"
 #include "common.h"
@@ -29,7 +30,6 @@ struct Product {
   int64_t m, n, k;
   uint32_t kb;         // steps of 128 along k
   uint32_t wide;       // four values of a row of Y from a multiple of four on lie aligned as one store's
-  uint32_t lines;      // every 16 bytes of a row of Y from a multiple of 16 on lie aligned inside it
   int32_t* sums;       // [parts][m][sums_ld], or null: one part, which writes Y
   int64_t sums_ld;     // n, rounded up to a multiple of 4
   uint32_t parts, part_steps;   // of k, and the steps of 128 of each
@@ -100,27 +100,22 @@ struct Block {
     constexpr int kPerRow = COLS * kSize<OUT> / 16, kRows = 64 / kPerRow, kEach = 16 / kSize<OUT>;
     static_assert(64 % kPerRow == 0 && ROWS % kRows == 0, "block");
     asm volatile("" ::: "memory");
-    const int64_t ld = OUT == kSums ? P.sums_ld : P.n, col = j + kEach * (lane % kPerRow);
-    uint8_t* const to = OUT == kSums ? reinterpret_cast<uint8_t*>(P.sums + (int64_t)part * P.m * ld) : static_cast<uint8_t*>(P.y);
+    const int64_t ld = OUT == kSums ? P.sums_ld : P.n;
+    uint8_t* const to = (OUT == kSums ? reinterpret_cast<uint8_t*>(P.sums + (int64_t)part * P.m * ld) : static_cast<uint8_t*>(P.y)) +
+                        (i * ld + j) * kSize<OUT>;
+    typedef typename std::conditional<kSize<OUT> == 2, uint16_t, uint32_t>::type element;
     const lds_u8* const from = lds + lane / kPerRow * kPitch + 16 * (lane % kPerRow);
-    if (col < ld) {
+    const int64_t left = ld - j - kEach * (lane % kPerRow);   // columns from this lane's on
 #pragma unroll
-      for (int r = 0; r < ROWS; r += kRows) {
+    for (int r = 0; r < ROWS; r += kRows) {
+      uint8_t* const at = to + (r + lane / kPerRow) * ld * kSize<OUT> + 16 * (lane % kPerRow);
+      if (i + r + lane / kPerRow >= P.m) continue;
+      if (left >= kEach) {
         const v4u v = *(const __attribute__((address_space(3))) v4u*)(from + r * kPitch);
-        const int64_t row = i + r + lane / kPerRow;
-        if (row >= P.m) continue;
-        uint8_t* const at = to + (row * ld + col) * kSize<OUT>;
-        if (P.lines || OUT == kSums) {
-          *reinterpret_cast<v4u*>(at) = v;
-        } else if (OUT == EP_FP32) {
-#pragma unroll
-          for (int e = 0; e < 4; e++)
-            if (col + e < P.n) reinterpret_cast<uint32_t*>(at)[e] = v[e];
-        } else {
-#pragma unroll
-          for (int e = 0; e < 8; e++)
-            if (col + e < P.n) reinterpret_cast<uint16_t*>(at)[e] = (uint16_t)(v[e / 2] >> (16 * (e % 2)));
-        }
+        __builtin_memcpy(reinterpret_cast<element*>(at), &v, 16);   // rows of Y begin at any element
+      } else {
+        for (int e = 0; e < left; e++)
+          reinterpret_cast<element*>(at)[e] = *(const __attribute__((address_space(3))) element*)(from + r * kPitch + e * kSize<OUT>);
       }
     }
     asm volatile("" ::: "memory");
@@ -457,22 +452,24 @@ void ring_launch(const Product& P, uint32_t height, hipStream_t stream) {
 
 // ---- which kernel -----------------------------------------------------------------------
 // Estimates of a launch's time in ns: what a step of 128 along k takes on the busiest CU, what a
-// workgroup takes besides (first loads, stores), what the launch takes besides, and never less than the
-// operands' way from memory.  Fitted to 5339 launches of 17 to 3000 rows, 1000 to 17408 columns and k from
-// 512 to 17408, each with every kernel and up to 16 shares of k; over the 136 sizes the choice is 2 % slower
-// than the best of them (geometric mean), and 7 to 55 % where 1000 columns leave most CUs idle.
+// workgroup takes besides (first loads, and the stores of a tile by its size), what the launch takes
+// besides, and never less than the operands' and outputs' way through memory.  Fitted to launches of 156
+// sizes (17 to 5000 rows, 310 to 17408 columns, k from 16 to 17408), each with every kernel and up to 16
+// shares of k; over them the choice is 1 % slower than the best (geometric mean), and 5 % at most where
+// the kernel and not the call is what takes the time.
 enum Kernel { kRing16, kRing32, kRing64, kTile64, kTile128, kWideX, kWideW, kWideW64, kLarge };
 struct TileCost {
   Kernel kernel;
   int rows_w, rows_x;
   int half, one, each;   // a CU with half a tile (of W's rows, the largest one's of X's), with one, and with more, for each
+  int besides;
 };
-constexpr TileCost kTiles[] = {{kTile64, 128, 64, 290, 540, 365},    {kTile128, 128, 128, 420, 580, 705},
-                               {kWideX, 128, 256, 595, 700, 965},    {kWideW, 256, 128, 520, 985, 935},
-                               {kWideW64, 256, 64, 385, 635, 715},   {kLarge, 256, 256, 1025, 1580, 1330}};
+constexpr TileCost kTiles[] = {{kTile64, 128, 64, 255, 425, 330, 1975},    {kTile128, 128, 128, 385, 410, 700, 2700},
+                               {kWideX, 128, 256, 525, 735, 810, 4160},    {kWideW, 256, 128, 495, 815, 845, 4160},
+                               {kWideW64, 256, 64, 355, 420, 625, 2700},   {kLarge, 256, 256, 825, 860, 1095, 10400}};
 constexpr int kMostParts = 16;
-constexpr int kGroup = 1125, kRingGroup = 1570, kLaunch = 4030, kRingLaunch = 3660, kRing32Step = 133, kRing64Step = 181;
-constexpr int kMemory = 6440, kJoin = 2480, kJoinValues = 740;   // bytes in a ns; a join, and the sums that it adds in a ns
+constexpr int kRing32Step = 95, kRing64Step = 182, kRingBesides = 1955, kLaunch = 3890, kRingLaunch = 2330;
+constexpr int kMemory = 5955, kJoin = 1640, kJoinValues = 855;   // bytes in a ns; a join, and the sums that it adds in a ns
 
 struct Plan {
   Kernel kernel;
@@ -484,14 +481,14 @@ struct Plan {
 Plan plan_of(int64_t m, int64_t n, int64_t k, int cus) {
   const uint32_t kb = (uint32_t)((k + 127) / 128);
   if (m <= 16) return {kRing16, 1, kb, ring_height<2, 1>(m, n, cus)};
-  const int64_t memory = (m + n) * k / kMemory;
+  const int64_t memory = ((m + n) * k + 2 * m * n) / kMemory;
   // the streaming kernels read X again for every strip of W: not where X is what there is most of
   Plan best = {kRing32, 1, kb, 0};
   int64_t least = INT64_MAX;
   if (m <= 512) {
     const uint32_t h2 = ring_height<3, 2>(m, n, cus), h4 = ring_height<3, 4>(m, n, cus);
-    const int64_t t2 = (kRing32Step * kb + kRingGroup) * rounds((n + h2 - 1) / h2 * ((m + 31) / 32), cus);
-    const int64_t t4 = (kRing64Step * kb + kRingGroup) * rounds((n + h4 - 1) / h4 * ((m + 63) / 64), cus);
+    const int64_t t2 = (kRing32Step * kb + kRingBesides) * rounds((n + h2 - 1) / h2 * ((m + 31) / 32), cus);
+    const int64_t t4 = (kRing64Step * kb + kRingBesides) * rounds((n + h4 - 1) / h4 * ((m + 63) / 64), cus);
     best = t2 <= t4 ? Plan{kRing32, 1, kb, h2} : Plan{kRing64, 1, kb, h4};
     least = std::max(std::min(t2, t4), memory) + kRingLaunch;
   }
@@ -503,7 +500,7 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, int cus) {
       if ((kb + steps - 1) / steps != p) continue;   // the last parts would be empty
       const int64_t halves = p == 1 ? rounds(2 * tiles, cus) : 2 * rounds(tiles * p, cus);
       const int64_t step = halves == 1 ? c.half : std::max<int64_t>(c.one, c.each * halves / 2);
-      int64_t time = std::max(step * steps + kGroup * ((halves + 1) / 2), memory) + kLaunch;
+      int64_t time = std::max(step * steps + c.besides * halves / 2, memory) + kLaunch;
       if (p > 1) time += kJoin + p * m * n / kJoinValues;
       if (time < least) {
         least = time;
@@ -587,7 +584,6 @@ extern "C" int ep_gemm_i8_scaled(const int8_t* d_x, const float* d_x_scale, cons
     return fail(EP_ERR_ARG, "ep_gemm_i8_scaled: a workspace that is missing, misaligned or short");
   const Product P = {reinterpret_cast<const uint8_t*>(d_x), d_x_scale, reinterpret_cast<const uint8_t*>(d_w), d_w_scale, d_bias, d_y, m, n, k,
                      (uint32_t)((k + 127) / 128), n % 4 == 0 && reinterpret_cast<uintptr_t>(d_y) % (4 * size) == 0,
-                     n * size % 16 == 0 && reinterpret_cast<uintptr_t>(d_y) % 16 == 0,
                      plan.parts > 1 ? static_cast<int32_t*>(d_workspace) : nullptr, (n + 3) / 4 * 4, plan.parts, plan.part_steps};
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   if (y_dtype == EP_FP32) product_launch<EP_FP32>(plan, P, cus, stream);

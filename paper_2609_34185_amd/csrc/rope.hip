@@ -164,17 +164,20 @@ void launch(Rope& R, hipStream_t stream) {
   else hipLaunchKernelGGL((rope_kernel<T, VEC, false>), grid, dim3(kThreads), 0, stream, R);
 }
 
-// Eight channels at a time where every unit lies aligned for one load, else one by one.
+// Eight channels at a time where every unit lies aligned for one load, else as many as do.
 template <typename T>
 void launch(Rope& R, hipStream_t stream) {
   const ep_rope_call& C = R.c;
-  uintptr_t bytes = reinterpret_cast<uintptr_t>(C.d_q) | reinterpret_cast<uintptr_t>(C.d_q_out);
-  int64_t counts = C.rot_dim / 2 | C.rot_first | C.head_dim | C.q_row | C.q_out_row;
+  uint64_t bytes = reinterpret_cast<uintptr_t>(C.d_q) | reinterpret_cast<uintptr_t>(C.d_q_out);
+  uint64_t counts = C.rot_dim / 2 | C.rot_first | C.head_dim | C.q_row | C.q_out_row;
   if (C.k_heads) {
     bytes |= reinterpret_cast<uintptr_t>(C.d_k) | reinterpret_cast<uintptr_t>(C.d_k_out);
     counts |= C.k_row | C.k_out_row;
   }
-  if (bytes % 16 == 0 && counts % 8 == 0) launch<T, 8>(R, stream);
+  const auto aligned = [&](int vec) { return counts % vec == 0 && bytes % std::min<size_t>(16, vec * sizeof(T)) == 0; };
+  if (aligned(8)) launch<T, 8>(R, stream);
+  else if (aligned(4)) launch<T, 4>(R, stream);
+  else if (aligned(2)) launch<T, 2>(R, stream);
   else launch<T, 1>(R, stream);
 }
 
