@@ -12,7 +12,6 @@ namespace ep {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kStaged = 1024;   // entries of d_cu that a workgroup holds in LDS
 
 // Cosine and sine of `phase` / 2^32 of a turn.  The nearest quarter is taken off as an integer, which
 // leaves at most an eighth of a turn either way; there the Taylor series to x^11 and x^10 are within
@@ -54,36 +53,70 @@ struct Rope {
   uint32_t heads, lanes;      // of queries and keys; threads that share a token's heads, for each unit
 };
 
+// The last request that begins at or before token t, by whole waves: a lane for every 64th part of those
+// that are left, so that 64 requests take one load and 4096 two.
+__device__ __forceinline__ uint32_t request_of(const int32_t* cu, uint32_t n, int64_t t) {
+  const uint32_t lane = threadIdx.x & 63;
+  uint32_t lo = 0;
+  while (n > 1) {
+    const uint32_t step = (n + 63) / 64, at = lane * step;
+    const uint64_t begun = __ballot(at < n && cu[lo + min(at, n - 1)] <= t);
+    const uint32_t part = begun ? 63 - __builtin_clzll(begun) : 0;
+    lo += part * step;
+    n = min(step, n - part * step);
+  }
+  return lo;
+}
+
 // A thread turns one unit (VEC pairs) of every lanes-th head of a token: its cosines and sines are
 // made once for all of them.
 template <typename T, int VEC, bool PAIRS>
 __global__ __launch_bounds__(kThreads) void rope_kernel(Rope R) {
-  __shared__ int32_t staged[kStaged];
   const ep_rope_call& C = R.c;
   const uint32_t units = R.rotated + R.copied, per_token = units * R.lanes;
-  uint32_t stride = 1;   // requests from one staged entry to the next
+  const uint64_t first = ((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * kThreads;
+  const int64_t t0 = (int64_t)(first / per_token);
+  if (t0 >= C.n_tokens) return;
+  const uint32_t into = (uint32_t)(first - (uint64_t)t0 * per_token) + threadIdx.x, ahead = into / per_token;
+  const int64_t t = t0 + ahead;
+  uint32_t b = 0, end = 1;   // the token's request is one of these
   if (!C.d_pos) {
-    stride = (uint32_t)((C.n_req + kStaged - 1) / kStaged);
-    for (uint32_t i = threadIdx.x; (int64_t)i * stride < C.n_req; i += kThreads) staged[i] = C.d_cu[(int64_t)i * stride];
-    __syncthreads();
+    b = request_of(C.d_cu, (uint32_t)C.n_req, t0);
+    const int64_t t1 = t0 + (kThreads - 1 + per_token - 1) / per_token;
+    end = b + 1 + (t1 > t0 && b + 1 < (uint32_t)C.n_req ? request_of(C.d_cu + b, (uint32_t)C.n_req - b, t1) : 0);
   }
-  const uint64_t id = ((uint64_t)blockIdx.y * gridDim.x + blockIdx.x) * kThreads + threadIdx.x;
-  const int64_t t = (int64_t)(id / per_token);
   if (t >= C.n_tokens) return;
-  const uint32_t in = (uint32_t)(id - (uint64_t)t * per_token), lane = in / units, unit = in - lane * units;
+  const uint32_t in = into - ahead * per_token, lane = in / units, unit = in - lane * units;
+
+  // what does not wait for the position: frequencies and the first head's values
+  const bool turns = unit < R.rotated;
+  uint32_t one, two;   // channels
+  uint64_t freq[VEC];
+  if (turns) {
+    one = C.rot_first + (PAIRS ? 2 : 1) * VEC * unit;
+    two = PAIRS ? one + VEC : one + C.rot_dim / 2;
+#pragma unroll
+    for (int i = 0; i < VEC; i++) freq[i] = C.d_freqs[VEC * unit + i];
+  } else {
+    one = VEC * (unit - R.rotated);
+    if (one >= (uint32_t)C.rot_first) one += C.rot_dim;
+    two = one;
+  }
+  typedef Pack<T, VEC> P;
+  const auto load = [&](uint32_t h, P& x, P& y) {
+    const bool key = h >= (uint32_t)C.q_heads;
+    const T* const from = static_cast<const T*>(key ? C.d_k : C.d_q) + t * (key ? C.k_row : C.q_row) +
+                          (int64_t)(key ? h - C.q_heads : h) * C.head_dim;
+    x = *reinterpret_cast<const P*>(from + one);
+    if (turns) y = *reinterpret_cast<const P*>(from + two);
+  };
+  P x, y;
+  load(lane, x, y);
 
   int32_t pos;
   if (C.d_pos) {
     pos = C.d_pos[t];
   } else {
-    // the last request that begins at or before t, first among the staged ones
-    uint32_t lo = 0, hi = (uint32_t)((C.n_req + stride - 1) / stride);
-    while (hi - lo > 1) {
-      const uint32_t mid = (lo + hi) / 2;
-      if (staged[mid] <= t) lo = mid;
-      else hi = mid;
-    }
-    uint32_t b = lo * stride, end = (uint32_t)min((int64_t)hi * stride, C.n_req);
     while (end - b > 1) {
       const uint32_t mid = (b + end) / 2;
       if (C.d_cu[mid] <= t) b = mid;
@@ -94,61 +127,47 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(Rope R) {
     pos = C.d_len[b] - past + (int32_t)t;
   }
 
-  const bool turns = unit < R.rotated;
-  uint32_t one, two;   // channels
   float co[VEC], si[VEC];
   if (turns) {
-    one = C.rot_first + (PAIRS ? 2 : 1) * VEC * unit;
-    two = PAIRS ? one + VEC : one + C.rot_dim / 2;
 #pragma unroll
     for (int i = 0; i < VEC; i++) {
-      const uint64_t phase = C.d_freqs[VEC * unit + i] * (uint64_t)(int64_t)pos;
+      const uint64_t phase = freq[i] * (uint64_t)(int64_t)pos;
       turn((uint32_t)((phase + 0x80000000u) >> 32), co[i], si[i]);
       co[i] *= C.amplitude;
       si[i] *= C.inverse ? -C.amplitude : C.amplitude;
     }
-  } else {
-    one = VEC * (unit - R.rotated);
-    if (one >= (uint32_t)C.rot_first) one += C.rot_dim;
-    two = 0;
   }
   for (uint32_t h = lane; h < R.heads; h += R.lanes) {
+    P next_x, next_y;
+    if (h + R.lanes < R.heads) load(h + R.lanes, next_x, next_y);   // heads lie apart, in place too
     const bool key = h >= (uint32_t)C.q_heads;
-    const int64_t head = (int64_t)(key ? h - C.q_heads : h) * C.head_dim;
-    const T* const from = static_cast<const T*>(key ? C.d_k : C.d_q) + t * (key ? C.k_row : C.q_row) + head;
-    T* const to = static_cast<T*>(key ? C.d_k_out : C.d_q_out) + t * (key ? C.k_out_row : C.q_out_row) + head;
-    typedef Pack<T, VEC> P;
-    if (!turns) {
-      *reinterpret_cast<P*>(to + one) = *reinterpret_cast<const P*>(from + one);
-      continue;
-    }
-    P x = *reinterpret_cast<const P*>(from + one), y = *reinterpret_cast<const P*>(from + two);
-    if (PAIRS) {   // x holds the first half of 2 VEC channels, y the second
+    T* const to = static_cast<T*>(key ? C.d_k_out : C.d_q_out) + t * (key ? C.k_out_row : C.q_out_row) +
+                  (int64_t)(key ? h - C.q_heads : h) * C.head_dim;
+    if (turns) {
 #pragma unroll
       for (int i = 0; i < VEC; i++) {
+        // pairs side by side: x holds the first half of 2 VEC channels, y the second
         const int k = 2 * i;
-        T& pa = k < VEC ? x.v[k] : y.v[k - VEC];
-        T& pb = k + 1 < VEC ? x.v[k + 1] : y.v[k + 1 - VEC];
+        T& pa = !PAIRS || k < VEC ? x.v[PAIRS ? k % VEC : i] : y.v[k % VEC];
+        T& pb = PAIRS && k + 1 < VEC ? x.v[(k + 1) % VEC] : y.v[PAIRS ? (k + 1) % VEC : i];
         const float a = value(pa), b = value(pb);
         pa = (T)__builtin_fmaf(a, co[i], -(b * si[i]));
         pb = (T)__builtin_fmaf(a, si[i], b * co[i]);
       }
-    } else {
-#pragma unroll
-      for (int i = 0; i < VEC; i++) {
-        const float a = value(x.v[i]), b = value(y.v[i]);
-        x.v[i] = (T)__builtin_fmaf(a, co[i], -(b * si[i]));
-        y.v[i] = (T)__builtin_fmaf(a, si[i], b * co[i]);
-      }
     }
     *reinterpret_cast<P*>(to + one) = x;
-    *reinterpret_cast<P*>(to + two) = y;
+    if (turns) *reinterpret_cast<P*>(to + two) = y;
+    x = next_x;
+    y = next_y;
   }
 }
 
-// Threads of a launch that fill the chip's 256 CUs four times over; beyond, a thread takes several
-// heads and makes its cosines and sines for all of them.
-constexpr int64_t kEnough = 256 * 2048 * 4;
+// A thread takes as many heads as make 96 bytes in and out, three at least, as long as there are threads
+// for 1024 on each of 256 CUs: its position and its cosines and sines are made once for them, and the
+// next head's values are on their way while one is turned.  14.5 thousand tokens of 40 + 8 heads of 128 in
+// BF16: 68 us with 2.7 or 3 heads a thread, 77 with 16; 4.3 thousand of 40 + 8 heads of 64, half of them
+// rotated: 14 us with 3, 20 with one.
+constexpr int64_t kEnough = 256 * 1024, kBytes = 96;
 
 template <typename T, int VEC>
 void launch(Rope& R, hipStream_t stream) {
@@ -157,7 +176,8 @@ void launch(Rope& R, hipStream_t stream) {
   R.rotated = C.rot_dim / 2 / VEC;
   R.copied = in_place ? 0 : (C.head_dim - C.rot_dim) / VEC;
   const int64_t each = C.n_tokens * (R.rotated + R.copied);
-  R.lanes = (uint32_t)std::max<int64_t>(1, std::min<int64_t>(R.heads, (kEnough + each - 1) / each));
+  constexpr int64_t kHeads = std::max<int64_t>(3, kBytes / (2 * VEC * sizeof(T)));
+  R.lanes = (uint32_t)std::min<int64_t>(R.heads, std::max((R.heads + kHeads - 1) / kHeads, (kEnough + each - 1) / each));
   const int64_t groups = (each * R.lanes + kThreads - 1) / kThreads, x = std::min<int64_t>(groups, 1 << 22);
   const dim3 grid((uint32_t)x, (uint32_t)((groups + x - 1) / x));
   if (C.layout == EP_ROPE_PAIRS) hipLaunchKernelGGL((rope_kernel<T, VEC, true>), grid, dim3(kThreads), 0, stream, R);

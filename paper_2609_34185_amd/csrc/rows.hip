@@ -360,15 +360,35 @@ __device__ __forceinline__ float exp_negative(float x) {
   const float f = __builtin_fmaf(x, 1.925963033e-8f, __builtin_fmaf(x, 1.44269502f, -n));
   return __builtin_ldexpf(__builtin_amdgcn_exp2f(f), (int)n);
 }
-// a / (1 + exp(-z)), by the exponential that does not overflow.  The quotient by one step of Newton's
-// on the instruction's reciprocal, which is within a unit.
-__device__ __forceinline__ float gated(float a, float z) {
-  const float e = exp_negative(-fabsf(z)), d = 1.0f + e;
-  float r = __builtin_amdgcn_rcpf(d);
-  r = __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r);
-  return (z < 0.0f ? a * e : a) * r;
+// 1 / d for d from 1 to 2^8, by one step of Newton's on the instruction's, which is within a unit.
+__device__ __forceinline__ float reciprocal(float d) {
+  const float r = __builtin_amdgcn_rcpf(d);
+  return __builtin_fmaf(__builtin_fmaf(-d, r, 1.0f), r, r);
 }
-__device__ __forceinline__ float gelu(float a) { return 0.5f * a * erfcf(-0.70710678118654752f * a); }
+// a / (1 + exp(-z)), by the exponential that does not overflow.
+__device__ __forceinline__ float gated(float a, float z) {
+  const float e = exp_negative(-fabsf(z));
+  return (z < 0.0f ? a * e : a) * reciprocal(1.0f + e);
+}
+// a Phi(a) = max(a, 0) - z Phi(-z) with z = |a|, and Phi(-z) = exp(-z^2 / 2) M(z).  M falls smoothly from
+// 1/2 to 1 / (z sqrt(2 pi)): t Q(t) with t = 1 / (1 + 0.24 z) and Q of degree 9, fitted for the least
+// relative error over 0 .. 14.6, where the exponential ends: 3e-9, and 7 2^-24 in FP32.  What z^2
+// loses when it is rounded moves the exponential by as much.
+__device__ __forceinline__ float gelu(float a) {
+  const float z = fminf(fabsf(a), 20.0f), sq = z * z, lost = __builtin_fmaf(z, z, -sq);
+  const float e = exp_negative(-0.5f * sq), t = reciprocal(__builtin_fmaf(0.24f, z, 1.0f));
+  float q = __builtin_fmaf(0.0255265534f, t, -0.124637879f);
+  q = __builtin_fmaf(q, t, 0.205476031f);
+  q = __builtin_fmaf(q, t, -0.144257292f);
+  q = __builtin_fmaf(q, t, 0.141432092f);
+  q = __builtin_fmaf(q, t, 0.028170027f);
+  q = __builtin_fmaf(q, t, 0.0877551958f);
+  q = __builtin_fmaf(q, t, 0.0889361501f);
+  q = __builtin_fmaf(q, t, 0.0958570391f);
+  q = __builtin_fmaf(q, t, 0.0957420841f);
+  const float h = q * t * __builtin_fmaf(e, -0.5f * lost, e);
+  return __builtin_fmaf(-z, h, a < 0.0f ? 0.0f : a);
+}
 // (1 + tanh z) / 2 is 1 / (1 + exp(-2 z))
 __device__ __forceinline__ float gelu_tanh(float a) { return gated(a, 1.5957691216057308f * __builtin_fmaf(0.044715f * a * a, a, a)); }
 
