@@ -229,8 +229,7 @@ __global__ __launch_bounds__(64 * KW) void ring_kernel(Product P, uint32_t heigh
 }
 
 // The tile of Y at row i0 of X and j0 of W.  Wave (ww, wx) of WW x WX owns NW x NX tiles of
-// 16 x 16; NS stages of operands are in LDS, written by direct loads while the stage before is
-// multiplied.
+// 16 x 16; NS stages of operands are in LDS, written by direct loads.
 template <int OUT, int NW, int NX, int WW, int WX, int NS>
 __device__ __forceinline__ void tile_product(const Product& P, uint32_t part, int64_t i0, int64_t j0, lds_u8* lds) {
   constexpr int kWaves = WW * WX, TW = 16 * NW * WW, TX = 16 * NX * WX;
@@ -273,29 +272,40 @@ __device__ __forceinline__ void tile_product(const Product& P, uint32_t part, in
   const uint32_t fs = swz(col);
   const uint32_t fo0 = 16 * (quarter ^ fs), fo1 = 16 * ((4 + quarter) ^ fs);
   const uint32_t fx = (16 * NX * wx + col) * 128, fw = (TX + 16 * NW * ww + col) * 128;
-  auto fragment = [&](const lds_u8* p) {
-    return Fragment{*reinterpret_cast<const __attribute__((address_space(3))) v4i*>(p + fo0),
-                    *reinterpret_cast<const __attribute__((address_space(3))) v4i*>(p + fo1)};
+  // The fragments of half a step (64 of k) are read while the half before is multiplied: without that the
+  // waves, which meet at a barrier every step, all read LDS and then all multiply.
+  struct Half {
+    v4i x[NX], w[NW];
+  };
+  const auto read = [&](Half& h, const lds_u8* p, uint32_t fo) {
+#pragma unroll
+    for (int t = 0; t < NX; t++) h.x[t] = *reinterpret_cast<const __attribute__((address_space(3))) v4i*>(p + fx + fo + 16 * 128 * t);
+#pragma unroll
+    for (int i = 0; i < NW; i++) h.w[i] = *reinterpret_cast<const __attribute__((address_space(3))) v4i*>(p + fw + fo + 16 * 128 * i);
+  };
+  const auto multiply = [&](const Half& h) {
+#pragma unroll
+    for (int i = 0; i < NW; i++)
+#pragma unroll
+      for (int t = 0; t < NX; t++) acc[i][t] = __builtin_amdgcn_mfma_i32_16x16x64_i8(h.w[i], h.x[t], acc[i][t], 0, 0, 0);
   };
 
 #pragma unroll
-  for (int s = 0; s < NS - 1; s++) fetch(b0 + s, s);
-  stage_barrier<(NS - 2) * kPerStep>();
+  for (int s = 0; s < NS; s++) fetch(b0 + s, s);
+  stage_barrier<(NS - 1) * kPerStep>();
+  Half first, second;
+  read(first, lds, fo0);
   uint32_t stage = 0;
   for (uint32_t b = b0; b < b1; b++) {
-    const lds_u8* const p = lds + kStage * stage;
-    fetch(b + NS - 1, stage == 0 ? NS - 1 : stage - 1);
-    Fragment xf[NX];
-#pragma unroll
-    for (int t = 0; t < NX; t++) xf[t] = fragment(p + fx + 16 * 128 * t);
-#pragma unroll
-    for (int i = 0; i < NW; i++) {
-      const Fragment wf = fragment(p + fw + 16 * 128 * i);
-#pragma unroll
-      for (int t = 0; t < NX; t++) acc[i][t] = tile_step(wf, xf[t], acc[i][t]);
-    }
+    const uint32_t next = stage + 1 == NS ? 0 : stage + 1;
+    read(second, lds + kStage * stage, fo1);
+    multiply(first);
+    // every wave has read this step, and the next one has landed; its place is free for the one NS later
     stage_barrier<(NS - 2) * kPerStep>();
-    stage = stage + 1 == NS ? 0 : stage + 1;
+    fetch(b + NS, stage);
+    read(first, lds + kStage * next, fo0);   // zeros after the last step
+    multiply(second);
+    stage = next;
   }
   __builtin_amdgcn_s_waitcnt(0);   // direct loads still in flight land before LDS is used again
   stage_scales<OUT>(P, j0, TW, lds);
@@ -453,10 +463,10 @@ void ring_launch(const Product& P, uint32_t height, hipStream_t stream) {
 // ---- which kernel -----------------------------------------------------------------------
 // Estimates of a launch's time in ns: what a step of 128 along k takes on the busiest CU, what a
 // workgroup takes besides (first loads, and the stores of a tile by its size), what the launch takes
-// besides, and never less than the operands' and outputs' way through memory.  Fitted to launches of 156
-// sizes (17 to 5000 rows, 310 to 17408 columns, k from 16 to 17408), each with every kernel and up to 16
-// shares of k; over them the choice is 1 % slower than the best (geometric mean), and 5 % at most where
-// the kernel and not the call is what takes the time.
+// besides, and never less than the operands' and outputs' way through memory.  Fitted to launches of 266
+// sizes (17 to 6000 rows, 64 to 18000 columns, k from 16 to 17600), each with every kernel and up to 16
+// shares of k; over them the choice is 1.3 % slower than the best (geometric mean), 22 % at most; a fit
+// to 156 of them is 2.4 % slower than the best over the others.
 enum Kernel { kRing16, kRing32, kRing64, kTile64, kTile128, kWideX, kWideW, kWideW64, kLarge };
 struct TileCost {
   Kernel kernel;
@@ -464,12 +474,14 @@ struct TileCost {
   int half, one, each;   // a CU with half a tile (of W's rows, the largest one's of X's), with one, and with more, for each
   int besides;
 };
-constexpr TileCost kTiles[] = {{kTile64, 128, 64, 255, 425, 330, 1975},    {kTile128, 128, 128, 385, 410, 700, 2700},
-                               {kWideX, 128, 256, 525, 735, 810, 4160},    {kWideW, 256, 128, 495, 815, 845, 4160},
-                               {kWideW64, 256, 64, 355, 420, 625, 2700},   {kLarge, 256, 256, 825, 860, 1095, 10400}};
-constexpr int kMostParts = 16;
-constexpr int kRing32Step = 95, kRing64Step = 182, kRingBesides = 1955, kLaunch = 3890, kRingLaunch = 2330;
-constexpr int kMemory = 5955, kJoin = 1640, kJoinValues = 855;   // bytes in a ns; a join, and the sums that it adds in a ns
+constexpr TileCost kTiles[] = {{kTile64, 128, 64, 220, 300, 340, 1910},    {kTile128, 128, 128, 375, 635, 650, 2580},
+                               {kWideX, 128, 256, 580, 695, 830, 3930},    {kWideW, 256, 128, 485, 830, 815, 3930},
+                               {kWideW64, 256, 64, 325, 330, 620, 2580},   {kLarge, 256, 256, 815, 1015, 1080, 11620}};
+constexpr int kMostParts = 16, kMemory = 5960;                      // kMemory, kJoinValues: bytes, and sums that are joined, in a ns
+constexpr int kLaunch = 4830, kJoin = 1610, kJoinValues = 1030;
+constexpr int kRing32Step = 125, kRing64Step = 211, kRingLaunch = 900;
+// of a streaming workgroup, for `columns` columns of a row group of 16 rows each
+constexpr int64_t ring_besides(int64_t columns, int groups) { return 1290 + 23 * columns * groups / 4; }
 
 struct Plan {
   Kernel kernel;
@@ -487,8 +499,8 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, int cus) {
   int64_t least = INT64_MAX;
   if (m <= 512) {
     const uint32_t h2 = ring_height<3, 2>(m, n, cus), h4 = ring_height<3, 4>(m, n, cus);
-    const int64_t t2 = (kRing32Step * kb + kRingBesides) * rounds((n + h2 - 1) / h2 * ((m + 31) / 32), cus);
-    const int64_t t4 = (kRing64Step * kb + kRingBesides) * rounds((n + h4 - 1) / h4 * ((m + 63) / 64), cus);
+    const int64_t t2 = (kRing32Step * kb + ring_besides(h2, 2)) * rounds((n + h2 - 1) / h2 * ((m + 31) / 32), cus);
+    const int64_t t4 = (kRing64Step * kb + ring_besides(h4, 4)) * rounds((n + h4 - 1) / h4 * ((m + 63) / 64), cus);
     best = t2 <= t4 ? Plan{kRing32, 1, kb, h2} : Plan{kRing64, 1, kb, h4};
     least = std::max(std::min(t2, t4), memory) + kRingLaunch;
   }
