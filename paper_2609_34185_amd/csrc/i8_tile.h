@@ -12,16 +12,10 @@
 // bytes, so that eight lanes cover one whole 128-byte line of a row.  (With
 // 64-byte row pieces each line is requested twice, in consecutive steps, and
 // a CU's stream of direct loads runs at about 60 % of the rate it reaches
-// with whole lines.)  Two stage buffers of 64 KiB alternate.  Per step s
-// (buffer s mod 2 holds step s, and step s + 1 is in flight):
-//   chunks 1..3: the MFMAs of chunk c - 1 while the fragments of chunk c are
-//           read;
-//   barrier (this wave's loads of step s + 1 landed, its LDS reads returned);
-//   then step s + 2 is requested into buffer s mod 2, which every wave has
-//   finished reading, and the MFMAs of chunk 3 run while the chunk-0
-//   fragments of step s + 1 are read.
-// A step's loads thus have a whole step of MFMAs to land.  The single barrier
-// sits between two MFMA groups whose operands are already in registers.
+// with whole lines.)  Five slots of 32 KiB, an operand's rows for one step each,
+// form a ring; its order stands at tile_product.  A step has one barrier, between
+// two MFMA groups whose operands are already in registers, and its loads have a
+// step of MFMAs or two to land.
 // Direct loads are bounded buffer loads: out-of-range chunks land as zeros.
 //
 // LDS rows are 128 bytes (eight 16-byte chunks) without padding; the chunk j

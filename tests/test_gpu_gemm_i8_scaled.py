@@ -75,6 +75,10 @@ SHAPES = [(1, 1, 16), (1, 17408, 5120), (1, 5120, 17408), (2, 7, 144), (15, 333,
           (32, 5120, 1024), (33, 129, 640), (61, 5120, 17408), (64, 300, 8192), (65, 64, 131056), (100, 2048, 5120), (128, 128, 128),
           (200, 17408, 512), (203, 5120, 2064), (257, 1025, 1040), (500, 63, 4096), (513, 5120, 1024), (1000, 3856, 272), (1024, 1024, 1024),
           (2048, 1300, 528), (2500, 4100, 64), (4441, 438, 1488)]
+# every tile size with whole tiles, with halves in the last round (one of them without a row) and with k shared out
+SHAPES += [(69, 4084, 16), (194, 4164, 160), (516, 8, 1872), (945, 2142, 1888), (1388, 2877, 352), (2989, 617, 144), (1189, 3508, 448),
+           (1464, 2657, 240), (2223, 930, 6352), (2601, 5855, 144), (552, 3658, 6128), (1570, 2546, 384), (455, 2089, 6320),
+           (2775, 4393, 928), (3842, 5192, 1040), (774, 5041, 5728)]
 
 
 @pytest.mark.parametrize("y_name", ["bf16", "fp16", "fp32"])
@@ -151,6 +155,26 @@ def test_product_repeats_its_bits_on_another_stream_and_in_a_graph(E, m, n, k):
         graph.replay()
         torch.cuda.synchronize()
         assert torch.equal(y, want), i
+
+
+def test_products_at_once(E):
+    """Two streams' calls side by side, each with a workspace of its own: the same bits as alone."""
+    sizes = [(203, 5120, 4096), (774, 5041, 5728), (9, 5120, 4096)]
+    streams = [torch.cuda.Stream() for _ in sizes]
+    calls = []
+    for i, (m, n, k) in enumerate(sizes):
+        x, xs, w, ws, b = inputs(m, n, k, 40 + i)
+        want = run(E, x, xs, w, ws, b, "bf16")
+        room = torch.empty(E.gemm_i8_scaled_workspace(m, n, k), dtype=torch.uint8, device="cuda")
+        calls.append((x, xs, w, ws, b, want, torch.zeros((8, m, n), dtype=torch.bfloat16, device="cuda"), room))
+    torch.cuda.synchronize()
+    for turn in range(8):
+        for (m, n, k), s, (x, xs, w, ws, b, _, y, room) in zip(sizes, streams, calls):
+            E.gemm_i8_scaled(x.data_ptr(), xs.data_ptr(), w.data_ptr(), ws.data_ptr(), y[turn].data_ptr(), m, n, k, d_bias=b.data_ptr(),
+                             d_ws=room.data_ptr(), ws_bytes=room.numel(), stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    for call in calls:
+        assert all(torch.equal(y, call[5]) for y in call[6])
 
 
 def test_product_of_a_decoded_container(E, oracle):

@@ -226,3 +226,36 @@ def test_rope_past_32_bit_offsets(E):
     assert torch.equal(q[-301:], y) and int((q != 0).sum()) == int((y != 0).sum())
     del q
     torch.cuda.empty_cache()
+
+
+def test_rope_in_a_graph(E):
+    """Captured on a stream of its own, in place and from lengths; replayed over other lengths: as called."""
+    n, dim, spare = 9, 64, 3
+    freqs = table(E, dim)
+    cu, lens = torch.empty(n + 1, dtype=torch.int32, device="cuda"), torch.empty(n, dtype=torch.int32, device="cuda")
+    rows = torch.empty((40, 6 * dim), dtype=torch.bfloat16, device="cuda")
+
+    def call():
+        E.rope(E.rope_call(rows.data_ptr(), rows.data_ptr(), freqs.data_ptr(), 40, 4, dim, E.BF16, d_k=rows.data_ptr() + 8 * dim, k_heads=1,
+                           d_k_out=rows.data_ptr() + 8 * dim, d_cu=cu.data_ptr(), d_len=lens.data_ptr(), n_req=n, q_row=6 * dim,
+                           q_out_row=6 * dim, k_row=6 * dim, k_out_row=6 * dim), stream())
+
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    rng = np.random.default_rng(12)
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        call()
+    for i in range(4):
+        new = rng.multinomial(40 - spare, np.ones(n) / n) * (rng.random(n) < 0.7)
+        cu.copy_(torch.from_numpy(np.concatenate(([0], np.cumsum(new)))))
+        lens.copy_(torch.from_numpy(new + rng.integers(0, 1 << 20, n)))
+        value = torch.randn(rows.shape, device="cuda").to(torch.bfloat16)
+        outs = []
+        for replayed in (False, True):
+            rows.copy_(value)
+            graph.replay() if replayed else call()
+            torch.cuda.synchronize()
+            outs.append(rows.clone())
+        total = int(new.sum())
+        assert torch.equal(*outs) and torch.equal(rows[total:], value[total:]) and torch.equal(rows[:, 5 * dim:], value[:, 5 * dim:]), i
+        assert not torch.equal(rows[:total, : 5 * dim], value[:total, : 5 * dim])

@@ -398,3 +398,39 @@ def test_row_operators_repeat_their_bits(E):
     for _ in range(3):
         for p, q in zip(first, norm_gpu(E, a, "e4m3")):
             assert torch.equal(p, q)
+
+
+@pytest.mark.parametrize("m,n", [(1, 5120), (67, 2064), (9, 256)])
+def test_row_operators_in_a_graph(E, m, n):
+    """Captured on a stream of their own and replayed over other inputs: norm (the stream in place, y over
+    x) and its product's other half, the activation and the quantiser, as called one by one."""
+    g = torch.Generator().manual_seed(m + n)
+    x, r, w, b = (torch.randn((rows, n), generator=g).to(torch.bfloat16).cuda() for rows in (m, m, 1, m))
+    y, codes, q = torch.empty_like(x), torch.empty_like(x, dtype=torch.uint8), torch.empty_like(x, dtype=torch.int8)
+    scale, rows = torch.empty((m, -(-n // 128)), device="cuda"), torch.empty(m, device="cuda")
+
+    def call():
+        s = stream()
+        E.norm(E.norm_call(x.data_ptr(), m, n, d_res=r.data_ptr(), d_res_out=r.data_ptr(), d_y=x.data_ptr(), d_w=w.data_ptr(), alpha=0.5), s)
+        E.glu(x.data_ptr(), b.data_ptr(), E.BF16, m, n, E.ACT_SILU, y.data_ptr(), stream=s)
+        E.glu(x.data_ptr(), b.data_ptr(), E.BF16, m, n, E.ACT_SILU, codes.data_ptr(), E.FP8_E4M3, scale.data_ptr(), stream=s)
+        E.quant_i8_row(y.data_ptr(), E.BF16, m, n, q.data_ptr(), rows.data_ptr(), stream=s)
+
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        call()
+    for i in range(4):
+        new = [torch.randn((m, n), generator=g).to(torch.bfloat16).cuda() for _ in range(3)]
+        outs = []
+        for replayed in (False, True):
+            for t, value in zip((x, r, b), new):
+                t.copy_(value)
+            for t in (y, codes, q, scale, rows):
+                t.zero_()
+            graph.replay() if replayed else call()
+            torch.cuda.synchronize()
+            outs.append([t.clone() for t in (x, r, y, codes, scale, q, rows)])
+        assert all(torch.equal(p, o) for p, o in zip(*outs)), i
+        h = (new[1].double() + 0.5 * new[0].double())
+        assert ((r.double() - h).abs() <= 2.0 ** -8 * h.abs() + 2.0 ** -22 * (new[1].double().abs() + new[0].double().abs())).all()
