@@ -329,19 +329,24 @@ __device__ __forceinline__ void tile_product(const Product& P, uint32_t part, in
   }
 }
 
-// Units [0, full) are whole tiles; the `split` last tiles are taken as two halves of W's rows each, so that
-// a last round of few tiles takes half as long.  Every unit is taken by `parts` workgroups, one for each
-// share of k, which follow each other on one XCD: they read the same rows of W or X.
+// Units [0, full) are whole tiles; the `split` last tiles are taken in `cut` pieces each, so that a last round
+// of few tiles is a short one: halves of W's rows, or quarters of half the rows of both.  Every unit is taken by
+// `parts` workgroups, one for each share of k, which follow each other on one XCD: they read the same rows of W
+// or X.
 struct Units {
-  uint32_t tw, tx, full, split;
-  // The unit and the share of k of this workgroup; whole tiles and halves are spread over the XCDs apart.
+  uint32_t tw, tx, full, split, cut;
+  // The unit and the share of k of this workgroup; whole tiles and pieces are spread over the XCDs apart.
   __device__ __forceinline__ void mine(uint32_t parts, uint32_t& unit, uint32_t& part) const {
     const uint32_t whole = full * parts;
-    const uint32_t id = blockIdx.x < whole ? xcd_spread(blockIdx.x, whole) : whole + xcd_spread(blockIdx.x - whole, 2 * split * parts);
+    const uint32_t id = blockIdx.x < whole ? xcd_spread(blockIdx.x, whole) : whole + xcd_spread(blockIdx.x - whole, cut * split * parts);
     unit = id / parts;
     part = id - unit * parts;
   }
 };
+// Pieces at most: quarters, where each of the workgroup's waves still has rows of both to load.
+template <int NW, int NX, int WW, int WX>
+constexpr int kMostCut = NW % 2 == 0 && NX % 2 == 0 && NX * WX % (WW * WX) == 0 && NW * WW % (WW * WX) == 0 ? 4 : 2;
+constexpr int kMostLarge = 8;
 template <int OUT, int NW, int NX, int WW, int WX, int NS>
 __global__ __launch_bounds__(64 * WW * WX) void tiles_kernel(Product P, Units U) {
   constexpr int TW = 16 * NW * WW, TX = 16 * NX * WX;
@@ -353,15 +358,19 @@ __global__ __launch_bounds__(64 * WW * WX) void tiles_kernel(Product P, Units U)
     tile_of(unit, U.tx, U.tw, ti, tj);
     tile_product<OUT, NW, NX, WW, WX, NS>(P, part, (int64_t)ti * TX, (int64_t)tj * TW, lds);
   } else {
-    const uint32_t u = unit - U.full;
-    tile_of(U.full + u / 2, U.tx, U.tw, ti, tj);
-    const int64_t j0 = (int64_t)tj * TW + TW / 2 * (u & 1);
-    if (j0 < P.n) tile_product<OUT, NW / 2, NX, WW, WX, NS>(P, part, (int64_t)ti * TX, j0, lds);
+    const uint32_t u = unit - U.full, piece = u % U.cut;
+    tile_of(U.full + u / U.cut, U.tx, U.tw, ti, tj);
+    const int64_t i0 = (int64_t)ti * TX + TX / 2 * (piece >> 1), j0 = (int64_t)tj * TW + TW / 2 * (piece & 1);
+    if (i0 >= P.m || j0 >= P.n) return;
+    if constexpr (kMostCut<NW, NX, WW, WX> == 4) {   // stages of half the size, twice as many
+      if (U.cut == 4) return tile_product<OUT, NW / 2, NX / 2, WW, WX, 2 * NS>(P, part, i0, j0, lds);
+    }
+    tile_product<OUT, NW / 2, NX, WW, WX, NS>(P, part, i0, j0, lds);
   }
 }
 
 // Many rows: tiles of 256 x 256 by four waves (i8_tile.h), W's rows as A so that a lane has four columns
-// of a row of Y side by side; halves are of X's rows.  Bound by power: 8192 x 5120 x 17408 to BF16 in 583 to
+// of a row of Y side by side; halves are of X's rows, quarters of 128 x 128 and eighths of 128 x 64.  Bound by power: 8192 x 5120 x 17408 to BF16 in 583 to
 // 600 us, 2.5 POP/s, as the product to int32 in the same tiles; the matrix unit is busy 70 % of the cycles.
 // Stores of a lane's four columns instead of whole lines take 604, with a load of its scales for each 680;
 // eight waves of 128 x 64, whose tiles of 16 x 16 read half as much LDS again for a product, 593.
@@ -400,12 +409,17 @@ __global__ __launch_bounds__(i8::kGemmThreads) void large_kernel(Product P, Unit
   U.mine(P.parts, unit, part);
   if (unit < U.full) {
     tile_of(unit, U.tw, U.tx, tj, ti);
-    large_tile<OUT, 256>(P, part, (int64_t)ti * 256, (int64_t)tj * 256, lds);
-  } else {
-    const uint32_t u = unit - U.full;
-    tile_of(U.full + u / 2, U.tw, U.tx, tj, ti);
-    large_tile<OUT, 128>(P, part, (int64_t)ti * 256 + 128 * (u & 1), (int64_t)tj * 256, lds);
+    return large_tile<OUT, 256>(P, part, (int64_t)ti * 256, (int64_t)tj * 256, lds);
   }
+  const uint32_t u = unit - U.full, piece = u % U.cut;
+  tile_of(U.full + u / U.cut, U.tw, U.tx, tj, ti);
+  int64_t i0 = (int64_t)ti * 256, j0 = (int64_t)tj * 256;
+  if (U.cut == 2) return large_tile<OUT, 128>(P, part, i0 + 128 * piece, j0, lds);
+  j0 += 128 * (piece & 1);
+  i0 += 256 / (U.cut / 2) * (piece >> 1);
+  if (i0 >= P.m || j0 >= P.n) return;
+  if (U.cut == 4) tile_product<OUT, 4, 4, 2, 2, 5>(P, part, i0, j0, lds);
+  else tile_product<OUT, 4, 2, 2, 2, 6>(P, part, i0, j0, lds);
 }
 
 // The parts' sums, scales, bias and rounding: a thread for four columns of a row.  Six parts of 203 x 5120, 25 MB,
@@ -429,20 +443,28 @@ __global__ __launch_bounds__(256) void join_kernel(Product P) {
   finish<OUT>(P, i, j, v);
 }
 
-Units units_of(const Product& P, int tw, int tx, int cus) {
+// How many pieces each of the last round's tiles is cut into: as many as leave no CU more than one piece.
+// 512 x 17408 x 5120 in 272 tiles of 128 x 256: 63 us with the last 16 in halves, 55 in quarters; 1024 x 17408 x
+// 5120 in as many of 256 x 256: 109 in halves, 103 in quarters, 93 in eighths.
+uint32_t cut_of(int64_t tiles, uint32_t most, int cus) {
+  uint32_t cut = most;
+  while (cut > 1 && cut * (tiles % cus) > cus) cut /= 2;
+  return cut;
+}
+Units units_of(const Product& P, int tw, int tx, uint32_t most, int cus) {
   const uint32_t x = (uint32_t)((P.m + tx - 1) / tx), w = (uint32_t)((P.n + tw - 1) / tw), tiles = x * w;
-  const uint32_t last = tiles % cus, split = P.parts == 1 && 2 * last <= (uint32_t)cus ? last : 0;
-  return {w, x, tiles - split, split};
+  const uint32_t cut = P.parts > 1 ? 1 : cut_of(tiles, most, cus), split = cut > 1 ? tiles % cus : 0;
+  return {w, x, tiles - split, split, cut};
 }
 template <int OUT, int NW, int NX, int WW, int WX, int NS>
 void tiles_launch(const Product& P, int cus, hipStream_t stream) {
-  const Units U = units_of(P, 16 * NW * WW, 16 * NX * WX, cus);
-  hipLaunchKernelGGL((tiles_kernel<OUT, NW, NX, WW, WX, NS>), dim3((U.full + 2 * U.split) * P.parts), dim3(64 * WW * WX), 0, stream, P, U);
+  const Units U = units_of(P, 16 * NW * WW, 16 * NX * WX, kMostCut<NW, NX, WW, WX>, cus);
+  hipLaunchKernelGGL((tiles_kernel<OUT, NW, NX, WW, WX, NS>), dim3((U.full + U.cut * U.split) * P.parts), dim3(64 * WW * WX), 0, stream, P, U);
 }
 template <int OUT>
 void large_launch(const Product& P, int cus, hipStream_t stream) {
-  const Units U = units_of(P, 256, 256, cus);
-  hipLaunchKernelGGL(large_kernel<OUT>, dim3((U.full + 2 * U.split) * P.parts), dim3(i8::kGemmThreads), 0, stream, P, U);
+  const Units U = units_of(P, 256, 256, kMostLarge, cus);
+  hipLaunchKernelGGL(large_kernel<OUT>, dim3((U.full + U.cut * U.split) * P.parts), dim3(i8::kGemmThreads), 0, stream, P, U);
 }
 
 // Rows of W for a workgroup of the streaming kernel: the multiple of 8 up to 16 NW that makes the
@@ -471,25 +493,33 @@ void ring_launch(const Product& P, uint32_t height, hipStream_t stream) {
 // ---- which kernel -----------------------------------------------------------------------
 // Estimates of a launch's time in ns: what a step of 128 along k takes on the busiest CU, what a
 // workgroup takes besides (first loads, and the stores of a tile by its size), what the launch takes
-// besides, and never less than the operands' and outputs' way through memory.  Fitted to launches of 266
-// sizes (17 to 6000 rows, 64 to 18000 columns, k from 16 to 17600), each with every kernel and up to 16
-// shares of k; over them the choice is 1.3 % slower than the best (geometric mean), 22 % at most; a fit
-// to 156 of them is 2.4 % slower than the best over the others.
+// besides, and never less than the operands' and outputs' way through memory.  Fitted to launches of 573
+// sizes (17 to 8200 rows, 64 to 18000 columns, k from 16 to 17600), each with every kernel and up to 16
+// shares of k; over them the choice is 1.4 % slower than the best (geometric mean), 37 % at most; fits
+// to 343 of them are 1.5 and 2.2 % slower than the best over the others.
 enum Kernel { kRing16, kRing32, kRing64, kTile64, kTile128, kWideX, kWideW, kWideW64, kLarge };
 struct TileCost {
   Kernel kernel;
   int rows_w, rows_x;
+  uint32_t most;         // pieces of a tile of the last round
   int half, one, each;   // a CU with half a tile (of W's rows, the largest one's of X's), with one, and with more, for each
   int besides;
 };
-constexpr TileCost kTiles[] = {{kTile64, 128, 64, 220, 300, 340, 1910},    {kTile128, 128, 128, 375, 635, 650, 2580},
-                               {kWideX, 128, 256, 580, 695, 830, 3930},    {kWideW, 256, 128, 485, 830, 815, 3930},
-                               {kWideW64, 256, 64, 325, 330, 620, 2580},   {kLarge, 256, 256, 815, 1015, 1080, 11620}};
+constexpr TileCost kTiles[] = {{kTile64, 128, 64, kMostCut<4, 2, 2, 2>, 227, 344, 356, 2230},
+                               {kTile128, 128, 128, kMostCut<4, 4, 2, 2>, 377, 513, 715, 2730},
+                               {kWideX, 128, 256, kMostCut<4, 4, 2, 4>, 521, 782, 913, 3710},
+                               {kWideW, 256, 128, kMostCut<4, 4, 4, 2>, 517, 965, 904, 3710},
+                               {kWideW64, 256, 64, kMostCut<4, 2, 4, 2>, 360, 580, 682, 2730},
+                               {kLarge, 256, 256, kMostLarge, 763, 1208, 1214, 12890}};
+// In percent, by log2 of the pieces: a last round's share of a whole one's time, and of halves' where it is the only one;
+// the least that a step of a last round of pieces takes.
+constexpr int kLeast = 188;
+constexpr int kShare[] = {100, 50, 32, 27}, kAlone[] = {0, 100, 73, 50};
 constexpr int kMostParts = 16, kMemory = 5960;                      // kMemory, kJoinValues: bytes, and sums that are joined, in a ns
-constexpr int kLaunch = 4830, kJoin = 1610, kJoinValues = 1030;
-constexpr int kRing32Step = 125, kRing64Step = 211, kRingLaunch = 900;
+constexpr int kLaunch = 4880, kJoin = 764, kJoinValues = 951;
+constexpr int kRing32Step = 105, kRing64Step = 195, kRingLaunch = 1090;
 // of a streaming workgroup, for `columns` columns of a row group of 16 rows each
-constexpr int64_t ring_besides(int64_t columns, int groups) { return 1290 + 23 * columns * groups / 4; }
+constexpr int64_t ring_besides(int64_t columns, int groups) { return 1800 + 35 * columns * groups / 4; }
 
 struct Plan {
   Kernel kernel;
@@ -518,9 +548,17 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, int cus) {
     for (uint32_t p = 1; p <= most && p <= kb; p++) {
       const uint32_t steps = (kb + p - 1) / p;
       if ((kb + steps - 1) / steps != p) continue;   // the last parts would be empty
-      const int64_t halves = p == 1 ? rounds(2 * tiles, cus) : 2 * rounds(tiles * p, cus);
-      const int64_t step = halves == 1 ? c.half : std::max<int64_t>(c.one, c.each * halves / 2);
-      int64_t time = std::max(step * steps + c.besides * halves / 2, memory) + kLaunch;
+      int64_t whole = rounds(tiles * p, cus), share = 0, step = 0;   // rounds of whole tiles, percent of one
+      if (p == 1 && tiles % cus) {
+        const int cut = __builtin_ctz(cut_of(tiles, c.most, cus));
+        if (cut) {
+          whole--;
+          share = kShare[cut];
+          step = whole ? std::max<int64_t>(c.each * share / 100, kLeast) : c.half * kAlone[cut] / 100;
+        }
+      }
+      if (whole) step = std::max<int64_t>(c.one, c.each * whole + step);
+      int64_t time = std::max(step * steps + c.besides * (100 * whole + share) / 100, memory) + kLaunch;
       if (p > 1) time += kJoin + p * m * n / kJoinValues;
       if (time < least) {
         least = time;

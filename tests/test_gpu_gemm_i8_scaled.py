@@ -79,6 +79,10 @@ SHAPES = [(1, 1, 16), (1, 17408, 5120), (1, 5120, 17408), (2, 7, 144), (15, 333,
 SHAPES += [(69, 4084, 16), (194, 4164, 160), (516, 8, 1872), (945, 2142, 1888), (1388, 2877, 352), (2989, 617, 144), (1189, 3508, 448),
            (1464, 2657, 240), (2223, 930, 6352), (2601, 5855, 144), (552, 3658, 6128), (1570, 2546, 384), (455, 2089, 6320),
            (2775, 4393, 928), (3842, 5192, 1040), (774, 5041, 5728)]
+# quarters and eighths in the last round, alone and after whole tiles
+SHAPES += [(166, 678, 16), (546, 9, 272), (195, 8750, 1680), (4483, 9, 144), (524, 7215, 80), (269, 4140, 176), (915, 8642, 16), (3093, 3118, 16),
+           (4335, 257, 16), (2218, 4434, 16), (520, 8757, 1712), (2874, 7002, 1184), (2260, 8505, 1424), (2569, 6250, 1696), (4498, 9, 3488),
+           (564, 8, 2800), (74, 8558, 5872)]
 
 
 @pytest.mark.parametrize("y_name", ["bf16", "fp16", "fp32"])
