@@ -496,30 +496,30 @@ void ring_launch(const Product& P, uint32_t height, hipStream_t stream) {
 // besides, and never less than the operands' and outputs' way through memory.  Fitted to launches of 573
 // sizes (17 to 8200 rows, 64 to 18000 columns, k from 16 to 17600), each with every kernel and up to 16
 // shares of k; over them the choice is 1.4 % slower than the best (geometric mean), 37 % at most; fits
-// to 343 of them are 1.5 and 2.2 % slower than the best over the others.
+// to 343 of them are 1.7 and 1.9 % slower than the best over the others.
 enum Kernel { kRing16, kRing32, kRing64, kTile64, kTile128, kWideX, kWideW, kWideW64, kLarge };
 struct TileCost {
   Kernel kernel;
   int rows_w, rows_x;
   uint32_t most;         // pieces of a tile of the last round
-  int half, one, each;   // a CU with half a tile (of W's rows, the largest one's of X's), with one, and with more, for each
+  int half, one, each;   // a CU with half a tile (of W's rows, the largest one's of X's), with one, and with more than one, for each
   int besides;
 };
-constexpr TileCost kTiles[] = {{kTile64, 128, 64, kMostCut<4, 2, 2, 2>, 227, 344, 356, 2230},
-                               {kTile128, 128, 128, kMostCut<4, 4, 2, 2>, 377, 513, 715, 2730},
-                               {kWideX, 128, 256, kMostCut<4, 4, 2, 4>, 521, 782, 913, 3710},
-                               {kWideW, 256, 128, kMostCut<4, 4, 4, 2>, 517, 965, 904, 3710},
-                               {kWideW64, 256, 64, kMostCut<4, 2, 4, 2>, 360, 580, 682, 2730},
-                               {kLarge, 256, 256, kMostLarge, 763, 1208, 1214, 12890}};
+constexpr TileCost kTiles[] = {{kTile64, 128, 64, kMostCut<4, 2, 2, 2>, 200, 318, 299, 2040},
+                               {kTile128, 128, 128, kMostCut<4, 4, 2, 2>, 339, 587, 704, 2460},
+                               {kWideX, 128, 256, kMostCut<4, 4, 2, 4>, 497, 808, 973, 3290},
+                               {kWideW, 256, 128, kMostCut<4, 4, 4, 2>, 454, 825, 927, 3290},
+                               {kWideW64, 256, 64, kMostCut<4, 2, 4, 2>, 381, 615, 699, 2460},
+                               {kLarge, 256, 256, kMostLarge, 751, 1173, 1231, 12840}};
 // In percent, by log2 of the pieces: a last round's share of a whole one's time, and of halves' where it is the only one;
 // the least that a step of a last round of pieces takes.
-constexpr int kLeast = 188;
-constexpr int kShare[] = {100, 50, 32, 27}, kAlone[] = {0, 100, 73, 50};
+constexpr int kLeast = 185;
+constexpr int kShare[] = {100, 50, 30, 24}, kAlone[] = {0, 100, 70, 50};
 constexpr int kMostParts = 16, kMemory = 5960;                      // kMemory, kJoinValues: bytes, and sums that are joined, in a ns
-constexpr int kLaunch = 4880, kJoin = 764, kJoinValues = 951;
-constexpr int kRing32Step = 105, kRing64Step = 195, kRingLaunch = 1090;
+constexpr int kLaunch = 5700, kJoin = 587, kJoinValues = 895;
+constexpr int kRing32Step = 107, kRing64Step = 212, kRingLaunch = 916;
 // of a streaming workgroup, for `columns` columns of a row group of 16 rows each
-constexpr int64_t ring_besides(int64_t columns, int groups) { return 1800 + 35 * columns * groups / 4; }
+constexpr int64_t ring_besides(int64_t columns, int groups) { return 1990 + 31 * columns * groups / 4; }
 
 struct Plan {
   Kernel kernel;
@@ -548,7 +548,7 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, int cus) {
     for (uint32_t p = 1; p <= most && p <= kb; p++) {
       const uint32_t steps = (kb + p - 1) / p;
       if ((kb + steps - 1) / steps != p) continue;   // the last parts would be empty
-      int64_t whole = rounds(tiles * p, cus), share = 0, step = 0;   // rounds of whole tiles, percent of one
+      int64_t whole = rounds(tiles * p, cus), share = 0, step = 0;   // rounds of whole tiles, percent of one in pieces
       if (p == 1 && tiles % cus) {
         const int cut = __builtin_ctz(cut_of(tiles, c.most, cus));
         if (cut) {
@@ -557,7 +557,7 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, int cus) {
           step = whole ? std::max<int64_t>(c.each * share / 100, kLeast) : c.half * kAlone[cut] / 100;
         }
       }
-      if (whole) step = std::max<int64_t>(c.one, c.each * whole + step);
+      if (whole) step = whole == 1 && !share ? c.one : c.each * whole + step;
       int64_t time = std::max(step * steps + c.besides * (100 * whole + share) / 100, memory) + kLaunch;
       if (p > 1) time += kJoin + p * m * n / kJoinValues;
       if (time < least) {

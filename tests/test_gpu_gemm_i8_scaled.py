@@ -82,7 +82,8 @@ SHAPES += [(69, 4084, 16), (194, 4164, 160), (516, 8, 1872), (945, 2142, 1888), 
 # quarters and eighths in the last round, alone and after whole tiles
 SHAPES += [(166, 678, 16), (546, 9, 272), (195, 8750, 1680), (4483, 9, 144), (524, 7215, 80), (269, 4140, 176), (915, 8642, 16), (3093, 3118, 16),
            (4335, 257, 16), (2218, 4434, 16), (520, 8757, 1712), (2874, 7002, 1184), (2260, 8505, 1424), (2569, 6250, 1696), (4498, 9, 3488),
-           (564, 8, 2800), (74, 8558, 5872)]
+           (564, 8, 2800), (74, 8558, 5872), (2861, 4105, 1168), (3807, 5487, 1344), (68, 8401, 6192), (133, 8333, 16), (154, 5746, 5696),
+           (3510, 3415, 16), (3204, 4869, 16), (4704, 9, 6224), (1303, 1282, 16), (2480, 1572, 544), (386, 8270, 16), (650, 5897, 8192)]
 
 
 @pytest.mark.parametrize("y_name", ["bf16", "fp16", "fp32"])
