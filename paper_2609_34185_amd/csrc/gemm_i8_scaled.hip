@@ -97,25 +97,25 @@ struct Block {
   }
   // the block's rows below m and columns below n to row i and column j of Y, or of the part's sums
   __device__ __forceinline__ void store(const Product& P, uint32_t part, int64_t i, int64_t j, int lane) const {
-    constexpr int kPerRow = COLS * kSize<OUT> / 16, kRows = 64 / kPerRow, kEach = 16 / kSize<OUT>;
-    static_assert(64 % kPerRow == 0 && ROWS % kRows == 0, "block");
+    constexpr int kPerRow = COLS * kSize<OUT> / 16, kEach = 16 / kSize<OUT>;   // pieces of 16 bytes
     asm volatile("" ::: "memory");
     const int64_t ld = OUT == kSums ? P.sums_ld : P.n;
     uint8_t* const to = (OUT == kSums ? reinterpret_cast<uint8_t*>(P.sums + (int64_t)part * P.m * ld) : static_cast<uint8_t*>(P.y)) +
                         (i * ld + j) * kSize<OUT>;
     typedef typename std::conditional<kSize<OUT> == 2, uint16_t, uint32_t>::type element;
-    const lds_u8* const from = lds + lane / kPerRow * kPitch + 16 * (lane % kPerRow);
-    const int64_t left = ld - j - kEach * (lane % kPerRow);   // columns from this lane's on
 #pragma unroll
-    for (int r = 0; r < ROWS; r += kRows) {
-      uint8_t* const at = to + (r + lane / kPerRow) * ld * kSize<OUT> + 16 * (lane % kPerRow);
-      if (i + r + lane / kPerRow >= P.m) continue;
+    for (int r = 0; r < ROWS * kPerRow; r += 64) {
+      const int row = 64 % kPerRow ? (r + lane) / kPerRow : r / kPerRow + lane / kPerRow, c = 64 % kPerRow ? (r + lane) % kPerRow : lane % kPerRow;
+      if ((ROWS * kPerRow % 64 && r + lane >= ROWS * kPerRow) || i + row >= P.m) continue;
+      const lds_u8* const from = lds + row * kPitch + 16 * c;
+      uint8_t* const at = to + row * ld * kSize<OUT> + 16 * c;
+      const int64_t left = ld - j - kEach * c;   // columns from this lane's on
       if (left >= kEach) {
-        const v4u v = *(const __attribute__((address_space(3))) v4u*)(from + r * kPitch);
+        const v4u v = *(const __attribute__((address_space(3))) v4u*)from;
         __builtin_memcpy(reinterpret_cast<element*>(at), &v, 16);   // rows of Y begin at any element
       } else {
         for (int e = 0; e < left; e++)
-          reinterpret_cast<element*>(at)[e] = *(const __attribute__((address_space(3))) element*)(from + r * kPitch + e * kSize<OUT>);
+          reinterpret_cast<element*>(at)[e] = *(const __attribute__((address_space(3))) element*)(from + e * kSize<OUT>);
       }
     }
     asm volatile("" ::: "memory");
@@ -343,9 +343,14 @@ struct Units {
     part = id - unit * parts;
   }
 };
-// Pieces at most: quarters, where each of the workgroup's waves still has rows of both to load.
+// What a tile is cut into: halves of W's rows or of X's, and quarters of both, where every wave of the workgroup
+// still has rows of both to load.
 template <int NW, int NX, int WW, int WX>
-constexpr int kMostCut = NW % 2 == 0 && NX % 2 == 0 && NX * WX % (WW * WX) == 0 && NW * WW % (WW * WX) == 0 ? 4 : 2;
+constexpr bool kCutW = NW % 2 == 0 && 16 * NW / 2 * WW % (8 * WW * WX) == 0;
+template <int NW, int NX, int WW, int WX>
+constexpr bool kCutX = NX % 2 == 0 && 16 * NX / 2 * WX % (8 * WW * WX) == 0;
+template <int NW, int NX, int WW, int WX>
+constexpr int kMostCut = (kCutW<NW, NX, WW, WX> ? 2 : 1) * (kCutX<NW, NX, WW, WX> ? 2 : 1);
 constexpr int kMostLarge = 8;
 template <int OUT, int NW, int NX, int WW, int WX, int NS>
 __global__ __launch_bounds__(64 * WW * WX) void tiles_kernel(Product P, Units U) {
@@ -358,14 +363,16 @@ __global__ __launch_bounds__(64 * WW * WX) void tiles_kernel(Product P, Units U)
     tile_of(unit, U.tx, U.tw, ti, tj);
     tile_product<OUT, NW, NX, WW, WX, NS>(P, part, (int64_t)ti * TX, (int64_t)tj * TW, lds);
   } else {
+    constexpr bool kW = kCutW<NW, NX, WW, WX>, kX = kCutX<NW, NX, WW, WX>;
     const uint32_t u = unit - U.full, piece = u % U.cut;
     tile_of(U.full + u / U.cut, U.tx, U.tw, ti, tj);
-    const int64_t i0 = (int64_t)ti * TX + TX / 2 * (piece >> 1), j0 = (int64_t)tj * TW + TW / 2 * (piece & 1);
+    const int64_t i0 = (int64_t)ti * TX + (kX ? TX / 2 * (kW ? piece >> 1 : piece) : 0), j0 = (int64_t)tj * TW + (kW ? TW / 2 * (piece & 1) : 0);
     if (i0 >= P.m || j0 >= P.n) return;
-    if constexpr (kMostCut<NW, NX, WW, WX> == 4) {   // stages of half the size, twice as many
+    if constexpr (kW && kX) {   // stages of half the size, twice as many
       if (U.cut == 4) return tile_product<OUT, NW / 2, NX / 2, WW, WX, 2 * NS>(P, part, i0, j0, lds);
     }
-    tile_product<OUT, NW / 2, NX, WW, WX, NS>(P, part, i0, j0, lds);
+    if constexpr (kW) tile_product<OUT, NW / 2, NX, WW, WX, NS>(P, part, i0, j0, lds);
+    else if constexpr (kX) tile_product<OUT, NW, NX / 2, WW, WX, NS>(P, part, i0, j0, lds);
   }
 }
 
@@ -493,33 +500,36 @@ void ring_launch(const Product& P, uint32_t height, hipStream_t stream) {
 // ---- which kernel -----------------------------------------------------------------------
 // Estimates of a launch's time in ns: what a step of 128 along k takes on the busiest CU, what a
 // workgroup takes besides (first loads, and the stores of a tile by its size), what the launch takes
-// besides, and never less than the operands' and outputs' way through memory.  Fitted to launches of 573
+// besides, and never less than the operands' and outputs' way through memory.  Fitted to launches of 574
 // sizes (17 to 8200 rows, 64 to 18000 columns, k from 16 to 17600), each with every kernel and up to 16
-// shares of k; over them the choice is 1.4 % slower than the best (geometric mean), 37 % at most; fits
-// to 343 of them are 1.7 and 1.9 % slower than the best over the others.
-enum Kernel { kRing16, kRing32, kRing64, kTile64, kTile128, kWideX, kWideW, kWideW64, kLarge };
+// shares of k; over them the choice is 1.2 % slower than the best (geometric mean), 34 % at most; fits
+// to 344 of them are 1.4 and 1.7 % slower than the best over the others.  Tiles of 192 rows of W are worth 1.5 %
+// of the best: 1703 x 4857 x 1872 takes 24 us in 192 x 192, 31 without.
+enum Kernel { kRing16, kRing32, kRing64, kTile64, kTile128, kWideX, kWideW, kWideW64, k192x128, k192x192, kLarge };
 struct TileCost {
   Kernel kernel;
   int rows_w, rows_x;
   uint32_t most;         // pieces of a tile of the last round
-  int half, one, each;   // a CU with half a tile (of W's rows, the largest one's of X's), with one, and with more than one, for each
+  int half, one, each;   // a CU with half a tile, with one, and with more than one, for each
   int besides;
 };
-constexpr TileCost kTiles[] = {{kTile64, 128, 64, kMostCut<4, 2, 2, 2>, 200, 318, 299, 2040},
-                               {kTile128, 128, 128, kMostCut<4, 4, 2, 2>, 339, 587, 704, 2460},
-                               {kWideX, 128, 256, kMostCut<4, 4, 2, 4>, 497, 808, 973, 3290},
-                               {kWideW, 256, 128, kMostCut<4, 4, 4, 2>, 454, 825, 927, 3290},
-                               {kWideW64, 256, 64, kMostCut<4, 2, 4, 2>, 381, 615, 699, 2460},
-                               {kLarge, 256, 256, kMostLarge, 751, 1173, 1231, 12840}};
+constexpr TileCost kTiles[] = {{kTile64, 128, 64, kMostCut<4, 2, 2, 2>, 204, 353, 328, 2280},
+                               {kTile128, 128, 128, kMostCut<4, 4, 2, 2>, 355, 679, 767, 2780},
+                               {kWideX, 128, 256, kMostCut<4, 4, 2, 4>, 514, 844, 939, 3790},
+                               {kWideW, 256, 128, kMostCut<4, 4, 4, 2>, 488, 806, 1017, 3790},
+                               {kWideW64, 256, 64, kMostCut<4, 2, 4, 2>, 300, 553, 709, 2780},
+                               {k192x128, 192, 128, kMostCut<3, 4, 4, 2>, 453, 609, 863, 3290},
+                               {k192x192, 192, 192, kMostCut<6, 3, 2, 4>, 0, 895, 1003, 4040},
+                               {kLarge, 256, 256, kMostLarge, 791, 1049, 1144, 15150}};
 // In percent, by log2 of the pieces: a last round's share of a whole one's time, and of halves' where it is the only one;
 // the least that a step of a last round of pieces takes.
-constexpr int kLeast = 185;
-constexpr int kShare[] = {100, 50, 30, 24}, kAlone[] = {0, 100, 70, 50};
+constexpr int kLeast = 195;
+constexpr int kShare[] = {100, 50, 30, 19}, kAlone[] = {0, 100, 69, 50};
 constexpr int kMostParts = 16, kMemory = 5960;                      // kMemory, kJoinValues: bytes, and sums that are joined, in a ns
-constexpr int kLaunch = 5700, kJoin = 587, kJoinValues = 895;
-constexpr int kRing32Step = 107, kRing64Step = 212, kRingLaunch = 916;
+constexpr int kLaunch = 5330, kJoin = 647, kJoinValues = 958;
+constexpr int kRing32Step = 108, kRing64Step = 220, kRingLaunch = 870;
 // of a streaming workgroup, for `columns` columns of a row group of 16 rows each
-constexpr int64_t ring_besides(int64_t columns, int groups) { return 1990 + 31 * columns * groups / 4; }
+constexpr int64_t ring_besides(int64_t columns, int groups) { return 2030 + 8 * columns * groups; }
 
 struct Plan {
   Kernel kernel;
@@ -579,6 +589,8 @@ void tile_launch(Kernel kernel, const Product& P, int cus, hipStream_t stream) {
   else if (kernel == kWideX) tiles_launch<OUT, 4, 4, 2, 4, 3>(P, cus, stream);
   else if (kernel == kWideW) tiles_launch<OUT, 4, 4, 4, 2, 3>(P, cus, stream);
   else if (kernel == kWideW64) tiles_launch<OUT, 4, 2, 4, 2, 4>(P, cus, stream);
+  else if (kernel == k192x128) tiles_launch<OUT, 3, 4, 4, 2, 4>(P, cus, stream);
+  else if (kernel == k192x192) tiles_launch<OUT, 6, 3, 2, 4, 3>(P, cus, stream);
   else large_launch<OUT>(P, cus, stream);
 }
 

@@ -84,6 +84,9 @@ SHAPES += [(166, 678, 16), (546, 9, 272), (195, 8750, 1680), (4483, 9, 144), (52
            (4335, 257, 16), (2218, 4434, 16), (520, 8757, 1712), (2874, 7002, 1184), (2260, 8505, 1424), (2569, 6250, 1696), (4498, 9, 3488),
            (564, 8, 2800), (74, 8558, 5872), (2861, 4105, 1168), (3807, 5487, 1344), (68, 8401, 6192), (133, 8333, 16), (154, 5746, 5696),
            (3510, 3415, 16), (3204, 4869, 16), (4704, 9, 6224), (1303, 1282, 16), (2480, 1572, 544), (386, 8270, 16), (650, 5897, 8192)]
+# tiles of 192 rows of W, and what else is chosen beside them
+SHAPES += [(1435, 8685, 1168), (3472, 5081, 1696), (644, 8374, 16), (1810, 8444, 16), (2088, 5490, 16), (1356, 6789, 16), (3586, 2067, 16),
+           (3077, 543, 16), (4921, 1583, 16), (3347, 4705, 16), (1703, 4857, 1872), (7420, 1058, 1008), (4228, 2875, 16), (1154, 2311, 16816)]
 
 
 @pytest.mark.parametrize("y_name", ["bf16", "fp16", "fp32"])
