@@ -230,10 +230,10 @@ __global__ __launch_bounds__(64 * KW) void ring_kernel(Product P, uint32_t heigh
 }
 
 // The tile of Y at row i0 of X and j0 of W.  Wave (ww, wx) of WW x WX owns NW x NX tiles of
-// 16 x 16; NS stages of operands are in LDS, written by direct loads.  203 x 5120 x 17408 in 6 shares of k: 29 us, of
-// which 18 are the 117 MB that come from memory (W once, X once for each XCD) and 5 the sums' 25 MB; the matrix
-// unit is busy a quarter of the cycles and LDS 15 %.  More of W in flight and less of X, by waves of their own
-// for each, takes 5 us more; tiles of half W's rows in half the shares, 4 more.
+// 16 x 16; NS stages of operands are in LDS, written by direct loads.  203 x 5120 x 17408 in tiles of
+// 192 x 128 and 4 shares of k: 30 us, of which 25 are the 131 MB that come from memory (W, X for each XCD, and some of
+// W for its second tile of X) and 3 the sums' 17 MB; the matrix unit is busy a quarter of the cycles and LDS 15 %.
+// More of W in flight and less of X, by waves of their own for each, takes 5 us more.
 template <int OUT, int NW, int NX, int WW, int WX, int NS>
 __device__ __forceinline__ void tile_product(const Product& P, uint32_t part, int64_t i0, int64_t j0, lds_u8* lds) {
   constexpr int kWaves = WW * WX, TW = 16 * NW * WW, TX = 16 * NX * WX;
@@ -429,8 +429,8 @@ __global__ __launch_bounds__(i8::kGemmThreads) void large_kernel(Product P, Unit
   else tile_product<OUT, 4, 2, 2, 2, 6>(P, part, i0, j0, lds);
 }
 
-// The parts' sums, scales, bias and rounding: a thread for four columns of a row.  Six parts of 203 x 5120, 25 MB,
-// in 7 us, half of it the launch.
+// The parts' sums, scales, bias and rounding: a thread for four columns of a row.  Four parts of 203 x 5120, 17 MB,
+// in 6 us, most of it the launch.
 template <int OUT>
 __global__ __launch_bounds__(256) void join_kernel(Product P) {
   const uint32_t per_row = (uint32_t)(P.sums_ld / 4), id = blockIdx.x * 256 + threadIdx.x;   // below 2^31
@@ -537,7 +537,7 @@ struct Plan {
 };
 
 // A launch of few tiles shares k out over workgroups, whose sums another launch joins.
-// 203 x 5120 x 17408 in tiles of 128 x 256, 40 of them: 39 us in 6 parts, 100 in one, 48 in tiles of half the size.
+// 203 x 5120 x 17408 in tiles of 192 x 128, 54 of them: 37.6 us in 4 parts, 70.6 in one; in 128 x 256, 40 of them: 37.9 in 5.
 Plan plan_of(int64_t m, int64_t n, int64_t k, int cus) {
   const uint32_t kb = (uint32_t)((k + 127) / 128);
   if (m <= 16) return {kRing16, 1, kb, ring_height<2, 1>(m, n, cus)};
