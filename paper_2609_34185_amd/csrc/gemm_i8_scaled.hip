@@ -555,10 +555,14 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, int cus) {
   for (const TileCost& c : kTiles) {
     const int64_t tiles = (m + c.rows_x - 1) / c.rows_x * ((n + c.rows_w - 1) / c.rows_w);
     const uint32_t most = tiles >= cus ? 1 : (uint32_t)std::min<int64_t>(kMostParts, 4 * cus / tiles);
+    int64_t filled = rounds(tiles, cus);
     for (uint32_t p = 1; p <= most && p <= kb; p++) {
+      const int64_t join = p > 1 ? kJoin + p * m * n / kJoinValues : 0;
+      if (memory + kLaunch + join >= least) break;   // and more parts take longer still
+      if (tiles * p > filled * cus) filled++;        // more than one part: of fewer tiles than CUs
       const uint32_t steps = (kb + p - 1) / p;
       if ((kb + steps - 1) / steps != p) continue;   // the last parts would be empty
-      int64_t whole = rounds(tiles * p, cus), share = 0, step = 0;   // rounds of whole tiles, percent of one in pieces
+      int64_t whole = filled, share = 0, step = 0;   // rounds of whole tiles, percent of one in pieces
       if (p == 1 && tiles % cus) {
         const int cut = __builtin_ctz(cut_of(tiles, c.most, cus));
         if (cut) {
@@ -568,8 +572,7 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, int cus) {
         }
       }
       if (whole) step = whole == 1 && !share ? c.one : c.each * whole + step;
-      int64_t time = std::max(step * steps + c.besides * (100 * whole + share) / 100, memory) + kLaunch;
-      if (p > 1) time += kJoin + p * m * n / kJoinValues;
+      const int64_t time = std::max(step * steps + c.besides * (100 * whole + share) / 100, memory) + kLaunch + join;
       if (time < least) {
         least = time;
         best = {c.kernel, p, steps, 0};
