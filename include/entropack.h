@@ -711,7 +711,9 @@ enum ep_act {
  * elements of x_dtype (EP_BF16, EP_FP16 or EP_FP32), a_row and b_row elements from one row
  * to the next, 16-byte aligned, so that both may lie in one fused projection's output; d_y:
  * m x n of y_dtype, row-major, 16-byte aligned, as ep_norm's y, with d_y_scale for 8-bit
- * ones.  Computed in FP32, rounded or quantised once.  m may be 0 (nothing is done).
+ * ones.  Computed in FP32, rounded or quantised once.  A NaN stays one and act(-inf) is
+ * one, as the formulas have it, in every y_dtype: an 8-bit y gets a NaN as its scale.
+ * m may be 0 (nothing is done).
  * Asynchronous on hip_stream, no allocation, one launch.
  * Errors: EP_ERR_ARG (null or misaligned pointers, m outside 0 .. 2^31 - 1, n outside
  * 8 .. 65536, n % 8, or n % 16 with an 8-bit y, short or misaligned rows, another dtype

@@ -381,7 +381,8 @@ __device__ __forceinline__ float gated(float a, float z) {
 // a Phi(a) = max(a, 0) - z Phi(-z) with z = |a|, and Phi(-z) = exp(-z^2 / 2) M(z).  M falls smoothly from
 // 1/2 to 1 / (z sqrt(2 pi)): t Q(t) with t = 1 / (1 + 0.24 z) and Q of degree 9, fitted for the least
 // relative error over 0 .. 14.6, where the exponential ends: 3e-9, and 7 2^-24 in FP32.  What z^2
-// loses when it is rounded moves the exponential by as much.
+// loses when it is rounded moves the exponential by as much.  max(a, 0) takes a negative a times -0: of -inf
+// the product is the NaN that the formula's -inf 0 is, where z and h, which are bounded, would make it 0.
 __device__ __forceinline__ float gelu(float a) {
   const float z = fminf(fabsf(a), 20.0f), sq = z * z, lost = __builtin_fmaf(z, z, -sq);
   const float e = exp_negative(-0.5f * sq), t = reciprocal(__builtin_fmaf(0.24f, z, 1.0f));
@@ -395,7 +396,7 @@ __device__ __forceinline__ float gelu(float a) {
   q = __builtin_fmaf(q, t, 0.0958570391f);
   q = __builtin_fmaf(q, t, 0.0957420841f);
   const float h = q * t * __builtin_fmaf(e, -0.5f * lost, e);
-  return __builtin_fmaf(-z, h, a < 0.0f ? 0.0f : a);
+  return __builtin_fmaf(-z, h, a < 0.0f ? a * -0.0f : a);
 }
 // (1 + tanh z) / 2 is 1 / (1 + exp(-2 z))
 __device__ __forceinline__ float gelu_tanh(float a) { return gated(a, 1.5957691216057308f * __builtin_fmaf(0.044715f * a * a, a, a)); }

@@ -363,6 +363,33 @@ def test_glu_large_and_non_finite_values(E, act):
     assert math.isnan(y[12]) and y[13] == math.inf and abs(y[14] - {"silu": 0.7310586, "gelu": 0.8413447, "gelu_tanh": 0.8411920}[act]) < 1e-6
 
 
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("dtype", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("bad", [-math.inf, math.nan])
+def test_glu_what_overflowed_below_shows_in_every_output(E, bad, dtype, act):
+    """-inf times 0 is a NaN for every activation: it shows in its own value of a wide output, and in
+    the scale of its block or row of a quantised one, the others as without it."""
+    a = torch.randn((5, 400), generator=torch.Generator().manual_seed(6)).to(TYPES[dtype]).cuda()
+    outs = ("fp32", "bf16", "fp16", "e4m3", "int8")
+    clean = [[t.clone() for t in glu_gpu(E, a, None, act, y)] for y in outs]
+    a[2, 131] = bad
+    keep = torch.ones((5, 400), dtype=torch.bool)
+    for y_name, (y0, s0) in zip(outs, clean):
+        y, s = glu_gpu(E, a, None, act, y_name)
+        if y_name in ("e4m3", "int8"):
+            block = 1 if y_name == "e4m3" else 0
+            assert torch.isnan(s[2, block])
+            other = torch.ones_like(s, dtype=torch.bool)
+            other[2, block] = False
+            assert torch.equal(s[other], s0[other])
+            keep[2] = False
+        else:
+            assert torch.isnan(y[2, 131])
+            keep[2, 131] = False
+        assert torch.equal(y[keep], y0[keep])
+        keep[2] = True
+
+
 # ---- all of them ------------------------------------------------------------------------------
 def test_row_operators_of_more_rows_than_a_grid_row_holds(E):
     """From 2^21 workgroups on a launch has more than one row of a grid: rows of a repeated batch get
