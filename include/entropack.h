@@ -621,10 +621,10 @@ int ep_kv8_attention(const ep_kv8_cache* cache, const ep_kv8_attn* call, void* d
  * nothing), so that what is made of it does not pass as finite.  d_x: m rows of k
  * elements (x_dtype EP_BF16, EP_FP16 or EP_FP32), x_row elements from one row to the
  * next (x_row >= k; 16-byte aligned rows); d_q: m x k codes, row-major, 16-byte
- * aligned; d_scale: m floats.  m may be 0 (nothing is done).
+ * aligned; d_scale: m floats.  Outputs overlap no input.  m may be 0 (nothing is done).
  * Asynchronous on hip_stream, no allocation, one launch.
  * Errors: EP_ERR_ARG (null or misaligned pointers, m outside 0 .. 2^31 - 1, k outside
- * 1 .. 65536, k % 16, x_row < k, another dtype), EP_ERR_HIP. */
+ * 1 .. 65536, k % 16, x_row < k, another dtype, d_q at d_x with more than one row), EP_ERR_HIP. */
 int ep_quant_i8_row(const void* d_x, int x_dtype, int64_t m, int64_t k, int64_t x_row, int8_t* d_q,
                     float* d_scale, void* hip_stream);
 
@@ -692,13 +692,14 @@ typedef struct {
  * (d_y_scale: m x ceil(n / 128)) as ep_quant_fp8_block with block_rows 1, EP_INT8 with a
  * scale for each row (d_y_scale: m) as ep_quant_i8_row.  Everything in between is FP32,
  * sums included; equal calls give equal bits.  A NaN or infinity changes its own row only.
- * d_y may be d_x itself where their types have one size and their rows one distance.
+ * d_y and d_res_out may be d_x or d_res itself where their types have one size and their
+ * rows one distance; outputs overlap no input otherwise, nor each other.
  * Rows of x, res, h and y and the vectors are 16-byte aligned.  m may be 0.
  * Asynchronous on hip_stream, no allocation, one launch.
  * Errors: EP_ERR_ARG (null or misaligned pointers, m outside 0 .. 2^31 - 1, n outside
  * 8 .. 65536, n % 8, or n % 16 with an 8-bit y, short or misaligned rows, a negative
  * group size or distance, another dtype or kind, eps or alpha out of range, nothing to
- * write), EP_ERR_HIP. */
+ * write, an output at an input whose rows lie otherwise or at the other output), EP_ERR_HIP. */
 int ep_norm(const ep_norm_call* call, void* hip_stream);
 
 enum ep_act {
@@ -713,11 +714,12 @@ enum ep_act {
  * m x n of y_dtype, row-major, 16-byte aligned, as ep_norm's y, with d_y_scale for 8-bit
  * ones.  Computed in FP32, rounded or quantised once.  A NaN stays one and act(-inf) is
  * one, as the formulas have it, in every y_dtype: an 8-bit y gets a NaN as its scale.
- * m may be 0 (nothing is done).
+ * d_y may be d_a or d_b itself where their types have one size and their rows one distance
+ * (n); it overlaps them in no other way.  m may be 0 (nothing is done).
  * Asynchronous on hip_stream, no allocation, one launch.
  * Errors: EP_ERR_ARG (null or misaligned pointers, m outside 0 .. 2^31 - 1, n outside
  * 8 .. 65536, n % 8, or n % 16 with an 8-bit y, short or misaligned rows, another dtype
- * or activation), EP_ERR_HIP. */
+ * or activation, d_y at d_a or d_b whose rows lie otherwise), EP_ERR_HIP. */
 int ep_glu(const void* d_a, const void* d_b, int x_dtype, int64_t m, int64_t n, int64_t a_row,
            int64_t b_row, int act, void* d_y, int y_dtype, float* d_y_scale, void* hip_stream);
 

@@ -564,6 +564,22 @@ bool misaligned(const void* p) { return reinterpret_cast<uintptr_t>(p) & 15; }
 bool wide_type(int t) { return t == EP_BF16 || t == EP_FP16 || t == EP_FP32; }
 bool off_row(int64_t row, int64_t n, int t) { return row < n || row % (t == EP_FP32 ? 4 : t == EP_BF16 || t == EP_FP16 ? 8 : 16); }
 
+int64_t size_of(int t) { return t == EP_FP32 ? 4 : t == EP_BF16 || t == EP_FP16 ? 2 : 1; }
+// Rows of an output of a call, or of an input.
+struct Rows {
+  const void* p;
+  int type;
+  int64_t row;   // elements from one to the next
+};
+// Whether an output at an input's address would be written over values that are still to be read: those
+// of another row, where the rows' distances in bytes differ, or of the same row by another thread, where
+// the types' sizes differ and a row is not read as a whole before any of it is written.
+bool clash(const Rows& out, const Rows& in, int64_t m, bool whole_first) {
+  if (!out.p || out.p != in.p) return false;
+  const int64_t a = size_of(out.type), b = size_of(in.type);
+  return (m > 1 && out.row * a != in.row * b) || (!whole_first && a != b);
+}
+
 // The distance of rows or vectors that are apart at all, in bytes, stays far from 2^63.
 constexpr int64_t kMostLd = (int64_t)1 << 40, kMostRows = 0x7FFFFFFF;
 
@@ -582,6 +598,7 @@ extern "C" int ep_quant_i8_row(const void* d_x, int x_dtype, int64_t m, int64_t 
   if (!d_x || !d_q || !d_scale) return fail(EP_ERR_ARG, "ep_quant_i8_row: null pointer");
   if (misaligned(d_x) || misaligned(d_q) || reinterpret_cast<uintptr_t>(d_scale) & 3)
     return fail(EP_ERR_ARG, "ep_quant_i8_row: x and q must be 16-byte aligned, scale by its elements");
+  if (clash({d_q, EP_INT8, k}, {d_x, x_dtype, x_row}, m, true)) return fail(EP_ERR_ARG, "ep_quant_i8_row: q at x, whose rows lie otherwise");
   const ActCall C = {d_x, nullptr, m, x_row, 0, 0, {d_q, d_scale, k, EP_INT8, (uint32_t)k}};
   act_launch<false>(C, x_dtype, static_cast<hipStream_t>(hip_stream));
   if (hipGetLastError() != hipSuccess) return fail(EP_ERR_HIP, "ep_quant_i8_row: launch failed");
@@ -603,6 +620,10 @@ extern "C" int ep_glu(const void* d_a, const void* d_b, int x_dtype, int64_t m, 
   if (!d_a || !d_y || (codes && !d_y_scale)) return fail(EP_ERR_ARG, "ep_glu: null pointer");
   if (misaligned(d_a) || misaligned(d_b) || misaligned(d_y) || (codes && reinterpret_cast<uintptr_t>(d_y_scale) & 3))
     return fail(EP_ERR_ARG, "ep_glu: a, b and y must be 16-byte aligned, scales by their elements");
+  const Rows y = {d_y, y_dtype, n};
+  const bool whole = y_dtype == EP_INT8;
+  if (clash(y, {d_a, x_dtype, a_row}, m, whole) || clash(y, {d_b, x_dtype, b_row}, m, whole))
+    return fail(EP_ERR_ARG, "ep_glu: y at a or b, whose rows lie otherwise");
   const ActCall C = {d_a, d_b, m, a_row, b_row, act, {d_y, d_y_scale, n, y_dtype, (uint32_t)n}};
   if (d_b) act_launch<true>(C, x_dtype, static_cast<hipStream_t>(hip_stream));
   else act_launch<false>(C, x_dtype, static_cast<hipStream_t>(hip_stream));
@@ -648,6 +669,10 @@ extern "C" int ep_norm(const ep_norm_call* call, void* hip_stream) {
     if (misaligned(p)) return fail(EP_ERR_ARG, "ep_norm: rows and vectors must be 16-byte aligned");
   if (normed && codes && reinterpret_cast<uintptr_t>(C.d_y_scale) & 3)
     return fail(EP_ERR_ARG, "ep_norm: scales must be aligned by their elements");
+  const Rows h = {C.d_res_out, C.res_dtype, C.res_out_row}, y = {normed ? C.d_y : nullptr, C.y_dtype, C.y_row};
+  for (const Rows& in : {Rows{C.d_x, C.x_dtype, C.x_row}, Rows{C.d_res, C.res_dtype, C.res_row}})
+    if (clash(h, in, C.m, false) || clash(y, in, C.m, true)) return fail(EP_ERR_ARG, "ep_norm: an output at an input whose rows lie otherwise");
+  if (y.p && y.p == h.p) return fail(EP_ERR_ARG, "ep_norm: y and the new stream in one place");
   const Shape s = shape_of(C.n);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   by_shape(s, [&](auto l, auto v) { hipLaunchKernelGGL((norm_kernel<l(), v()>), row_grid(C.m, s), dim3(s.threads), 0, stream, C); });

@@ -390,6 +390,31 @@ def test_glu_what_overflowed_below_shows_in_every_output(E, bad, dtype, act):
         keep[2] = True
 
 
+@pytest.mark.parametrize("dtype", ["bf16", "fp32"])
+@pytest.mark.parametrize("m,n", [(1, 640), (67, 136), (9, 5120), (3, 17408)])
+def test_row_operators_in_place_of_any_input(E, m, n, dtype):
+    """y over a or b, y over x or the stream, the new stream over x: as into buffers of their own."""
+    g = torch.Generator().manual_seed(n)
+    a, b = (torch.randn((m, n), generator=g).to(TYPES[dtype]).cuda() for _ in range(2))
+    act, name = E.ACT_GELU_TANH, code(E, dtype)
+    want = glu_gpu(E, a, b, "gelu_tanh", dtype)[0]
+    for i in range(2):
+        x = [a.clone(), b.clone()]
+        E.glu(x[0].data_ptr(), x[1].data_ptr(), name, m, n, act, x[i].data_ptr(), name, stream=stream())
+        assert torch.equal(x[i], want) and torch.equal(x[1 - i], (a, b)[1 - i])
+    h0, y0 = torch.empty_like(a), torch.empty_like(a)
+
+    def norm(x, r, h, y):
+        E.norm(E.norm_call(x.data_ptr(), m, n, x_dtype=name, res_dtype=name, y_dtype=name, d_res=r.data_ptr(), d_res_out=h.data_ptr(),
+                           d_y=y.data_ptr(), post=E.NORM_LAYER, pre=E.NORM_RMS, alpha=0.5), stream())
+
+    norm(a, b, h0, y0)
+    for ih, iy in ((0, 1), (1, 0), (0, 2), (2, 0), (1, 2), (2, 1)):
+        x = [a.clone(), b.clone(), torch.empty_like(a), torch.empty_like(a)]
+        norm(x[0], x[1], x[ih], x[iy] if iy < 2 else x[3])
+        assert torch.equal(x[ih], h0) and torch.equal(x[iy] if iy < 2 else x[3], y0), (ih, iy)
+
+
 # ---- all of them ------------------------------------------------------------------------------
 def test_row_operators_of_more_rows_than_a_grid_row_holds(E):
     """From 2^21 workgroups on a launch has more than one row of a grid: rows of a repeated batch get

@@ -96,6 +96,37 @@ def test_norm_refusals(E):
     E.norm(E.norm_call(0, 0, 256))                        # no rows: nothing to do
 
 
+def test_outputs_at_inputs_whose_rows_lie_otherwise(E):
+    """Such outputs would be written over values that other threads still read."""
+    quant = dict(x_dtype=E.BF16, m=2, k=256, d_scale=D)
+    refused(E, E.quant_i8_row, A, d_q=A, **quant)
+    refused(E, E.quant_i8_row, A, d_q=A, **{**quant, "x_dtype": E.FP32, "x_row": 512})
+    glu = dict(x_dtype=E.BF16, m=2, n=256, act=E.ACT_SILU, d_y_scale=F)
+    for at in (A, B):
+        refused(E, E.glu, A, B, d_y=at, y_dtype=E.BF16, a_row=512, b_row=512, **glu)      # a half of a fused projection's rows
+        refused(E, E.glu, A, B, d_y=at, y_dtype=E.FP32, **glu)
+        for y in (E.FP8_E4M3, E.INT8):
+            refused(E, E.glu, A, B, d_y=at, y_dtype=y, **glu)
+        refused(E, E.glu, A, B, d_y=at, y_dtype=E.FP8_E4M3, **{**glu, "m": 1})
+        refused(E, E.glu, A, B, d_y=at, y_dtype=E.FP32, **{**glu, "m": 1})
+
+    def norm(**kw):
+        E.norm(E.norm_call(**{**dict(d_x=A, m=2, n=256, d_res=B, d_res_out=D, d_y=F, d_y_scale=G), **kw}))
+
+    for at in (A, B):
+        refused(E, norm, d_y=at, y_dtype=E.FP32)
+        refused(E, norm, d_y=at, y_dtype=E.FP8_E4M3)
+        refused(E, norm, d_y=at, y_dtype=E.INT8)
+        refused(E, norm, d_y=at, y_row=512)
+    refused(E, norm, d_res_out=A, res_dtype=E.FP32)
+    refused(E, norm, d_res_out=A, res_dtype=E.FP32, m=1)
+    refused(E, norm, d_res_out=A, res_out_row=512)
+    refused(E, norm, d_res_out=A, x_row=512)
+    refused(E, norm, d_res=0, d_res_out=A, res_dtype=E.FP32, x_row=512, pre=E.NORM_NONE)     # rows at one distance, values not
+    refused(E, norm, d_y=D)
+    refused(E, norm, d_y=B, d_res_out=B)
+
+
 def test_rope_refusals(E):
     ok = dict(d_q=A, d_q_out=B, d_freqs=D, n_tokens=5, q_heads=8, head_dim=128, dtype=E.BF16, d_k=F, d_k_out=G, k_heads=2, d_pos=H)
 
