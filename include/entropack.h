@@ -647,7 +647,10 @@ int ep_gemm_i8_scaled(const int8_t* d_x, const float* d_x_scale, const int8_t* d
                       int64_t n, int64_t k, void* d_workspace, uint64_t ws_bytes, void* hip_stream);
 
 /* Device bytes ep_gemm_i8_scaled needs for these sizes on the current device (0 for bad
- * ones or where no device is present). */
+ * ones or where no device is present).  They do not grow with m: k is shared out where the
+ * rows make few tiles, so that a batch of many rows may need none and one of fewer rows tens of
+ * megabytes.  A workspace for calls of several sizes takes the largest of theirs; 1 MiB for
+ * each CU of the device (256 MiB on 256) is enough for any. */
 uint64_t ep_gemm_i8_scaled_workspace(int64_t m, int64_t n, int64_t k);
 
 /* ---- norms, residual sums, gated activations ---------------------------------- */

@@ -581,6 +581,7 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, int cus) {
   }
   return best;
 }
+// Bytes of a launch's partial sums.  At most 4 x cus tiles in all hold 65536 sums of 4 bytes: 1 MiB for each CU.
 uint64_t workspace_of(const Plan& plan, int64_t m, int64_t n) {
   return plan.parts > 1 ? (uint64_t)plan.parts * m * ((n + 3) / 4 * 4) * 4 : 0;
 }

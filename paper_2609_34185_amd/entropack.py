@@ -461,6 +461,8 @@ def quant_i8_row(d_x: int, x_dtype: int, m: int, k: int, d_q: int, d_scale: int,
 
 
 def gemm_i8_scaled_workspace(m: int, n: int, k: int) -> int:
+    """Bytes that gemm_i8_scaled needs for these sizes; fewer rows may need more.  1 MiB for each CU is
+    enough for all."""
     return int(lib().ep_gemm_i8_scaled_workspace(m, n, k))
 
 

@@ -215,3 +215,46 @@ def test_product_of_a_large_weight(E, m):
     assert torch.equal(y[:, -1000:], run(E, x, xs, w, ws, None, "bf16")) and (y[:, :-1000] == 0).all()
     del big, y
     torch.cuda.empty_cache()
+
+
+# sizes whose k is shared out over workgroups: the sums pass through a workspace, and a second launch joins them
+SHARED = [(203, 5120, 17408), (512, 5120, 17408), (1154, 2311, 16816), (455, 2089, 6320)]
+
+
+def shared(E, m, n, k):
+    """The workspace that these sizes need; a choice of kernel that needs none would leave a test without its subject."""
+    size = E.gemm_i8_scaled_workspace(m, n, k)
+    assert size > 0, "k is not shared out here any more: take other sizes"
+    return size
+
+
+@pytest.mark.parametrize("m,n,k", SHARED)
+def test_product_refuses_a_workspace_that_is_missing_short_or_misaligned(E, m, n, k):
+    """On the host, before anything is launched: the outputs stay as they were."""
+    size = shared(E, m, n, k)
+    x, xs, w, ws, b = inputs(m, n, k, 3)
+    room = torch.zeros(size + 16, dtype=torch.uint8, device="cuda")
+    y = torch.full((m, n), 7.0, dtype=torch.bfloat16, device="cuda")
+    for d_ws, ws_bytes in ((0, 0), (0, size), (room.data_ptr(), size - 1), (room.data_ptr(), 0), (room.data_ptr() + 8, size)):
+        with pytest.raises(E.EntroPackError) as e:
+            E.gemm_i8_scaled(x.data_ptr(), xs.data_ptr(), w.data_ptr(), ws.data_ptr(), y.data_ptr(), m, n, k, d_bias=b.data_ptr(), d_ws=d_ws,
+                             ws_bytes=ws_bytes, stream=stream())
+        assert e.value.code == E.ERR_ARG and "workspace" in str(e.value)
+    torch.cuda.synchronize()
+    assert (y == 7.0).all() and (room == 0).all()
+
+
+def test_product_one_workspace_for_any_size(E):
+    """1 MiB for each CU is enough whatever the sizes, which one batch's own need is not."""
+    most = torch.cuda.get_device_properties(0).multi_processor_count << 20
+    rng = np.random.default_rng(1)
+    for m, n, k in np.exp(rng.uniform(np.log((1, 1, 1)), np.log((20000, 20000, 8190)), (20000, 3))).astype(int).tolist():
+        assert E.gemm_i8_scaled_workspace(m, n, 16 * k) <= most
+    room = torch.empty(most, dtype=torch.uint8, device="cuda")
+    n, k = 2056, 8192
+    x, xs, w, ws, b = inputs(700, n, k, 4)
+    for m in (700, 300, 90, 20, 1):
+        y = torch.empty((m, n), dtype=torch.float32, device="cuda")
+        E.gemm_i8_scaled(x.data_ptr(), xs.data_ptr(), w.data_ptr(), ws.data_ptr(), y.data_ptr(), m, n, k, y_dtype=E.FP32, d_bias=b.data_ptr(),
+                         d_ws=room.data_ptr(), ws_bytes=most, stream=stream())
+        assert torch.equal(y, torch.from_numpy(reference(x[:m], xs[:m], w, ws, b)).cuda())
