@@ -26,6 +26,9 @@ inline Layout layout_of(uint32_t rows, uint32_t table_bytes, uint32_t n_tiles, u
   return L;
 }
 
+// Workgroups of a launch, and how many of them a CU takes in all.
+inline int64_t rounds(int64_t groups, int cus) { return (groups + cus - 1) / cus; }
+
 // Records a thread-local message for ep_last_error and returns code.
 int fail(int code, const char* msg);
 

@@ -68,8 +68,5 @@ __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p, int64_t
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), (short)0, (int)bytes, 0x00020000);
 }
 
-// Workgroups of a launch, and how many of them a CU takes in all.
-inline int64_t rounds(int64_t groups, int cus) { return (groups + cus - 1) / cus; }
-
 }  // namespace
 }  // namespace ep

@@ -220,6 +220,18 @@ def test_product_of_a_large_weight(E, m):
 # sizes whose k is shared out over workgroups: the sums pass through a workspace, and a second launch joins them
 SHARED = [(203, 5120, 17408), (512, 5120, 17408), (1154, 2311, 16816), (455, 2089, 6320)]
 
+# and paths that none of the sizes above takes: 256 x 128 tiles with k shared out, 256 x 256 tiles in several rounds without
+# pieces, 192 x 128 tiles in halves after whole rounds (and as many tiles as CUs), 32 rows streamed in several rounds
+# (test_i8_plan.py holds these lists to the choice)
+PATHS = [(2221, 389, 9840), (685, 1998, 32192), (255, 5251, 49344), (2065, 13441, 1296), (2317, 12974, 3088), (598, 14405, 16),
+         (844, 10266, 384), (1943, 3055, 1840), (18, 12503, 16), (63, 17723, 17184)]
+
+
+@pytest.mark.parametrize("y_name", ["bf16", "fp16", "fp32"])
+@pytest.mark.parametrize("m,n,k", PATHS + SHARED)
+def test_product_matches_definition_on_every_path(E, m, n, k, y_name):
+    test_product_matches_definition(E, m, n, k, y_name)
+
 
 def shared(E, m, n, k):
     """The workspace that these sizes need; a choice of kernel that needs none would leave a test without its subject."""
