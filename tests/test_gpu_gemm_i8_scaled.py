@@ -270,3 +270,52 @@ def test_product_one_workspace_for_any_size(E):
         E.gemm_i8_scaled(x.data_ptr(), xs.data_ptr(), w.data_ptr(), ws.data_ptr(), y.data_ptr(), m, n, k, y_dtype=E.FP32, d_bias=b.data_ptr(),
                          d_ws=room.data_ptr(), ws_bytes=most, stream=stream())
         assert torch.equal(y, torch.from_numpy(reference(x[:m], xs[:m], w, ws, b)).cuda())
+
+
+@pytest.mark.parametrize("m,n,k", SHARED)
+def test_products_with_shared_k_in_a_graph(E, m, n, k):
+    """Both launches captured, twice over one workspace, and replayed over other operands, with whatever
+    the workspace and the outputs held before."""
+    size = shared(E, m, n, k)
+    x, xs, w, ws, b = inputs(m, n, k, 6)
+    want = run(E, x, xs, w, ws, b, "bf16").clone()
+    other = run(E, x, xs, w, ws, None, "fp32").clone()
+    y, z, room = torch.empty_like(want), torch.empty_like(other), torch.empty(size, dtype=torch.uint8, device="cuda")
+
+    def call():
+        for out, dtype, bias in ((y, E.BF16, b.data_ptr()), (z, E.FP32, 0)):
+            E.gemm_i8_scaled(x.data_ptr(), xs.data_ptr(), w.data_ptr(), ws.data_ptr(), out.data_ptr(), m, n, k, y_dtype=dtype, d_bias=bias,
+                             d_ws=room.data_ptr(), ws_bytes=size, stream=stream())
+
+    side, graph = torch.cuda.Stream(), torch.cuda.CUDAGraph()
+    torch.cuda.synchronize()
+    with torch.cuda.graph(graph, stream=side):
+        call()
+    for i in range(4):
+        x.copy_(torch.roll(x, 1, 1))
+        w.copy_(torch.roll(w, 1, 1))        # the same sums, every operand moved
+        y.fill_(3)
+        z.fill_(-3)
+        room.fill_(0x5B + 17 * i)
+        call() if i == 2 else graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(y, want) and torch.equal(z, other), i
+
+
+def test_products_with_shared_k_at_once(E):
+    """Calls of several streams side by side, each with a workspace of its own that other calls have
+    filled: the same bits as alone."""
+    calls = []
+    for i, (m, n, k) in enumerate(SHARED):
+        x, xs, w, ws, b = inputs(m, n, k, 60 + i)
+        want = run(E, x, xs, w, ws, b, "bf16").clone()
+        room = torch.full((shared(E, m, n, k),), 0x7F, dtype=torch.uint8, device="cuda")
+        calls.append((torch.cuda.Stream(), x, xs, w, ws, b, want, torch.zeros((6, m, n), dtype=torch.bfloat16, device="cuda"), room))
+    torch.cuda.synchronize()
+    for turn in range(6):
+        for (m, n, k), (s, x, xs, w, ws, b, _, y, room) in zip(SHARED, calls):
+            E.gemm_i8_scaled(x.data_ptr(), xs.data_ptr(), w.data_ptr(), ws.data_ptr(), y[turn].data_ptr(), m, n, k, d_bias=b.data_ptr(),
+                             d_ws=room.data_ptr(), ws_bytes=room.numel(), stream=s.cuda_stream)
+    torch.cuda.synchronize()
+    for call in calls:
+        assert all(torch.equal(y, call[6]) for y in call[7])
