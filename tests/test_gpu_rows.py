@@ -390,6 +390,41 @@ def test_glu_what_overflowed_below_shows_in_every_output(E, bad, dtype, act):
         keep[2] = True
 
 
+@pytest.mark.parametrize("gated", [False, True])
+@pytest.mark.parametrize("act", ["silu", "gelu", "gelu_tanh"])
+def test_glu_error_by_its_steps(E, act, gated):
+    """FP32 to FP32, in units of 2^-24 of the value; an operation that rounds adds one.
+    exp: its argument's fraction of a power of two is off by 2^-24, 0.7 units of the result, and the instruction
+    by one of its last places, 2: 2.7.  Reciprocal: an instruction within 2^-23, a step that squares that, and a
+    rounding: 1.01.  Logistic function of Z, off by dz: 1 / (1 + e) is off by (2.7 + dz) e / (1 + e) + 1 + 1.01, the
+    product adds 1; for Z < 0 the numerator is a e, another 1 and 2.7 + dz in all, of which 1 + e takes a share back.
+    SiLU: Z is exact.  By tanh: Z = c a (1 + d a^2) has two rounded constants and four operations, 6 of |Z| at most.
+    GELU: |a| Phi(-|a|) = |a| exp(-a^2 / 2) P(t), t = 1 / (1 + 0.24 |a|) off by 2.01 and P by 3.33 times that where it is
+    steepest, at 0: 6.7; P's Horner steps 3.9 there, what P leaves out of the function 0.6, exp 2.7, three products
+    and the last one 4: 17.9, less further out.  Above 0 it is taken from a: Phi(-a) / Phi(a) of 16.9, and 1.
+    The other factor adds 1.  Where a step's result is below FP32's normal range it is off by 2^-150."""
+    g = torch.Generator().manual_seed(12)
+    far = torch.logspace(-44, 4, 16384, dtype=torch.float64)
+    a = torch.cat((torch.linspace(-15, 15, 32768, dtype=torch.float64), far, -far)).float()[None]
+    b = torch.randn(a.shape, generator=g) if gated else None
+    y, _ = glu_gpu(E, a.cuda(), None if b is None else b.cuda(), act, "fp32")
+    x = a.double().numpy()
+    with np.errstate(over="ignore"):
+        want = act_ref(x, act)
+        z = 2 * math.sqrt(2 / math.pi) * (x + 0.044715 * x ** 3) if act == "gelu_tanh" else x
+        e = np.exp(-np.abs(z))
+    if act == "gelu":
+        below = np.array([0.5 * math.erfc(abs(v) * math.sqrt(0.5)) for v in x.reshape(-1)]).reshape(x.shape)   # Phi(-|a|)
+        units = np.where(x < 0, 17.9, 1 + 16.9 * below / (1 - below))
+    else:
+        dz = 2.7 + (6 * np.abs(z) if act == "gelu_tanh" else 0)
+        units = np.where(x < 0, dz + 4.01, dz * e / (1 + e) + 3.01)
+    other = 1.0 if b is None else b.double().numpy()
+    tol = (units + gated) * 2.0 ** -24 * np.abs(want * other) * (1 + 2.0 ** -18) + 2.0 ** -150 * (4 * (1 + np.abs(x)) * np.abs(other) + 1)
+    off = np.abs(y.double().cpu().numpy() - want * other)
+    assert (off <= tol).all()
+
+
 @pytest.mark.parametrize("dtype", ["bf16", "fp32"])
 @pytest.mark.parametrize("m,n", [(1, 640), (67, 136), (9, 5120), (3, 17408)])
 def test_row_operators_in_place_of_any_input(E, m, n, dtype):
