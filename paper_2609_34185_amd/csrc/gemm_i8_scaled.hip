@@ -232,8 +232,8 @@ __global__ __launch_bounds__(64 * KW) void ring_kernel(Product P, uint32_t heigh
 
 // The tile of Y at row i0 of X and j0 of W.  Wave (ww, wx) of WW x WX owns NW x NX tiles of
 // 16 x 16; NS stages of operands are in LDS, written by direct loads.  203 x 5120 x 17408 in tiles of
-// 192 x 128 and 4 shares of k: 30 us, of which 25 are the 131 MB that come from memory (W, X for each XCD, and some of
-// W for its second tile of X) and 3 the sums' 17 MB; the matrix unit is busy a quarter of the cycles and LDS 15 %.
+// 192 x 128 and 4 shares of k, on a card where the whole call takes 37.6 us: 30, of which 25 are the 131 MB that come from
+// memory (W, X for each XCD, and some of W for its second tile of X) and 3 the sums' 17 MB; the matrix unit is busy a quarter of the cycles and LDS 15 %.
 // More of W in flight and less of X, by waves of their own for each, takes 5 us more.
 template <int OUT, int NW, int NX, int WW, int WX, int NS>
 __device__ __forceinline__ void tile_product(const Product& P, uint32_t part, int64_t i0, int64_t j0, lds_u8* lds) {
@@ -332,8 +332,8 @@ __device__ __forceinline__ void tile_product(const Product& P, uint32_t part, in
 
 // Units [0, full) are whole tiles; the `split` last tiles are taken in `cut` pieces each, so that a last round
 // of few tiles is a short one: halves of W's rows, or quarters of half the rows of both.  Every unit is taken by
-// `parts` workgroups, one for each share of k, which follow each other on one XCD: they read the same rows of W
-// or X.
+// `parts` workgroups, one for each share of k, which follow each other on one XCD.  They read other columns of the same
+// rows, so that nothing is shared between them, and every XCD reads all of X.
 struct Units {
   uint32_t tw, tx, full, split, cut;
   // The unit and the share of k of this workgroup; whole tiles and pieces are spread over the XCDs apart.
@@ -422,7 +422,8 @@ __global__ __launch_bounds__(i8::kGemmThreads) void large_kernel(Product P, Unit
 }
 
 // The parts' sums, scales, bias and rounding: a thread for four columns of a row.  Four parts of 203 x 5120, 17 MB,
-// in 6 us, most of it the launch.
+// in 6 us, most of it the launch.  What a workspace held before the call does not matter, so that there is no cleared
+// counter by which the last workgroup of a tile could know itself and join in the same launch.
 template <int OUT>
 __global__ __launch_bounds__(256) void join_kernel(Product P) {
   const uint32_t per_row = (uint32_t)(P.sums_ld / 4), id = blockIdx.x * 256 + threadIdx.x;   // below 2^31

@@ -82,7 +82,8 @@ struct Plan {
 };
 
 // A launch of few tiles shares k out over workgroups, whose sums another launch joins.
-// 203 x 5120 x 17408 in tiles of 192 x 128, 54 of them: 37.6 us in 4 parts, 70.6 in one; in 128 x 256, 40 of them: 37.9 in 5.
+// 203 x 5120 x 17408 in tiles of 192 x 128, 54 of them, on a card where that takes 37.6 us in 4 parts: 70.6 in one; in
+// 128 x 256, 40 of them: 37.9 in 5.  Cards differ by more than that: 33 to 39.
 Plan plan_of(int64_t m, int64_t n, int64_t k, int cus) {
   const uint32_t kb = (uint32_t)((k + 127) / 128);
   if (m <= 16) return {kRing16, 1, kb, ring_height<2, 1>(m, n, cus)};
@@ -127,7 +128,8 @@ Plan plan_of(int64_t m, int64_t n, int64_t k, int cus) {
   return best;
 }
 
-// Bytes of a launch's partial sums.  At most 4 x cus tiles in all hold 65536 sums of 4 bytes: 1 MiB for each CU.
+// Bytes of a launch's partial sums.  Where k is shared out, tiles times parts are at most 4 x cus, of up to 65536 sums of
+// 4 bytes each: 1 MiB for each CU.
 uint64_t workspace_of(const Plan& plan, int64_t m, int64_t n) {
   return plan.parts > 1 ? (uint64_t)plan.parts * m * ((n + 3) / 4 * 4) * 4 : 0;
 }
