@@ -793,8 +793,8 @@ typedef struct {
  * Errors: EP_ERR_ARG (null pointers or ones off their elements, n_tokens outside 0 .. 2^31
  * - 1, n_req outside 1 .. 2^31 - 2 without d_pos, heads outside 1 .. 65536 (0 for keys),
  * head_dim outside 2 .. 1024, a rotated part that is odd, empty or beyond it, short rows,
- * another layout or dtype, an output at its input with another distance of rows, amplitude
- * that is not finite), EP_ERR_HIP. */
+ * another layout or dtype, an output at its input with another distance of rows or at the
+ * other's input or output, amplitude that is not finite), EP_ERR_HIP. */
 int ep_rope(const ep_rope_call* call, void* hip_stream);
 
 /* ---- errors -------------------------------------------------------------- */

@@ -275,6 +275,8 @@ extern "C" int ep_rope(const ep_rope_call* call, void* hip_stream) {
     return fail(EP_ERR_ARG, "ep_rope: pointers off their elements");
   if ((C.d_q == C.d_q_out && C.q_row != C.q_out_row) || (C.k_heads && C.d_k == C.d_k_out && C.k_row != C.k_out_row))
     return fail(EP_ERR_ARG, "ep_rope: a rotation in place needs one distance of rows");
+  if (C.k_heads && (C.d_q_out == C.d_k || C.d_k_out == C.d_q || C.d_q_out == C.d_k_out))
+    return fail(EP_ERR_ARG, "ep_rope: an output at the other's input or output");
   R.heads = (uint32_t)(C.q_heads + C.k_heads);
   const hipStream_t stream = static_cast<hipStream_t>(hip_stream);
   if (C.dtype == EP_BF16) launch<__bf16>(R, stream);

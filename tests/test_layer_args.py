@@ -148,6 +148,13 @@ def test_rope_refusals(E):
     call(n_tokens=0, d_q=0, d_q_out=0, d_k=0, d_k_out=0, d_freqs=0)
 
 
+def test_rope_outputs_at_the_other_ones_rows(E):
+    """Queries turned into the keys' rows or the reverse, or both into one place: heads that are still to be read."""
+    ok = dict(d_q=A, d_q_out=B, d_freqs=D, n_tokens=5, q_heads=2, head_dim=128, dtype=E.BF16, d_k=F, d_k_out=G, k_heads=2, d_pos=H)
+    for bad in (dict(d_q_out=F), dict(d_k_out=A), dict(d_k_out=B), dict(d_q_out=F, d_k_out=A)):
+        refused(E, E.rope, E.rope_call(**{**ok, **bad}))
+
+
 def test_rope_freqs_refusals(E):
     ok = dict(rot_dim=64, base=1e4, stretch=E.ROPE_TURNS, factor=4.0, trained_len=4096.0, low=1.0, high=4.0)
     for bad in (dict(rot_dim=0), dict(rot_dim=3), dict(rot_dim=1026), dict(base=0.5), dict(base=1e19), dict(base=NAN), dict(stretch=-1),
