@@ -319,3 +319,34 @@ def test_products_with_shared_k_at_once(E):
     torch.cuda.synchronize()
     for call in calls:
         assert all(torch.equal(y, call[6]) for y in call[7])
+
+
+def test_product_of_a_large_batch(E):
+    """X of more than 2^31 bytes: the last rows get what they get alone."""
+    n, k = 200, 4096
+    m = (1 << 31) // k + 700
+    x, xs, w, ws, b = inputs(1000, n, k, 9)
+    big, bxs = torch.zeros((m, k), dtype=torch.int8, device="cuda"), torch.ones(m, device="cuda")
+    big[-1000:], bxs[-1000:] = x, xs
+    y = run(E, big, bxs, w, ws, None, "bf16")
+    assert torch.equal(y[-1000:], run(E, x, xs, w, ws, None, "bf16")) and (y[:-1000] == 0).all()
+    del big, y
+    torch.cuda.empty_cache()
+
+
+@pytest.mark.parametrize("m,n", [(70000, 65604), (260, 1 << 24), (1 << 24, 260), (16, 1 << 24)])
+def test_product_of_a_large_output(E, m, n):
+    """Y of more than 2^32 elements, and as many rows or columns as there may be: every element."""
+    if torch.cuda.mem_get_info()[0] < 3 * m * n + (8 << 30):
+        pytest.skip("needs more device memory")
+    x, xs, w, ws, _ = inputs(m, n, 16, 10)
+    y = torch.empty((m, n), dtype=torch.bfloat16, device="cuda")
+    room = torch.empty(E.gemm_i8_scaled_workspace(m, n, 16) + 16, dtype=torch.uint8, device="cuda")
+    E.gemm_i8_scaled(x.data_ptr(), xs.data_ptr(), w.data_ptr(), ws.data_ptr(), y.data_ptr(), m, n, 16, d_ws=room.data_ptr(),
+                     ws_bytes=room.numel(), stream=stream())
+    step = max(1, (1 << 27) // n)
+    for i in range(0, m, step):
+        want = (x[i: i + step].float() @ w.float().t()) * xs[i: i + step, None] * ws       # sums of 16 products: exact
+        assert torch.equal(y[i: i + step], want.to(torch.bfloat16)), i
+    del y
+    torch.cuda.empty_cache()
